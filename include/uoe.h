@@ -246,6 +246,63 @@ uoe_status uoe_smha_backward(const uoe_problem* prob, const void* x, const void*
                              float* dWq, float* dWk, float* dWv, float* dWo, float* dW_r,
                              void* ws, size_t ws_bytes, void* cuda_stream);
 
+/*
+ * 8-bit operands.  A matrix is held as e4m3 values (1 sign, 4 exponent, 3 mantissa bits, largest value 448) and a float32
+ * scale for each block of UOE_FP8_BLOCK elements of a row, or of UOE_FP8_BLOCK x UOE_FP8_BLOCK elements; an element stands for
+ * value * scale.  The axis that a product contracts is contiguous and padded with zeros to whole blocks.
+ *
+ * uoe_fp8_quantize: G matrices x [G, R, C] (float32 or bfloat16) in one of four layouts; Cp, Rp: C, R rounded up to UOE_FP8_BLOCK,
+ * Cb, Rb: the number of blocks.
+ *   UOE_FP8_ROWS      q [G, R, Cp], scale [G, Cb, R]     a scale per row and 128 columns: activations and gradients as rows of a product
+ *   UOE_FP8_COLS      q [G, C, Rp], scale [G, Rb, C]     the same of the transposed matrix: operands of uoe_fp8_wgrad
+ *   UOE_FP8_BLOCKS    q [G, R, Cp], scale [G, Rb, Cb]    a scale per 128 x 128 block: weights, contracted over their columns
+ *   UOE_FP8_BLOCKS_T  q [G, C, Rp], scale [G, Cb, Rb]    the same of the transposed matrices: weights [n, d, d_e], contracted over d
+ * The scale of a block is the smallest power of two s with max |x| <= 448 s (max |x| taken as at least 2^-100), a value is
+ * x / s rounded to e4m3 (nearest, ties to even).  A block that holds an infinity or NaN gets the scale NaN and zeros as values.
+ * All pointers are device pointers.
+ */
+#define UOE_FP8_BLOCK 128
+typedef enum { UOE_FP8_ROWS = 0, UOE_FP8_COLS = 1, UOE_FP8_BLOCKS = 2, UOE_FP8_BLOCKS_T = 3 } uoe_fp8_layout;
+uoe_status uoe_fp8_quantize(int32_t G, int32_t R, int32_t C, int32_t dtype, int32_t layout, const void* x, void* q, float* scale,
+                            void* cuda_stream);
+
+/* A product of 8-bit operands.  Any sizes >= 1; n <= 32. */
+typedef struct {
+    int32_t n;        /* experts */
+    int32_t M;        /* rows of the result (uoe_fp8_gemm: of all regions, padding included) */
+    int32_t N;        /* columns of the result */
+    int32_t K;        /* contraction (uoe_fp8_wgrad: rows of all regions, padding included) */
+    int32_t dtype;    /* uoe_dtype of the result; uoe_fp8_wgrad: UOE_F32 */
+} uoe_fp8_problem;
+
+/* Bytes of device workspace of the two products (0 on an invalid problem).  Prepared with uoe_workspace_init like any other. */
+size_t uoe_fp8_workspace_bytes(const uoe_fp8_problem* prob);
+
+/*
+ * Expert products on 8-bit operands (the products of Eq. 38-39 and, with the weights quantised the other way round, of their
+ * gradients with respect to the rows):
+ *   C[r, j] = sum over blocks b of  a_scale[b, r] * w_scale[e, j / 128, b] * sum over k in b of  A[r, k] * W[e, j, k]
+ * for the rows r of expert e's region, products and sums in float32.
+ *   A [M, Kp], a_scale [Kb, M]: UOE_FP8_ROWS of the rows.   W [n, N, Kp], w_scale [n, Nb, Kb]: UOE_FP8_BLOCKS of [n, N, K] or
+ *   UOE_FP8_BLOCKS_T of [n, K, N].   Scales may be any float32 numbers.
+ *   expert_offsets [n+1]: multiples of UOE_ROW_ALIGN, ascending, at most M ("Routed buffers" above); rows of a region's padding are
+ *   computed like any other, rows from expert_offsets[n] on are left as they were.  NULL with n = 1: all M rows.  Offsets of
+ *   another form are reported in the workspace's status word (UOE_ERR_DEVICE_INDEX) and nothing is computed.
+ *   C [M, N] in prob->dtype.
+ */
+uoe_status uoe_fp8_gemm(const uoe_fp8_problem* prob, const void* A, const float* a_scale, const void* W, const float* w_scale,
+                        const int32_t* expert_offsets, void* C, void* ws, size_t ws_bytes, void* cuda_stream);
+
+/*
+ * Weight gradients from 8-bit operands:
+ *   dW[e, i, j] = sum over blocks b of 128 rows of expert e's region of  a_scale[b, i] * b_scale[b, j] * sum over r in b of A[i, r] * B[j, r]
+ *   A [M, Kp], a_scale [Kb, M] and B [N, Kp], b_scale [Kb, N]: UOE_FP8_COLS of the routed inputs [K, M] and of the gradients [K, N].
+ *   Every region is whole blocks; its padding rows must be zeros in A or B.  expert_offsets as above (at most K rounded up to a block).
+ *   dW [n, M, N] float32; zeros for an expert without rows.
+ */
+uoe_status uoe_fp8_wgrad(const uoe_fp8_problem* prob, const void* A, const float* a_scale, const void* B, const float* b_scale,
+                         const int32_t* expert_offsets, float* dW, void* ws, size_t ws_bytes, void* cuda_stream);
+
 /* Device arrays written by a router (shapes as for uoe_route).  A set is complete or absent as a whole. */
 typedef struct {
     int32_t* expert_idx;      /* [B,k] */

@@ -22,6 +22,8 @@ ACTS = {"gelu_erf": 0, "gelu_tanh": 1, "silu": 2, "identity": 3}
 UOE_FLAG_RESIDUAL, UOE_FLAG_GATE, UOE_FLAG_CAUSAL, UOE_FLAG_DYNAMIC_C, UOE_FLAG_GENERAL_PATH = 1, 2, 4, 8, 16
 UOE_OP_ROUTE, UOE_OP_MLP_FWD, UOE_OP_MLP_BWD, UOE_OP_SMHA_FWD, UOE_OP_SMHA_BWD = 0, 1, 2, 3, 4
 UOE_OP_BALANCE_BWD = 5
+UOE_FP8_BLOCK = 128
+FP8_LAYOUTS = {"rows": 0, "cols": 1, "blocks": 2, "blocks_t": 3}
 
 
 class UoeError(RuntimeError):
@@ -38,6 +40,27 @@ class _Problem(ctypes.Structure):
     _fields_ = [(f, ctypes.c_int32) for f in
                 ("B", "L", "L_valid", "d", "n", "k", "m", "c", "d_e", "H", "d_h", "dtype", "act")] + \
                [("flags", ctypes.c_uint32), ("d_rope", ctypes.c_int32)]
+
+
+class _Fp8Problem(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in ("n", "M", "N", "K", "dtype")]
+
+
+@dataclass
+class Fp8Problem:
+    """Mirror of the C struct uoe_fp8_problem: a product of 8-bit operands (dtype: of the result)."""
+    n: int
+    M: int
+    N: int
+    K: int
+    dtype: str = "bf16"
+
+    def c_struct(self) -> _Fp8Problem:
+        return _Fp8Problem(self.n, self.M, self.N, self.K, UOE_BF16 if self.dtype == "bf16" else UOE_F32)
+
+    @property
+    def torch_dtype(self):
+        return torch.bfloat16 if self.dtype == "bf16" else torch.float32
 
 
 @dataclass
@@ -112,6 +135,14 @@ def _load():
     lib.uoe_route_balance.argtypes = [pp, f32p, ctypes.c_float, f32p, i32p, i32p, vp]
     lib.uoe_route_balance_backward.restype = ctypes.c_int
     lib.uoe_route_balance_backward.argtypes = [pp, vp, vp, f32p, ctypes.c_float, f32p, vp, f32p, vp, sz, vp]
+    p8, i32 = ctypes.POINTER(_Fp8Problem), ctypes.c_int32
+    lib.uoe_fp8_quantize.restype = ctypes.c_int
+    lib.uoe_fp8_quantize.argtypes = [i32, i32, i32, i32, i32, vp, vp, f32p, vp]
+    lib.uoe_fp8_workspace_bytes.restype = sz
+    lib.uoe_fp8_workspace_bytes.argtypes = [p8]
+    for f in (lib.uoe_fp8_gemm, lib.uoe_fp8_wgrad):
+        f.restype = ctypes.c_int
+        f.argtypes = [p8, vp, f32p, vp, f32p, i32p, vp, vp, sz, vp]
     lib.uoe_block_workspace_bytes.restype = sz
     lib.uoe_block_workspace_bytes.argtypes = [pp, pp]
     lib.uoe_block_forward.restype = ctypes.c_int
@@ -367,6 +398,89 @@ def uoe_route_balance_backward(prob: Problem, x, W_r, p_patch, alpha: float, dlo
     if check:
         _check(uoe_read_device_status(ws), "uoe_route_balance_backward (device)")
     return dx, dW_r
+
+
+def uoe_fp8_quantize(x, layout: str, q=None, scale=None):
+    """(q float8_e4m3fn, scale float32) of x [R,C] or [G,R,C] in layout "rows", "cols", "blocks" or "blocks_t" (see uoe.h)."""
+    assert x.dim() in (2, 3) and x.dtype in (torch.float32, torch.bfloat16), "x must be [R,C] or [G,R,C], float32 or bfloat16"
+    if layout not in FP8_LAYOUTS:
+        raise ValueError(f"layout must be one of {sorted(FP8_LAYOUTS)}")
+    _contig(x)
+    R, C = x.shape[-2:]
+    blk = lambda v: -(-v // UOE_FP8_BLOCK)
+    lead = x.shape[:-2]
+    rows, inner = (R, C) if layout in ("rows", "blocks") else (C, R)      # of the stored matrix
+    shape = (*lead, rows, blk(inner) * UOE_FP8_BLOCK)
+    s_shape = (*lead, blk(inner), rows) if layout in ("rows", "cols") else (*lead, blk(rows), blk(inner))
+    q = q if q is not None else torch.empty(shape, dtype=torch.float8_e4m3fn, device=x.device)
+    scale = scale if scale is not None else torch.empty(s_shape, dtype=torch.float32, device=x.device)
+    _contig(q, torch.float8_e4m3fn)
+    _contig(scale, torch.float32)
+    assert tuple(q.shape) == shape and tuple(scale.shape) == s_shape, f"expected q {shape} and scale {s_shape}"
+    st = _lib.uoe_fp8_quantize(lead[0] if lead else 1, R, C, UOE_BF16 if x.dtype == torch.bfloat16 else UOE_F32, FP8_LAYOUTS[layout],
+                               _ptr(x), _ptr(q), _ptr(scale), _stream())
+    _check(st, "uoe_fp8_quantize")
+    return q, scale
+
+
+def uoe_fp8_workspace_bytes(prob: Fp8Problem) -> int:
+    return int(_lib.uoe_fp8_workspace_bytes(ctypes.byref(prob.c_struct())))
+
+
+def alloc_fp8_workspace(prob: Fp8Problem, device="cuda") -> torch.Tensor:
+    nbytes = uoe_fp8_workspace_bytes(prob)
+    if nbytes == 0:
+        raise UoeError(1, "uoe_fp8_workspace_bytes")
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with torch.cuda.device(ws.device):
+        _check(_lib.uoe_workspace_init(_ptr(ws), nbytes, _stream()), "uoe_workspace_init")
+    return ws
+
+
+def _fp8_operand(t, scale, shape, s_shape):
+    _contig(t, torch.float8_e4m3fn)
+    _contig(scale, torch.float32)
+    assert t.numel() == shape[0] * shape[1] * shape[2] and scale.numel() == s_shape[0] * s_shape[1] * s_shape[2], \
+        f"expected values {shape} and scales {s_shape}, got {tuple(t.shape)} and {tuple(scale.shape)}"
+
+
+def uoe_fp8_gemm(prob: Fp8Problem, A, a_scale, W, w_scale, expert_offsets=None, C=None, ws=None, check: bool = True):
+    """C [M,N] = rows A times the weights of each row's expert (8-bit operands, see uoe.h).  Without C a new tensor is returned, zero
+    behind the last region."""
+    blk = lambda v: -(-v // UOE_FP8_BLOCK)
+    Kb, Nb = blk(prob.K), blk(prob.N)
+    _fp8_operand(A, a_scale, (1, prob.M, Kb * UOE_FP8_BLOCK), (1, Kb, prob.M))
+    _fp8_operand(W, w_scale, (prob.n, prob.N, Kb * UOE_FP8_BLOCK), (prob.n, Nb, Kb))
+    _contig(expert_offsets, torch.int32)
+    if C is None:
+        C = (torch.empty if expert_offsets is None else torch.zeros)(prob.M, prob.N, dtype=prob.torch_dtype, device=A.device)
+    _contig(C, prob.torch_dtype)
+    assert C.numel() == prob.M * prob.N and (expert_offsets is None or expert_offsets.numel() == prob.n + 1)
+    ws = ws if ws is not None else alloc_fp8_workspace(prob, A.device)
+    st = _lib.uoe_fp8_gemm(ctypes.byref(prob.c_struct()), _ptr(A), _ptr(a_scale), _ptr(W), _ptr(w_scale), _ptr(expert_offsets), _ptr(C),
+                           _ptr(ws), ws.numel(), _stream())
+    _check(st, "uoe_fp8_gemm")
+    if check:
+        _check(uoe_read_device_status(ws), "uoe_fp8_gemm (device)")
+    return C
+
+
+def uoe_fp8_wgrad(prob: Fp8Problem, A, a_scale, B, b_scale, expert_offsets=None, dW=None, ws=None, check: bool = True):
+    """dW [n,M,N] float32 = A B^T over the rows of each expert's region (8-bit operands, see uoe.h)."""
+    Kb = -(-prob.K // UOE_FP8_BLOCK)
+    _fp8_operand(A, a_scale, (1, prob.M, Kb * UOE_FP8_BLOCK), (1, Kb, prob.M))
+    _fp8_operand(B, b_scale, (1, prob.N, Kb * UOE_FP8_BLOCK), (1, Kb, prob.N))
+    _contig(expert_offsets, torch.int32)
+    dW = dW if dW is not None else torch.empty(prob.n, prob.M, prob.N, dtype=torch.float32, device=A.device)
+    _contig(dW, torch.float32)
+    assert dW.numel() == prob.n * prob.M * prob.N and (expert_offsets is None or expert_offsets.numel() == prob.n + 1)
+    ws = ws if ws is not None else alloc_fp8_workspace(prob, A.device)
+    st = _lib.uoe_fp8_wgrad(ctypes.byref(prob.c_struct()), _ptr(A), _ptr(a_scale), _ptr(B), _ptr(b_scale), _ptr(expert_offsets), _ptr(dW),
+                            _ptr(ws), ws.numel(), _stream())
+    _check(st, "uoe_fp8_wgrad")
+    if check:
+        _check(uoe_read_device_status(ws), "uoe_fp8_wgrad (device)")
+    return dW
 
 
 def uoe_block_workspace_bytes(att: Problem | None, mlp: Problem | None) -> int:

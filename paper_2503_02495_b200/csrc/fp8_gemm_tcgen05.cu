@@ -1,0 +1,441 @@
+// Products of 8-bit operands with a scale per block of 128 (fp8.cuh) on the tcgen05 tensor cores, grouped by expert:
+//
+//   rows    C[r, j]    = sum_kb sa[kb, r] sb[e(r), j / 128, kb]  sum_{k in block kb} A[r, k] B[e(r), j, k]
+//   wgrad   C[e, i, j] = sum_kb sa[kb, i] sb[kb, j]              sum_{r in block kb} A[i, r] B[j, r],   kb over expert e's region
+//
+// The tensor cores form one block's product at a time (K = 128: four instructions) in TMEM, and eight warps add it, times its
+// scales, to accumulators in registers: the scales are any float32 numbers, and the sum over blocks is float32 arithmetic.
+// A persistent CTA per SM walks the 128 x BN tiles:
+//   warp 0      TMA producer: a stage is one block, 128 x 128 bytes of A and BN x 128 of B (128-byte rows, swizzled)
+//   warp 1      MMA issuer: a block's product into one of two TMEM accumulators, which the other warps empty in turn
+//   warps 4..11 a warp has 32 rows (its TMEM lane quarter) and half of the columns: one row's BN / 2 sums per thread.  The
+//               columns are one block of B's scales, so a thread's factor is one number per block; the rows' scales are one line
+//               per warp and block, asked for two blocks ahead.
+// Regions of experts are whole 128-row tiles, so no tile straddles two experts, and in wgrad no block does.
+#include "fp8.cuh"
+#include "tc.cuh"
+#include "tmap.cuh"
+
+namespace uoe {
+namespace {
+
+using namespace tc;
+
+constexpr int BM = 128;
+constexpr int kMaxExperts = 32;
+
+template <int BN> struct Cfg {
+    static constexpr int A_BYTES = BM * kQ, B_BYTES = BN * kQ, STAGE = A_BYTES + B_BYTES;
+    static constexpr int STAGES = BN == 256 ? 4 : 6;
+    static constexpr int CW = BN / 2;                 // columns of an accumulating warp
+    static constexpr int EPI_WARPS = 8, THREADS = 128 + 32 * EPI_WARPS;
+    static constexpr int TMEM_COLS = 2 * BN;
+    static constexpr int SB_BYTES = EPI_WARPS * CW * 4;        // wgrad: the columns' scales of a block, a copy per warp
+    static constexpr int CTL_BYTES = 1024;
+    static constexpr int SMEM = STAGES * STAGE + 1024 /* alignment */ + CTL_BYTES + SB_BYTES;
+};
+
+struct Ctl {
+    uint64_t full[8], empty[8], tfull[2], tempty[2];
+    uint32_t tmem_base;
+    int abort_flag;
+    int bad;                                          // offsets that are no regions: nothing is computed
+    int offs[kMaxExperts + 1];
+    int tstart[kMaxExperts + 1];                      // first row tile of each expert
+};
+static_assert(sizeof(Ctl) <= 1024, "control block");
+
+struct Fp8Args {
+    const float *sa, *sb;
+    const int* offsets;
+    int n, N, Nb;                     // columns of C, blocks of 128 of them
+    long long M;                      // rows of C (rows of the A operand)
+    int Kb;                           // blocks of the contraction (wgrad: in all regions together)
+    void* C;
+    int out_bf16, vec;                // vec: rows of C may be stored in 32-byte pieces
+    const __nv_bfloat16* bias;
+    int act;
+    uint8_t* q;
+    float* qs;
+    long long ldq;
+    int* status;
+};
+
+// phi with errors of float32 size (the result is compared with a rounding border of its own)
+__device__ __forceinline__ float act_precise(float h, int act) {
+    switch (act) {
+        case UOE_ACT_SILU: return __fdividef(h, 1.0f + __expf(-h));
+        case UOE_ACT_GELU_TANH: {
+            const float u = 0.79788456080286536f * (h + 0.044715f * h * h * h);
+            return __fdividef(h, 1.0f + __expf(-2.0f * u));             // h/2 (1 + tanh u)
+        }
+        default: return act_apply(h, act);
+    }
+}
+
+template <int BN, bool WGRAD, int EPI>
+__global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
+fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ Fp8Args a) {
+    pdl_trigger();
+    using Cf = Cfg<BN>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    Ctl* ctl = (Ctl*)(smem + Cf::STAGES * Cf::STAGE);
+    volatile int* abort_flag = &ctl->abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int n = a.n;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < Cf::STAGES; ++s) { mbar_init(&ctl->full[s], 1); mbar_init(&ctl->empty[s], 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&ctl->tfull[i], 1); mbar_init(&ctl->tempty[i], Cf::EPI_WARPS); }
+        ctl->abort_flag = 0;
+        fence_barrier_init();
+        prefetch_tmap(&tmA);
+        prefetch_tmap(&tmB);
+    }
+    if (warp == 1) tmem_alloc(&ctl->tmem_base, Cf::TMEM_COLS);
+    pdl_wait();
+    // tiles of the rows: per expert its 128-row blocks; without offsets all rows are one expert's; wgrad: every expert has all of C
+    const int m_tiles = (int)((a.M + BM - 1) / BM);
+    if (warp == 2) {
+        const long long limit = WGRAD ? (long long)a.Kb * kQ : a.M;
+        int o = 0, o1 = 0;
+        if (a.offsets) {
+            o = lane < n ? a.offsets[lane] : 0;
+            o1 = lane < n ? a.offsets[lane + 1] : 0;
+        } else if (lane == 0) {
+            o1 = WGRAD ? a.Kb * kQ : m_tiles * BM;
+        }
+        const bool ok = lane >= n || !a.offsets || (o >= 0 && o1 >= o && o1 <= limit && ((o | o1) & (BM - 1)) == 0);
+        const bool bad = !__all_sync(0xffffffffu, ok);
+        const int tiles = lane < n && !bad ? (WGRAD ? m_tiles : (o1 - o) / BM) : 0;
+        int incl = tiles;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, d);
+            if (lane >= d) incl += v;
+        }
+        if (lane < n) {
+            ctl->offs[lane] = o;
+            ctl->offs[lane + 1] = o1;                 // (the neighbour writes the same number)
+            ctl->tstart[lane] = incl - tiles;
+            if (lane == n - 1) ctl->tstart[n] = incl;
+        }
+        if (lane == 0 && bad) set_status(a.status, UOE_ERR_DEVICE_INDEX);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = ctl->tmem_base;
+    const int n_tiles = (a.N + BN - 1) / BN;
+    const int total = ctl->tstart[n] * n_tiles;
+
+    // tile -> expert, first row of A and C, first block of the contraction and their number
+    auto locate = [&](int tile, int& e, int& row0, int& col0, int& kb0, int& kbs) {
+        const int rt = tile / n_tiles;
+        while (e + 1 < n && rt >= ctl->tstart[e + 1]) ++e;
+        row0 = (rt - ctl->tstart[e]) * BM + (WGRAD ? 0 : ctl->offs[e]);
+        col0 = (tile - rt * n_tiles) * BN;
+        kb0 = WGRAD ? ctl->offs[e] / kQ : 0;
+        kbs = WGRAD ? (ctl->offs[e + 1] - ctl->offs[e]) / kQ : a.Kb;
+    };
+
+    // Registers: 384 threads start with 168 each; the first warpgroup gives 128 of its up, the accumulating ones take 64 more
+    // (128 * 40 + 256 * 232 = 384 * 168).
+    if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    else asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+    if (warp == 0) {
+        int stage = 0, e = 0;
+        uint32_t phase = 0, issued = 0, issued_parity = 0;
+        bool stop = false;
+        for (int tile = blockIdx.x; tile < total && !stop; tile += gridDim.x) {
+            int row0, col0, kb0, kbs;
+            locate(tile, e, row0, col0, kb0, kbs);
+            for (int kb = 0; kb < kbs; ++kb) {
+                if (!mbar_wait_warp(&ctl->empty[stage], phase ^ 1, abort_flag, a.status)) { stop = true; break; }
+                if (lane == 0) {
+                    uint8_t* st = smem + stage * Cf::STAGE;
+                    mbar_arrive_expect_tx(&ctl->full[stage], Cf::STAGE);
+                    tma_load_2d(st, &tmA, (kb0 + kb) * kQ, row0, &ctl->full[stage]);
+                    tma_load_3d(st + Cf::A_BYTES, &tmB, (kb0 + kb) * kQ, col0, WGRAD ? 0 : e, &ctl->full[stage]);
+                }
+                __syncwarp();
+                issued |= 1u << stage;
+                issued_parity = (issued_parity & ~(1u << stage)) | (phase << stage);
+                if (++stage == Cf::STAGES) { stage = 0; phase ^= 1; }
+            }
+        }
+        if (lane == 0 && *abort_flag)                 // copies in flight land before the CTA exits
+            for (int s = 0; s < Cf::STAGES; ++s)
+                if (issued & (1u << s)) mbar_wait(&ctl->full[s], (issued_parity >> s) & 1, abort_flag, a.status);
+    } else if (warp == 1) {
+        const uint32_t el = elect_one();
+        constexpr uint32_t idesc = instr_desc_e4m3(BM, BN);
+        int stage = 0, acc = 0, e = 0;
+        uint32_t phase = 0, acc_phase = 0;
+        bool stop = false;
+        for (int tile = blockIdx.x; tile < total && !stop; tile += gridDim.x) {
+            int row0, col0, kb0, kbs;
+            locate(tile, e, row0, col0, kb0, kbs);
+            for (int kb = 0; kb < kbs; ++kb) {
+                if (!mbar_wait_warp(&ctl->tempty[acc], acc_phase ^ 1, abort_flag, a.status) ||
+                    !mbar_wait_warp(&ctl->full[stage], phase, abort_flag, a.status)) { stop = true; break; }
+                tc_fence_after();
+                const uint32_t st = smem_u32(smem + stage * Cf::STAGE);
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks)
+                    mma_f8(el, tmem_base + acc * BN, smem_desc(st + ks * 32, 16, 1024), smem_desc(st + Cf::A_BYTES + ks * 32, 16, 1024), idesc, ks != 0);
+                mma_commit(el, &ctl->empty[stage]);
+                mma_commit(el, &ctl->tfull[acc]);
+                if (++stage == Cf::STAGES) { stage = 0; phase ^= 1; }
+                if (++acc == 2) { acc = 0; acc_phase ^= 1; }
+            }
+        }
+    } else if (warp >= 4) {
+        constexpr int CW = Cf::CW;
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        [[maybe_unused]] float* s_sb = (float*)((uint8_t*)ctl + Cf::CTL_BYTES) + (warp - 4) * CW;
+        int acc = 0, e = 0;
+        uint32_t acc_phase = 0;
+        bool stop = false;
+        for (int tile = blockIdx.x; tile < total && !stop; tile += gridDim.x) {
+            int row0, col0, kb0, kbs;
+            locate(tile, e, row0, col0, kb0, kbs);
+            const long long row = row0 + quarter * 32 + lane;
+            const int col = col0 + half * CW;
+            const bool row_ok = row < a.M;
+            unsigned long long sum[CW / 2];
+#pragma unroll
+            for (int q = 0; q < CW / 2; ++q) sum[q] = 0ull;
+            // scale of block kb: the row's, times the column block's; asked for two blocks ahead
+            const float* sa = a.sa + (size_t)kb0 * a.M + row;
+            const float* sb = WGRAD ? a.sb + (size_t)kb0 * a.N : a.sb + ((size_t)e * a.Nb + min(col / kQ, a.Nb - 1)) * a.Kb;
+            auto row_scale = [&](int kb) { return row_ok && kb < kbs ? __ldg(sa + (size_t)kb * a.M) : 0.f; };
+            auto col_scale = [&](int kb) { return !WGRAD && kb < kbs ? __ldg(sb + kb) : 1.f; };
+            float ra0 = row_scale(0), ca0 = col_scale(0), ra1 = row_scale(1), ca1 = col_scale(1);
+            float cs0[CW / 32], cs1[CW / 32];                    // wgrad: this lane's columns' scales, a block ahead
+            auto cols_of = [&](int kb, float* cs) {
+#pragma unroll
+                for (int q = 0; q < CW / 32; ++q) {
+                    const int c = col + q * 32 + lane;
+                    cs[q] = WGRAD && kb < kbs && c < a.N ? __ldg(sb + (size_t)kb * a.N + c) : 0.f;
+                }
+            };
+            if constexpr (WGRAD) cols_of(0, cs0);
+            for (int kb = 0; kb < kbs; ++kb) {
+                const float f = ra0 * ca0;
+                ra0 = ra1; ca0 = ca1;
+                ra1 = row_scale(kb + 2); ca1 = col_scale(kb + 2);
+                if constexpr (WGRAD) {
+                    __syncwarp();
+#pragma unroll
+                    for (int q = 0; q < CW / 32; ++q) s_sb[q * 32 + lane] = cs0[q];
+                    __syncwarp();
+                    cols_of(kb + 1, cs1);
+#pragma unroll
+                    for (int q = 0; q < CW / 32; ++q) cs0[q] = cs1[q];
+                }
+                if (!mbar_wait_warp(&ctl->tfull[acc], acc_phase, abort_flag, a.status)) { stop = true; break; }
+                tc_fence_after();
+                const uint32_t taddr = tmem_base + acc * BN + half * CW + ((uint32_t)(quarter * 32) << 16);
+                const unsigned long long f2 = f2_pack(f, f);
+                uint32_t v[2][16];
+                tmem_ld16(taddr, v[0]);
+#pragma unroll
+                for (int g = 0; g < CW / 16; ++g) {
+                    tmem_ld_wait();
+                    if (g + 1 < CW / 16) tmem_ld16(taddr + (g + 1) * 16, v[(g + 1) & 1]);
+                    else {                                       // the last of them is in registers: the accumulator is free
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&ctl->tempty[acc]);
+                    }
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        const unsigned long long t = f2_pack(__uint_as_float(v[g & 1][2 * q]), __uint_as_float(v[g & 1][2 * q + 1]));
+                        if constexpr (WGRAD) {
+                            const float2 c2 = *(const float2*)(s_sb + g * 16 + 2 * q);
+                            f2_fma(sum[g * 8 + q], t, f2_mul(f2, f2_pack(c2.x, c2.y)));
+                        } else {
+                            f2_fma(sum[g * 8 + q], t, f2);
+                        }
+                    }
+                }
+                if (++acc == 2) { acc = 0; acc_phase ^= 1; }
+            }
+            if (stop) break;
+            if (!row_ok || col >= a.N) continue;
+            if constexpr (EPI == kFp8ActQuant) {
+                static_assert(EPI != kFp8ActQuant || (!WGRAD && CW == kQ), "a thread holds one block of the result");
+                uint32_t m = 0;
+#pragma unroll
+                for (int q = 0; q < CW / 2; ++q) {
+                    float2 h = f2_unpack(sum[q]);
+                    const int c = col + 2 * q;
+                    if (a.bias) {
+                        if (c < a.N) h.x += to_f32(a.bias[(size_t)e * a.N + c]);
+                        if (c + 1 < a.N) h.y += to_f32(a.bias[(size_t)e * a.N + c + 1]);
+                    }
+                    h.x = act_precise(h.x, a.act);
+                    h.y = act_precise(h.y, a.act);
+                    m = max(m, max(abs_bits(h.x), abs_bits(h.y)));
+                    sum[q] = f2_pack(h.x, h.y);
+                }
+                const BlockScale b = block_scale(m);
+                a.qs[(size_t)(col / kQ) * a.M + row] = b.s;
+                uint8_t* o = a.q + (size_t)row * a.ldq + col;
+#pragma unroll
+                for (int q = 0; q < CW / 2; q += 16) {
+                    uint32_t w[8];
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) {
+                        const float2 x = f2_unpack(sum[q + 2 * u]), y = f2_unpack(sum[q + 2 * u + 1]);
+                        w[u] = e4m3x4(x.x, x.y, y.x, y.y, b.inv);
+                    }
+                    st_sector(o + 2 * q, make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]), sector_aligned(o));
+                }
+            } else {
+                const size_t at = ((WGRAD ? (size_t)e * a.M : 0) + row) * a.N + col;
+                if (a.bias) {
+#pragma unroll
+                    for (int q = 0; q < CW / 2; ++q) {
+                        float2 h = f2_unpack(sum[q]);
+                        const int c = col + 2 * q;
+                        if (c < a.N) h.x += to_f32(a.bias[(size_t)e * a.N + c]);
+                        if (c + 1 < a.N) h.y += to_f32(a.bias[(size_t)e * a.N + c + 1]);
+                        sum[q] = f2_pack(h.x, h.y);
+                    }
+                }
+                if (a.out_bf16) {
+                    __nv_bfloat16* o = (__nv_bfloat16*)a.C + at;
+                    const bool whole = sector_aligned(o);
+#pragma unroll
+                    for (int q = 0; q < CW / 2; q += 8) {
+                        uint32_t w[8];
+#pragma unroll
+                        for (int u = 0; u < 8; ++u) { const float2 h = f2_unpack(sum[q + u]); w[u] = pack_bf16x2(h.x, h.y); }
+                        if (a.vec && col + 2 * q + 16 <= a.N) {
+                            st_sector(o + 2 * q, make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]), whole);
+                        } else {
+#pragma unroll
+                            for (int u = 0; u < 16; ++u)
+                                if (col + 2 * q + u < a.N) ((uint16_t*)o)[2 * q + u] = (uint16_t)(w[u >> 1] >> (16 * (u & 1)));
+                        }
+                    }
+                } else {
+                    float* o = (float*)a.C + at;
+                    const bool whole = sector_aligned(o);
+#pragma unroll
+                    for (int q = 0; q < CW / 2; q += 4) {
+                        float h[8];
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) { const float2 t = f2_unpack(sum[q + u]); h[2 * u] = t.x; h[2 * u + 1] = t.y; }
+                        if (a.vec && col + 2 * q + 8 <= a.N) {
+                            st_sector(o + 2 * q, pack16<float>(h), pack16<float>(h + 4), whole);
+                        } else {
+#pragma unroll
+                            for (int u = 0; u < 8; ++u)
+                                if (col + 2 * q + u < a.N) o[2 * q + u] = h[u];
+                        }
+                    }
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        __syncwarp();
+        tmem_dealloc(tmem_base, Cf::TMEM_COLS);
+    }
+}
+
+template <int BN, bool WGRAD, int EPI>
+uoe_status launch_one(const Fp8Gemm& g, int* status, cudaStream_t s) {
+    using Cf = Cfg<BN>;
+    static DeviceOnce once;
+    auto kern = fp8_gemm_kernel<BN, WGRAD, EPI>;
+    const uoe_status st = smem_opt_in(once, kern, Cf::SMEM);
+    if (st != UOE_OK) return st;
+    const uint64_t Kp = (uint64_t)((g.K + kQ - 1) / kQ * kQ);
+    CUtensorMap tmA, tmB;
+    {
+        const uint64_t dims[2] = {Kp, (uint64_t)g.M};
+        const uint64_t str[1] = {Kp};
+        const uint32_t box[2] = {kQ, BM};
+        if (!make_tmap(&tmA, g.A, 2, dims, str, box, CU_TENSOR_MAP_DATA_TYPE_UINT8)) return UOE_ERR_CUDA;
+    }
+    {
+        const uint64_t dims[3] = {Kp, (uint64_t)g.N, (uint64_t)(g.wgrad ? 1 : g.n)};
+        const uint64_t str[2] = {Kp, Kp * (uint64_t)g.N};
+        const uint32_t box[3] = {kQ, BN, 1};
+        if (!make_tmap(&tmB, g.B, 3, dims, str, box, CU_TENSOR_MAP_DATA_TYPE_UINT8)) return UOE_ERR_CUDA;
+    }
+    Fp8Args a = {};
+    a.sa = g.sa; a.sb = g.sb; a.offsets = g.offsets;
+    a.n = g.n; a.N = g.N; a.Nb = q_blocks(g.N); a.M = g.M; a.Kb = (int)(Kp / kQ);
+    a.C = g.C; a.out_bf16 = g.out_bf16;
+    a.vec = ((size_t)g.N * (g.out_bf16 ? 2 : 4)) % 16 == 0 && aligned16(g.C);
+    a.bias = (const __nv_bfloat16*)g.bias; a.act = g.act;
+    a.q = (uint8_t*)g.q; a.qs = g.qs; a.ldq = q_pad(g.N);
+    a.status = status;
+    const long long m_tiles = (g.M + BM - 1) / BM, n_tiles = (g.N + BN - 1) / BN;
+    const long long tiles = m_tiles * n_tiles * (g.wgrad ? g.n : 1);
+    if (tiles > 0x3fffffffll) return UOE_ERR_UNSUPPORTED;
+    const int grid = (int)(tiles < sm_count() ? tiles : sm_count());
+    ProfScope ps(g.label, s);
+    launch_k(kern, dim3(grid), dim3(Cf::THREADS), (size_t)Cf::SMEM, s, tmA, tmB, a);
+    UOE_LAUNCHED();
+    return UOE_OK;
+}
+
+}  // namespace
+
+uoe_status launch_fp8_gemm(const Fp8Gemm& g, int* status, cudaStream_t s) {
+    if (g.n > kMaxExperts) return UOE_ERR_UNSUPPORTED;
+    if (g.epi == kFp8ActQuant) return launch_one<256, false, kFp8ActQuant>(g, status, s);
+    const long long tiles256 = (g.M + BM - 1) / BM * ((g.N + 255) / 256) * (g.wgrad ? g.n : 1);
+    const bool wide = g.N > 128 && tiles256 >= sm_count();
+    if (g.wgrad) return wide ? launch_one<256, true, kFp8Store>(g, status, s) : launch_one<128, true, kFp8Store>(g, status, s);
+    return wide ? launch_one<256, false, kFp8Store>(g, status, s) : launch_one<128, false, kFp8Store>(g, status, s);
+}
+
+}  // namespace uoe
+
+using namespace uoe;
+
+namespace {
+uoe_status fp8_check(const uoe_fp8_problem* p, const void* A, const float* sa, const void* B, const float* sb, const int32_t* offsets, const void* C,
+                     const void* ws, size_t ws_bytes) {
+    if (!p || p->n < 1 || p->M < 1 || p->N < 1 || p->K < 1) return UOE_ERR_INVALID_ARG;
+    if (p->dtype != UOE_F32 && p->dtype != UOE_BF16) return UOE_ERR_INVALID_ARG;
+    if (!A || !sa || !B || !sb || !C || !ws) return UOE_ERR_INVALID_ARG;
+    if (!aligned16(A) || !aligned16(sa) || !aligned16(B) || !aligned16(sb) || !aligned16(C) || !aligned16(ws)) return UOE_ERR_INVALID_ARG;
+    if (!offsets && p->n > 1) return UOE_ERR_INVALID_ARG;
+    if (p->n > kMaxExperts || p->M > (1 << 30) || p->N > (1 << 30) || p->K > (1 << 30)) return UOE_ERR_UNSUPPORTED;
+    if (ws_bytes < uoe_fp8_workspace_bytes(p)) return UOE_ERR_WORKSPACE;
+    return UOE_OK;
+}
+}  // namespace
+
+extern "C" size_t uoe_fp8_workspace_bytes(const uoe_fp8_problem* p) {
+    if (!p || p->n < 1 || p->M < 1 || p->N < 1 || p->K < 1) return 0;
+    return kStatusBytes;
+}
+
+extern "C" uoe_status uoe_fp8_gemm(const uoe_fp8_problem* p, const void* A, const float* a_scale, const void* W, const float* w_scale,
+                                   const int32_t* expert_offsets, void* C, void* ws, size_t ws_bytes, void* cuda_stream) {
+    const uoe_status st = fp8_check(p, A, a_scale, W, w_scale, expert_offsets, C, ws, ws_bytes);
+    if (st != UOE_OK) return st;
+    Fp8Gemm g{A, a_scale, W, w_scale, expert_offsets, p->n, p->M, p->N, p->K, false, C, p->dtype == UOE_BF16};
+    return launch_fp8_gemm(g, (int*)ws, (cudaStream_t)cuda_stream);
+}
+
+extern "C" uoe_status uoe_fp8_wgrad(const uoe_fp8_problem* p, const void* A, const float* a_scale, const void* B, const float* b_scale,
+                                    const int32_t* expert_offsets, float* dW, void* ws, size_t ws_bytes, void* cuda_stream) {
+    const uoe_status st = fp8_check(p, A, a_scale, B, b_scale, expert_offsets, dW, ws, ws_bytes);
+    if (st != UOE_OK) return st;
+    if (p->dtype != UOE_F32) return UOE_ERR_UNSUPPORTED;
+    Fp8Gemm g{A, a_scale, B, b_scale, expert_offsets, p->n, p->M, p->N, p->K, true, dW, false};
+    g.label = "fp8_wgrad";
+    return launch_fp8_gemm(g, (int*)ws, (cudaStream_t)cuda_stream);
+}
