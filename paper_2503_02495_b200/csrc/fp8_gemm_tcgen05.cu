@@ -141,56 +141,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
 
     // Registers: 384 threads start with 168 each; the first warpgroup gives 128 of its up, the accumulating ones take 64 more
     // (128 * 40 + 256 * 232 = 384 * 168).
-    if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-    else asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
-    if (warp == 0) {
-        int stage = 0, e = 0;
-        uint32_t phase = 0, issued = 0, issued_parity = 0;
-        bool stop = false;
-        for (int tile = blockIdx.x; tile < total && !stop; tile += gridDim.x) {
-            int row0, col0, kb0, kbs;
-            locate(tile, e, row0, col0, kb0, kbs);
-            for (int kb = 0; kb < kbs; ++kb) {
-                if (!mbar_wait_warp(&ctl->empty[stage], phase ^ 1, abort_flag, a.status)) { stop = true; break; }
-                if (lane == 0) {
-                    uint8_t* st = smem + stage * Cf::STAGE;
-                    mbar_arrive_expect_tx(&ctl->full[stage], Cf::STAGE);
-                    tma_load_2d(st, &tmA, (kb0 + kb) * kQ, row0, &ctl->full[stage]);
-                    tma_load_3d(st + Cf::A_BYTES, &tmB, (kb0 + kb) * kQ, col0, WGRAD ? 0 : e, &ctl->full[stage]);
-                }
-                __syncwarp();
-                issued |= 1u << stage;
-                issued_parity = (issued_parity & ~(1u << stage)) | (phase << stage);
-                if (++stage == Cf::STAGES) { stage = 0; phase ^= 1; }
-            }
-        }
-        if (lane == 0 && *abort_flag)                 // copies in flight land before the CTA exits
-            for (int s = 0; s < Cf::STAGES; ++s)
-                if (issued & (1u << s)) mbar_wait(&ctl->full[s], (issued_parity >> s) & 1, abort_flag, a.status);
-    } else if (warp == 1) {
-        const uint32_t el = elect_one();
-        constexpr uint32_t idesc = instr_desc_e4m3(BM, BN);
-        int stage = 0, acc = 0, e = 0;
-        uint32_t phase = 0, acc_phase = 0;
-        bool stop = false;
-        for (int tile = blockIdx.x; tile < total && !stop; tile += gridDim.x) {
-            int row0, col0, kb0, kbs;
-            locate(tile, e, row0, col0, kb0, kbs);
-            for (int kb = 0; kb < kbs; ++kb) {
-                if (!mbar_wait_warp(&ctl->tempty[acc], acc_phase ^ 1, abort_flag, a.status) ||
-                    !mbar_wait_warp(&ctl->full[stage], phase, abort_flag, a.status)) { stop = true; break; }
-                tc_fence_after();
-                const uint32_t st = smem_u32(smem + stage * Cf::STAGE);
-#pragma unroll
-                for (int ks = 0; ks < 4; ++ks)
-                    mma_f8(el, tmem_base + acc * BN, smem_desc(st + ks * 32, 16, 1024), smem_desc(st + Cf::A_BYTES + ks * 32, 16, 1024), idesc, ks != 0);
-                mma_commit(el, &ctl->empty[stage]);
-                mma_commit(el, &ctl->tfull[acc]);
-                if (++stage == Cf::STAGES) { stage = 0; phase ^= 1; }
-                if (++acc == 2) { acc = 0; acc_phase ^= 1; }
-            }
-        }
-    } else if (warp >= 4) {
+    if (warp >= 4) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
         constexpr int CW = Cf::CW;
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         [[maybe_unused]] float* s_sb = (float*)((uint8_t*)ctl + Cf::CTL_BYTES) + (warp - 4) * CW;
@@ -337,6 +289,56 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                                 if (col + 2 * q + u < a.N) o[2 * q + u] = h[u];
                         }
                     }
+                }
+            }
+        }
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (warp == 0) {
+            int stage = 0, e = 0;
+            uint32_t phase = 0, issued = 0, issued_parity = 0;
+            bool stop = false;
+            for (int tile = blockIdx.x; tile < total && !stop; tile += gridDim.x) {
+                int row0, col0, kb0, kbs;
+                locate(tile, e, row0, col0, kb0, kbs);
+                for (int kb = 0; kb < kbs; ++kb) {
+                    if (!mbar_wait_warp(&ctl->empty[stage], phase ^ 1, abort_flag, a.status)) { stop = true; break; }
+                    if (lane == 0) {
+                        uint8_t* st = smem + stage * Cf::STAGE;
+                        mbar_arrive_expect_tx(&ctl->full[stage], Cf::STAGE);
+                        tma_load_2d(st, &tmA, (kb0 + kb) * kQ, row0, &ctl->full[stage]);
+                        tma_load_3d(st + Cf::A_BYTES, &tmB, (kb0 + kb) * kQ, col0, WGRAD ? 0 : e, &ctl->full[stage]);
+                    }
+                    __syncwarp();
+                    issued |= 1u << stage;
+                    issued_parity = (issued_parity & ~(1u << stage)) | (phase << stage);
+                    if (++stage == Cf::STAGES) { stage = 0; phase ^= 1; }
+                }
+            }
+            if (lane == 0 && *abort_flag)                 // copies in flight land before the CTA exits
+                for (int s = 0; s < Cf::STAGES; ++s)
+                    if (issued & (1u << s)) mbar_wait(&ctl->full[s], (issued_parity >> s) & 1, abort_flag, a.status);
+        } else if (warp == 1) {
+            const uint32_t el = elect_one();
+            constexpr uint32_t idesc = instr_desc_e4m3(BM, BN);
+            int stage = 0, acc = 0, e = 0;
+            uint32_t phase = 0, acc_phase = 0;
+            bool stop = false;
+            for (int tile = blockIdx.x; tile < total && !stop; tile += gridDim.x) {
+                int row0, col0, kb0, kbs;
+                locate(tile, e, row0, col0, kb0, kbs);
+                for (int kb = 0; kb < kbs; ++kb) {
+                    if (!mbar_wait_warp(&ctl->tempty[acc], acc_phase ^ 1, abort_flag, a.status) ||
+                        !mbar_wait_warp(&ctl->full[stage], phase, abort_flag, a.status)) { stop = true; break; }
+                    tc_fence_after();
+                    const uint32_t st = smem_u32(smem + stage * Cf::STAGE);
+#pragma unroll
+                    for (int ks = 0; ks < 4; ++ks)
+                        mma_f8(el, tmem_base + acc * BN, smem_desc(st + ks * 32, 16, 1024), smem_desc(st + Cf::A_BYTES + ks * 32, 16, 1024), idesc, ks != 0);
+                    mma_commit(el, &ctl->empty[stage]);
+                    mma_commit(el, &ctl->tfull[acc]);
+                    if (++stage == Cf::STAGES) { stage = 0; phase ^= 1; }
+                    if (++acc == 2) { acc = 0; acc_phase ^= 1; }
                 }
             }
         }
