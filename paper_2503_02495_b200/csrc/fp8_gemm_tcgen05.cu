@@ -8,9 +8,9 @@
 // A persistent CTA per SM walks the 128 x BN tiles:
 //   warp 0      TMA producer: a stage is one block, 128 x 128 bytes of A and BN x 128 of B (128-byte rows, swizzled)
 //   warp 1      MMA issuer: a block's product into one of two TMEM accumulators, which the other warps empty in turn
+//   warp 2      the scales of the blocks to come, by 4-byte asynchronous copies (their rows start anywhere) into a ring of their own
 //   warps 4..11 a warp has 32 rows (its TMEM lane quarter) and half of the columns: one row's BN / 2 sums per thread.  The
-//               columns are one block of B's scales, so a thread's factor is one number per block; the rows' scales are one line
-//               per warp and block, asked for two blocks ahead.
+//               columns are one block of B's scales, so a thread's factor is one number per block.
 // Regions of experts are whole 128-row tiles, so no tile straddles two experts, and in wgrad no block does.
 #include "fp8.cuh"
 #include "tc.cuh"
@@ -23,20 +23,29 @@ using namespace tc;
 
 constexpr int BM = 128;
 constexpr int kMaxExperts = 32;
-
+constexpr int kScaleSlots = 8;
 template <int BN> struct Cfg {
     static constexpr int A_BYTES = BM * kQ, B_BYTES = BN * kQ, STAGE = A_BYTES + B_BYTES;
     static constexpr int STAGES = BN == 256 ? 4 : 6;
     static constexpr int CW = BN / 2;                 // columns of an accumulating warp
     static constexpr int EPI_WARPS = 8, THREADS = 128 + 32 * EPI_WARPS;
     static constexpr int TMEM_COLS = 2 * BN;
-    static constexpr int SB_BYTES = EPI_WARPS * CW * 4;        // wgrad: the columns' scales of a block, a copy per warp
+    static constexpr int SCALES = BM + BN;            // floats of a block's scales: the rows', then the columns' (or column blocks')
     static constexpr int CTL_BYTES = 1024;
-    static constexpr int SMEM = STAGES * STAGE + 1024 /* alignment */ + CTL_BYTES + SB_BYTES;
+    static constexpr int SMEM = STAGES * STAGE + 1024 /* alignment */ + CTL_BYTES + kScaleSlots * SCALES * 4;
 };
 
+// four bytes, zero where `real` is false (the address is a valid one all the same)
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, bool real) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" :: "r"(dst), "l"(src), "r"(real ? 4 : 0) : "memory");
+}
+// one arrival of this thread on the barrier when all its copies so far have landed (counted in the barrier's 32)
+__device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" :: "r"(smem_u32(bar)) : "memory");
+}
+
 struct Ctl {
-    uint64_t full[8], empty[8], tfull[2], tempty[2];
+    uint64_t full[8], empty[8], tfull[2], tempty[2], sfull[kScaleSlots], sempty[kScaleSlots];
     uint32_t tmem_base;
     int abort_flag;
     int bad;                                          // offsets that are no regions: nothing is computed
@@ -87,6 +96,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     if (threadIdx.x == 0) {
         for (int s = 0; s < Cf::STAGES; ++s) { mbar_init(&ctl->full[s], 1); mbar_init(&ctl->empty[s], 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(&ctl->tfull[i], 1); mbar_init(&ctl->tempty[i], Cf::EPI_WARPS); }
+        for (int i = 0; i < kScaleSlots; ++i) { mbar_init(&ctl->sfull[i], 32); mbar_init(&ctl->sempty[i], Cf::EPI_WARPS); }
         ctl->abort_flag = 0;
         fence_barrier_init();
         prefetch_tmap(&tmA);
@@ -126,6 +136,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = ctl->tmem_base;
+    float* s_scales = (float*)((uint8_t*)ctl + Cf::CTL_BYTES);
     const int n_tiles = (a.N + BN - 1) / BN;
     const int total = ctl->tstart[n] * n_tiles;
 
@@ -145,9 +156,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
         constexpr int CW = Cf::CW;
         const int quarter = warp & 3, half = (warp - 4) >> 2;
-        [[maybe_unused]] float* s_sb = (float*)((uint8_t*)ctl + Cf::CTL_BYTES) + (warp - 4) * CW;
-        int acc = 0, e = 0;
-        uint32_t acc_phase = 0;
+        int acc = 0, e = 0, slot = 0;
+        uint32_t acc_phase = 0, slot_phase = 0;
         bool stop = false;
         for (int tile = blockIdx.x; tile < total && !stop; tile += gridDim.x) {
             int row0, col0, kb0, kbs;
@@ -155,64 +165,61 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             const long long row = row0 + quarter * 32 + lane;
             const int col = col0 + half * CW;
             const bool row_ok = row < a.M;
-            unsigned long long sum[CW / 2];
+            float sum[CW];
 #pragma unroll
-            for (int q = 0; q < CW / 2; ++q) sum[q] = 0ull;
-            // scale of block kb: the row's, times the column block's; asked for two blocks ahead
-            const float* sa = a.sa + (size_t)kb0 * a.M + row;
-            const float* sb = WGRAD ? a.sb + (size_t)kb0 * a.N : a.sb + ((size_t)e * a.Nb + min(col / kQ, a.Nb - 1)) * a.Kb;
-            auto row_scale = [&](int kb) { return row_ok && kb < kbs ? __ldg(sa + (size_t)kb * a.M) : 0.f; };
-            auto col_scale = [&](int kb) { return !WGRAD && kb < kbs ? __ldg(sb + kb) : 1.f; };
-            float ra0 = row_scale(0), ca0 = col_scale(0), ra1 = row_scale(1), ca1 = col_scale(1);
-            float cs0[CW / 32], cs1[CW / 32];                    // wgrad: this lane's columns' scales, a block ahead
-            auto cols_of = [&](int kb, float* cs) {
-#pragma unroll
-                for (int q = 0; q < CW / 32; ++q) {
-                    const int c = col + q * 32 + lane;
-                    cs[q] = WGRAD && kb < kbs && c < a.N ? __ldg(sb + (size_t)kb * a.N + c) : 0.f;
-                }
-            };
-            if constexpr (WGRAD) cols_of(0, cs0);
+            for (int q = 0; q < CW; ++q) sum[q] = 0.f;
             for (int kb = 0; kb < kbs; ++kb) {
-                const float f = ra0 * ca0;
-                ra0 = ra1; ca0 = ca1;
-                ra1 = row_scale(kb + 2); ca1 = col_scale(kb + 2);
-                if constexpr (WGRAD) {
-                    __syncwarp();
-#pragma unroll
-                    for (int q = 0; q < CW / 32; ++q) s_sb[q * 32 + lane] = cs0[q];
-                    __syncwarp();
-                    cols_of(kb + 1, cs1);
-#pragma unroll
-                    for (int q = 0; q < CW / 32; ++q) cs0[q] = cs1[q];
-                }
-                if (!mbar_wait_warp(&ctl->tfull[acc], acc_phase, abort_flag, a.status)) { stop = true; break; }
+                if (!mbar_wait_warp_quick(&ctl->sfull[slot], slot_phase, abort_flag, a.status)) { stop = true; break; }
+                const float* sc = s_scales + slot * Cf::SCALES;
+                const float f = WGRAD ? sc[quarter * 32 + lane] : sc[quarter * 32 + lane] * sc[BM + half];
+                const float* s_sb = sc + BM + half * CW;
+                if (!mbar_wait_warp_quick(&ctl->tfull[acc], acc_phase, abort_flag, a.status)) { stop = true; break; }
                 tc_fence_after();
                 const uint32_t taddr = tmem_base + acc * BN + half * CW + ((uint32_t)(quarter * 32) << 16);
-                const unsigned long long f2 = f2_pack(f, f);
-                uint32_t v[2][16];
-                tmem_ld16(taddr, v[0]);
+                // 32 columns at a time, two pieces on their way while two are added: a thread waits twice per block (one piece of
+                // 16 at a time, eight waits: 1390 cycles per block of 128 x 256 x 128 where the tensor cores take 540)
+                uint32_t v[2][32];
+                tmem_ld32(taddr, v[0]);
+                tmem_ld32(taddr + 32, v[1]);
+                auto add = [&](const uint32_t* w, int g) {
 #pragma unroll
-                for (int g = 0; g < CW / 16; ++g) {
-                    tmem_ld_wait();
-                    if (g + 1 < CW / 16) tmem_ld16(taddr + (g + 1) * 16, v[(g + 1) & 1]);
-                    else {                                       // the last of them is in registers: the accumulator is free
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&ctl->tempty[acc]);
-                    }
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        const unsigned long long t = f2_pack(__uint_as_float(v[g & 1][2 * q]), __uint_as_float(v[g & 1][2 * q + 1]));
+                    for (int q = 0; q < 32; q += 4) {
                         if constexpr (WGRAD) {
-                            const float2 c2 = *(const float2*)(s_sb + g * 16 + 2 * q);
-                            f2_fma(sum[g * 8 + q], t, f2_mul(f2, f2_pack(c2.x, c2.y)));
+                            const float4 c = *(const float4*)(s_sb + g * 32 + q);
+                            sum[g * 32 + q] = fmaf(__uint_as_float(w[q]), f * c.x, sum[g * 32 + q]);
+                            sum[g * 32 + q + 1] = fmaf(__uint_as_float(w[q + 1]), f * c.y, sum[g * 32 + q + 1]);
+                            sum[g * 32 + q + 2] = fmaf(__uint_as_float(w[q + 2]), f * c.z, sum[g * 32 + q + 2]);
+                            sum[g * 32 + q + 3] = fmaf(__uint_as_float(w[q + 3]), f * c.w, sum[g * 32 + q + 3]);
                         } else {
-                            f2_fma(sum[g * 8 + q], t, f2);
+#pragma unroll
+                            for (int u = 0; u < 4; ++u) sum[g * 32 + q + u] = fmaf(__uint_as_float(w[q + u]), f, sum[g * 32 + q + u]);
                         }
                     }
+                };
+                auto release = [&]() {                           // all of it is in registers: the accumulator is free
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&ctl->tempty[acc]);
+                };
+                tmem_ld_wait();
+                if constexpr (CW == 64) {
+                    release();
+                    add(v[0], 0);
+                    add(v[1], 1);
+                } else {
+                    add(v[0], 0);
+                    tmem_ld32(taddr + 64, v[0]);
+                    add(v[1], 1);
+                    tmem_ld32(taddr + 96, v[1]);
+                    tmem_ld_wait();
+                    release();
+                    add(v[0], 2);
+                    add(v[1], 3);
                 }
+                if constexpr (WGRAD) __syncwarp();
+                if (lane == 0) mbar_arrive(&ctl->sempty[slot]);
                 if (++acc == 2) { acc = 0; acc_phase ^= 1; }
+                if (++slot == kScaleSlots) { slot = 0; slot_phase ^= 1; }
             }
             if (stop) break;
             if (!row_ok || col >= a.N) continue;
@@ -220,74 +227,50 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 static_assert(EPI != kFp8ActQuant || (!WGRAD && CW == kQ), "a thread holds one block of the result");
                 uint32_t m = 0;
 #pragma unroll
-                for (int q = 0; q < CW / 2; ++q) {
-                    float2 h = f2_unpack(sum[q]);
-                    const int c = col + 2 * q;
-                    if (a.bias) {
-                        if (c < a.N) h.x += to_f32(a.bias[(size_t)e * a.N + c]);
-                        if (c + 1 < a.N) h.y += to_f32(a.bias[(size_t)e * a.N + c + 1]);
-                    }
-                    h.x = act_precise(h.x, a.act);
-                    h.y = act_precise(h.y, a.act);
-                    m = max(m, max(abs_bits(h.x), abs_bits(h.y)));
-                    sum[q] = f2_pack(h.x, h.y);
+                for (int q = 0; q < CW; ++q) {
+                    if (a.bias && col + q < a.N) sum[q] += to_f32(a.bias[(size_t)e * a.N + col + q]);
+                    sum[q] = act_precise(sum[q], a.act);
+                    m = max(m, abs_bits(sum[q]));
                 }
                 const BlockScale b = block_scale(m);
                 a.qs[(size_t)(col / kQ) * a.M + row] = b.s;
                 uint8_t* o = a.q + (size_t)row * a.ldq + col;
+                const bool whole = sector_aligned(o);
 #pragma unroll
-                for (int q = 0; q < CW / 2; q += 16) {
+                for (int q = 0; q < CW; q += 32) {
                     uint32_t w[8];
 #pragma unroll
-                    for (int u = 0; u < 8; ++u) {
-                        const float2 x = f2_unpack(sum[q + 2 * u]), y = f2_unpack(sum[q + 2 * u + 1]);
-                        w[u] = e4m3x4(x.x, x.y, y.x, y.y, b.inv);
-                    }
-                    st_sector(o + 2 * q, make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]), sector_aligned(o));
+                    for (int u = 0; u < 8; ++u) w[u] = e4m3x4(sum[q + 4 * u], sum[q + 4 * u + 1], sum[q + 4 * u + 2], sum[q + 4 * u + 3], b.inv);
+                    st_sector(o + q, make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]), whole);
                 }
             } else {
                 const size_t at = ((WGRAD ? (size_t)e * a.M : 0) + row) * a.N + col;
                 if (a.bias) {
 #pragma unroll
-                    for (int q = 0; q < CW / 2; ++q) {
-                        float2 h = f2_unpack(sum[q]);
-                        const int c = col + 2 * q;
-                        if (c < a.N) h.x += to_f32(a.bias[(size_t)e * a.N + c]);
-                        if (c + 1 < a.N) h.y += to_f32(a.bias[(size_t)e * a.N + c + 1]);
-                        sum[q] = f2_pack(h.x, h.y);
-                    }
+                    for (int q = 0; q < CW; ++q)
+                        if (col + q < a.N) sum[q] += to_f32(a.bias[(size_t)e * a.N + col + q]);
                 }
                 if (a.out_bf16) {
                     __nv_bfloat16* o = (__nv_bfloat16*)a.C + at;
-                    const bool whole = sector_aligned(o);
+                    if (a.vec && col + CW <= a.N) {
+                        const bool whole = sector_aligned(o);
 #pragma unroll
-                    for (int q = 0; q < CW / 2; q += 8) {
-                        uint32_t w[8];
+                        for (int q = 0; q < CW; q += 16) st_sector(o + q, pack16<__nv_bfloat16>(sum + q), pack16<__nv_bfloat16>(sum + q + 8), whole);
+                    } else {
 #pragma unroll
-                        for (int u = 0; u < 8; ++u) { const float2 h = f2_unpack(sum[q + u]); w[u] = pack_bf16x2(h.x, h.y); }
-                        if (a.vec && col + 2 * q + 16 <= a.N) {
-                            st_sector(o + 2 * q, make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]), whole);
-                        } else {
-#pragma unroll
-                            for (int u = 0; u < 16; ++u)
-                                if (col + 2 * q + u < a.N) ((uint16_t*)o)[2 * q + u] = (uint16_t)(w[u >> 1] >> (16 * (u & 1)));
-                        }
+                        for (int q = 0; q < CW; ++q)
+                            if (col + q < a.N) o[q] = __float2bfloat16_rn(sum[q]);
                     }
                 } else {
                     float* o = (float*)a.C + at;
-                    const bool whole = sector_aligned(o);
+                    if (a.vec && col + CW <= a.N) {
+                        const bool whole = sector_aligned(o);
 #pragma unroll
-                    for (int q = 0; q < CW / 2; q += 4) {
-                        float h[8];
+                        for (int q = 0; q < CW; q += 8) st_sector(o + q, pack16<float>(sum + q), pack16<float>(sum + q + 4), whole);
+                    } else {
 #pragma unroll
-                        for (int u = 0; u < 4; ++u) { const float2 t = f2_unpack(sum[q + u]); h[2 * u] = t.x; h[2 * u + 1] = t.y; }
-                        if (a.vec && col + 2 * q + 8 <= a.N) {
-                            st_sector(o + 2 * q, pack16<float>(h), pack16<float>(h + 4), whole);
-                        } else {
-#pragma unroll
-                            for (int u = 0; u < 8; ++u)
-                                if (col + 2 * q + u < a.N) o[2 * q + u] = h[u];
-                        }
+                        for (int q = 0; q < CW; ++q)
+                            if (col + q < a.N) o[q] = sum[q];
                     }
                 }
             }
@@ -302,7 +285,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 int row0, col0, kb0, kbs;
                 locate(tile, e, row0, col0, kb0, kbs);
                 for (int kb = 0; kb < kbs; ++kb) {
-                    if (!mbar_wait_warp(&ctl->empty[stage], phase ^ 1, abort_flag, a.status)) { stop = true; break; }
+                    if (!mbar_wait_warp_quick(&ctl->empty[stage], phase ^ 1, abort_flag, a.status)) { stop = true; break; }
                     if (lane == 0) {
                         uint8_t* st = smem + stage * Cf::STAGE;
                         mbar_arrive_expect_tx(&ctl->full[stage], Cf::STAGE);
@@ -328,8 +311,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 int row0, col0, kb0, kbs;
                 locate(tile, e, row0, col0, kb0, kbs);
                 for (int kb = 0; kb < kbs; ++kb) {
-                    if (!mbar_wait_warp(&ctl->tempty[acc], acc_phase ^ 1, abort_flag, a.status) ||
-                        !mbar_wait_warp(&ctl->full[stage], phase, abort_flag, a.status)) { stop = true; break; }
+                    if (!mbar_wait_warp_quick(&ctl->tempty[acc], acc_phase ^ 1, abort_flag, a.status) ||
+                        !mbar_wait_warp_quick(&ctl->full[stage], phase, abort_flag, a.status)) { stop = true; break; }
                     tc_fence_after();
                     const uint32_t st = smem_u32(smem + stage * Cf::STAGE);
 #pragma unroll
@@ -341,6 +324,36 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                     if (++acc == 2) { acc = 0; acc_phase ^= 1; }
                 }
             }
+        } else if (warp == 2) {
+            int slot = 0, e = 0;
+            uint32_t phase = 0;
+            bool stop = false;
+            for (int tile = blockIdx.x; tile < total && !stop; tile += gridDim.x) {
+                int row0, col0, kb0, kbs;
+                locate(tile, e, row0, col0, kb0, kbs);
+                const float* sa = a.sa + (size_t)kb0 * a.M + row0;
+                const int rows = (int)(a.M - row0 < BM ? a.M - row0 : BM);
+                const float* sb = WGRAD ? a.sb + (size_t)kb0 * a.N + col0 : a.sb + ((size_t)e * a.Nb + col0 / kQ) * a.Kb;
+                const int cols = WGRAD ? min(a.N - col0, BN) : 0, nb = min(a.Nb - col0 / kQ, 2);
+                for (int kb = 0; kb < kbs; ++kb, sa += a.M) {
+                    if (!mbar_wait_warp_quick(&ctl->sempty[slot], phase ^ 1, abort_flag, a.status)) { stop = true; break; }
+                    const uint32_t dst = smem_u32(s_scales + slot * Cf::SCALES);
+#pragma unroll
+                    for (int r = lane; r < BM; r += 32) cp_async4(dst + 4 * r, sa + (r < rows ? r : 0), r < rows);
+                    if constexpr (WGRAD) {
+                        for (int c = lane; c < BN; c += 32) cp_async4(dst + 4 * (BM + c), sb + (c < cols ? c : 0), c < cols);
+                        sb += a.N;
+                    } else {      // a warp of either column half reads its own: with 128 columns they are the same block
+                        if (lane < 2) {
+                            const int b = BN == 256 ? lane : 0;
+                            cp_async4(dst + 4 * (BM + lane), sb + (size_t)(b < nb ? b : 0) * a.Kb + kb, b < nb);
+                        }
+                    }
+                    cp_async_arrive(&ctl->sfull[slot]);
+                    if (++slot == kScaleSlots) { slot = 0; phase ^= 1; }
+                }
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");      // none in flight when the CTA exits
         }
     }
     tc_fence_before();
