@@ -58,7 +58,8 @@ typedef enum {
     UOE_ERR_CUDA = 4,          /* a CUDA runtime / driver call failed */
     UOE_ERR_TIMEOUT = 5,       /* device status: a bounded wait inside a kernel ran out */
     UOE_ERR_DEVICE_INDEX = 6,  /* device status: a routing index was out of range */
-    UOE_ERR_STATIC_SCRATCH = 7 /* uoe_route_static: the problem needs more scratch than the built-in array holds */
+    UOE_ERR_STATIC_SCRATCH = 7,/* uoe_route_static: the problem needs more scratch than the built-in array holds */
+    UOE_ERR_FP8_SCALE = 8      /* device status: a scale of an 8-bit operand is not a power of two */
 } uoe_status;
 
 typedef enum { UOE_F32 = 0, UOE_BF16 = 1 } uoe_dtype;
@@ -273,7 +274,13 @@ typedef struct {
     int32_t N;        /* columns of the result */
     int32_t K;        /* contraction (uoe_fp8_wgrad: rows of all regions, padding included) */
     int32_t dtype;    /* uoe_dtype of the result; uoe_fp8_wgrad: UOE_F32 */
+    uint32_t flags;   /* UOE_FP8_ANY_SCALE or 0 */
 } uoe_fp8_problem;
+
+/* The scales may be any float32 numbers, as weights quantised elsewhere have them.  Without it they are powers of two, as
+ * uoe_fp8_quantize writes them, or NaN, and the tensor cores apply them; a scale that is neither counts as NaN and is reported in the
+ * workspace's status word (UOE_ERR_FP8_SCALE). */
+enum { UOE_FP8_ANY_SCALE = 1 };
 
 /* Bytes of device workspace of the two products (0 on an invalid problem).  Prepared with uoe_workspace_init like any other. */
 size_t uoe_fp8_workspace_bytes(const uoe_fp8_problem* prob);
@@ -284,7 +291,7 @@ size_t uoe_fp8_workspace_bytes(const uoe_fp8_problem* prob);
  *   C[r, j] = sum over blocks b of  a_scale[b, r] * w_scale[e, j / 128, b] * sum over k in b of  A[r, k] * W[e, j, k]
  * for the rows r of expert e's region, products and sums in float32.
  *   A [M, Kp], a_scale [Kb, M]: UOE_FP8_ROWS of the rows.   W [n, N, Kp], w_scale [n, Nb, Kb]: UOE_FP8_BLOCKS of [n, N, K] or
- *   UOE_FP8_BLOCKS_T of [n, K, N].   Scales may be any float32 numbers.
+ *   UOE_FP8_BLOCKS_T of [n, K, N].
  *   expert_offsets [n+1]: multiples of UOE_ROW_ALIGN, ascending, at most M ("Routed buffers" above); rows of a region's padding are
  *   computed like any other, rows from expert_offsets[n] on are left as they were.  NULL with n = 1: all M rows.  Offsets of
  *   another form are reported in the workspace's status word (UOE_ERR_DEVICE_INDEX) and nothing is computed.

@@ -22,7 +22,7 @@ ACTS = {"gelu_erf": 0, "gelu_tanh": 1, "silu": 2, "identity": 3}
 UOE_FLAG_RESIDUAL, UOE_FLAG_GATE, UOE_FLAG_CAUSAL, UOE_FLAG_DYNAMIC_C, UOE_FLAG_GENERAL_PATH = 1, 2, 4, 8, 16
 UOE_OP_ROUTE, UOE_OP_MLP_FWD, UOE_OP_MLP_BWD, UOE_OP_SMHA_FWD, UOE_OP_SMHA_BWD = 0, 1, 2, 3, 4
 UOE_OP_BALANCE_BWD = 5
-UOE_FP8_BLOCK = 128
+UOE_FP8_BLOCK, UOE_FP8_ANY_SCALE = 128, 1
 FP8_LAYOUTS = {"rows": 0, "cols": 1, "blocks": 2, "blocks_t": 3}
 
 
@@ -43,7 +43,7 @@ class _Problem(ctypes.Structure):
 
 
 class _Fp8Problem(ctypes.Structure):
-    _fields_ = [(f, ctypes.c_int32) for f in ("n", "M", "N", "K", "dtype")]
+    _fields_ = [(f, ctypes.c_int32) for f in ("n", "M", "N", "K", "dtype")] + [("flags", ctypes.c_uint32)]
 
 
 @dataclass
@@ -54,9 +54,11 @@ class Fp8Problem:
     N: int
     K: int
     dtype: str = "bf16"
+    any_scale: bool = False         # UOE_FP8_ANY_SCALE: scales that are not powers of two
 
     def c_struct(self) -> _Fp8Problem:
-        return _Fp8Problem(self.n, self.M, self.N, self.K, UOE_BF16 if self.dtype == "bf16" else UOE_F32)
+        return _Fp8Problem(self.n, self.M, self.N, self.K, UOE_BF16 if self.dtype == "bf16" else UOE_F32,
+                           UOE_FP8_ANY_SCALE if self.any_scale else 0)
 
     @property
     def torch_dtype(self):

@@ -84,6 +84,7 @@ extern "C" const char* uoe_status_string(int status) {
         case UOE_ERR_TIMEOUT: return "device wait timed out";
         case UOE_ERR_DEVICE_INDEX: return "routing index out of range";
         case UOE_ERR_STATIC_SCRATCH: return "problem too large for the built-in static scratch of uoe_route_static";
+        case UOE_ERR_FP8_SCALE: return "scale of an 8-bit operand is not a power of two";
         default: return "unknown status";
     }
 }

@@ -61,6 +61,7 @@ struct Fp8Gemm {
     int act = UOE_ACT_IDENTITY;
     Fp8Epilogue epi = kFp8Store;
     void* q = nullptr; float* qs = nullptr;      // kFp8ActQuant: [M, Np], [Np / 128, M]
+    bool any_scale = false;                // scales need not be powers of two
     const char* label = "fp8_gemm";
 };
 uoe_status launch_fp8_gemm(const Fp8Gemm& g, int* status, cudaStream_t s);

@@ -1,18 +1,20 @@
-// Products of 8-bit operands with a scale per block of 128 (fp8.cuh) on the tcgen05 tensor cores, grouped by expert:
+// Products of 8-bit operands whose scales are powers of two (fp8.cuh) on the tcgen05 tensor cores, grouped by expert:
 //
 //   rows    C[r, j]    = sum_kb sa[kb, r] sb[e(r), j / 128, kb]  sum_{k in block kb} A[r, k] B[e(r), j, k]
 //   wgrad   C[e, i, j] = sum_kb sa[kb, i] sb[kb, j]              sum_{r in block kb} A[i, r] B[j, r],   kb over expert e's region
 //
-// The tensor cores form one block's product at a time (K = 128: four instructions) in TMEM, and eight warps add it, times its
-// scales, to accumulators in registers: the scales are any float32 numbers, and the sum over blocks is float32 arithmetic.
-// A persistent CTA per SM walks the 128 x BN tiles:
-//   warp 0      TMA producer: a stage is one block, 128 x 128 bytes of A and BN x 128 of B (128-byte rows, swizzled)
-//   warp 1      MMA issuer: a block's product into one of two TMEM accumulators, which the other warps empty in turn
-//   warp 2      the scales of the blocks to come, by 4-byte asynchronous copies (their rows start anywhere) into a ring of their own
-//   warps 4..11 a warp has 32 rows (its TMEM lane quarter) and half of the columns: one row's BN / 2 sums per thread.  The
-//               columns are one block of B's scales, so a thread's factor is one number per block.
-// Regions of experts are whole 128-row tiles, so no tile straddles two experts, and in wgrad no block does.
-#include "fp8.cuh"
+// The block-scaled MMA takes an exponent byte per row of A and of B, so the sum over all blocks stays in one float32 TMEM
+// accumulator and nothing has to be added outside (any other scale: fp8_gemm_any_tcgen05.cu, where that addition is what bounds the
+// kernel).  A persistent CTA (pair) per SM (two) walks the tiles, 128 x BN or, by a pair of CTAs (cta_group::2), 256 x 256:
+//   warp 0       TMA producer: a stage is one block of the contraction, 128 bytes of every row of A and of B (128-byte swizzle)
+//   warp 1       MMA issuer: four steps of 32 per stage
+//   warps 4..7   the stage's scales: float32 -> exponent byte, once for every lane quarter of TMEM (a warp each), four blocks ahead
+//                in registers.  A scale holds for the whole stage, so its byte fills the word and the steps need no index.
+//   warps 8..15  write-out: a warp has 32 rows (its TMEM lane quarter) and half of the columns, all of them in registers before it
+//                gives the accumulator back (256 columns and the scales leave room for one accumulator: the next tile's products
+//                wait for these loads, not for the arithmetic and the stores)
+// Regions of experts are whole 128-row blocks; the second half of a pair's last tile may be rows of nobody, which are not stored.
+#include "fp8_tile.cuh"
 #include "tc.cuh"
 #include "tmap.cuh"
 
@@ -22,275 +24,198 @@ namespace {
 using namespace tc;
 
 constexpr int BM = 128;
-constexpr int kMaxExperts = 32;
-constexpr int kScaleSlots = 8;
-template <int BN> struct Cfg {
-    static constexpr int A_BYTES = BM * kQ, B_BYTES = BN * kQ, STAGE = A_BYTES + B_BYTES;
-    static constexpr int STAGES = BN == 256 ? 4 : 6;
-    static constexpr int CW = BN / 2;                 // columns of an accumulating warp
-    static constexpr int EPI_WARPS = 8, THREADS = 128 + 32 * EPI_WARPS;
-    static constexpr int TMEM_COLS = 2 * BN;
-    static constexpr int SCALES = BM + BN;            // floats of a block's scales: the rows', then the columns' (or column blocks')
-    static constexpr int CTL_BYTES = 1024;
-    static constexpr int SMEM = STAGES * STAGE + 1024 /* alignment */ + CTL_BYTES + kScaleSlots * SCALES * 4;
+
+template <int BN, bool PAIR> struct Cfg {
+    static_assert(!PAIR || BN == 256, "a pair works 256 x 256");
+    static constexpr int BN_CTA = PAIR ? BN / 2 : BN;                 // rows of B this CTA loads
+    static constexpr int TILE = PAIR ? 2 * BM : BM;
+    static constexpr int A_BYTES = BM * kQ, B_BYTES = BN_CTA * kQ, STAGE = A_BYTES + B_BYTES;
+    static constexpr int STAGES = BN_CTA == 256 ? 4 : 6;
+    static constexpr int NACC = BN == 256 ? 1 : 2;
+    static constexpr int CW = BN / 2;
+    static constexpr int EPI_WARPS = 8, SCALE_WARPS = 4, THREADS = 128 + 128 + 32 * EPI_WARPS;
+    static constexpr int TMEM_COLS = 512, SF_COL = 256, SF_STRIDE = 16, SFB = 8;      // scales of stage s: A at SF_COL + 16 s, B 8 behind
+    static constexpr int SMEM = STAGES * STAGE + 1024 /* alignment */ + 1024 /* control */;
 };
 
-// four bytes, zero where `real` is false (the address is a valid one all the same)
-__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, bool real) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" :: "r"(dst), "l"(src), "r"(real ? 4 : 0) : "memory");
-}
-// one arrival of this thread on the barrier when all its copies so far have landed (counted in the barrier's 32)
-__device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
-    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" :: "r"(smem_u32(bar)) : "memory");
-}
-
 struct Ctl {
-    uint64_t full[8], empty[8], tfull[2], tempty[2], sfull[kScaleSlots], sempty[kScaleSlots];
+    uint64_t full[8], empty[8], tfull[2], tempty[2];
     uint32_t tmem_base;
     int abort_flag;
-    int bad;                                          // offsets that are no regions: nothing is computed
-    int offs[kMaxExperts + 1];
-    int tstart[kMaxExperts + 1];                      // first row tile of each expert
+    Regions reg;
 };
 static_assert(sizeof(Ctl) <= 1024, "control block");
 
-struct Fp8Args {
-    const float *sa, *sb;
-    const int* offsets;
-    int n, N, Nb;                     // columns of C, blocks of 128 of them
-    long long M;                      // rows of C (rows of the A operand)
-    int Kb;                           // blocks of the contraction (wgrad: in all regions together)
-    void* C;
-    int out_bf16, vec;                // vec: rows of C may be stored in 32-byte pieces
-    const __nv_bfloat16* bias;
-    int act;
-    uint8_t* q;
-    float* qs;
-    long long ldq;
-    int* status;
-};
-
-// phi with errors of float32 size (the result is compared with a rounding border of its own)
-__device__ __forceinline__ float act_precise(float h, int act) {
-    switch (act) {
-        case UOE_ACT_SILU: return __fdividef(h, 1.0f + __expf(-h));
-        case UOE_ACT_GELU_TANH: {
-            const float u = 0.79788456080286536f * (h + 0.044715f * h * h * h);
-            return __fdividef(h, 1.0f + __expf(-2.0f * u));             // h/2 (1 + tanh u)
-        }
-        default: return act_apply(h, act);
+// The scale's exponent byte in all four bytes of a word; 0xff stands for NaN.
+__device__ __forceinline__ uint32_t exponent_word(float s, int* status) {
+    const uint32_t b = __float_as_uint(s);
+    uint32_t e = b >> 23;
+    if (((b & 0x7fffffu) != 0 || e - 1 >= 254u) && e != 255) {        // not a power of two
+        set_status(status, UOE_ERR_FP8_SCALE);
+        e = 255;
     }
+    return e * 0x01010101u;
 }
 
-template <int BN, bool WGRAD, int EPI>
-__global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
+template <int BN, bool WGRAD, int EPI, bool PAIR>
+__global__ void __launch_bounds__(Cfg<BN, PAIR>::THREADS, 1)
 fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ Fp8Args a) {
     pdl_trigger();
-    using Cf = Cfg<BN>;
+    using Cf = Cfg<BN, PAIR>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     Ctl* ctl = (Ctl*)(smem + Cf::STAGES * Cf::STAGE);
     volatile int* abort_flag = &ctl->abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = PAIR ? (int)cluster_ctarank() : 0;
+    const int worker = PAIR ? blockIdx.x >> 1 : blockIdx.x, workers = PAIR ? gridDim.x >> 1 : gridDim.x;
     const int n = a.n;
+    constexpr int CTAS = PAIR ? 2 : 1;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < Cf::STAGES; ++s) { mbar_init(&ctl->full[s], 1); mbar_init(&ctl->empty[s], 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(&ctl->tfull[i], 1); mbar_init(&ctl->tempty[i], Cf::EPI_WARPS); }
-        for (int i = 0; i < kScaleSlots; ++i) { mbar_init(&ctl->sfull[i], 32); mbar_init(&ctl->sempty[i], Cf::EPI_WARPS); }
+        // (a pair's products are issued by rank 0, on whose barriers both CTAs' copies, scales and write-outs arrive)
+        for (int s = 0; s < Cf::STAGES; ++s) { mbar_init(&ctl->full[s], 1 + CTAS * Cf::SCALE_WARPS); mbar_init(&ctl->empty[s], 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&ctl->tfull[i], 1); mbar_init(&ctl->tempty[i], CTAS * Cf::EPI_WARPS); }
         ctl->abort_flag = 0;
         fence_barrier_init();
         prefetch_tmap(&tmA);
         prefetch_tmap(&tmB);
     }
-    if (warp == 1) tmem_alloc(&ctl->tmem_base, Cf::TMEM_COLS);
-    pdl_wait();
-    // tiles of the rows: per expert its 128-row blocks; without offsets all rows are one expert's; wgrad: every expert has all of C
-    const int m_tiles = (int)((a.M + BM - 1) / BM);
-    if (warp == 2) {
-        const long long limit = WGRAD ? (long long)a.Kb * kQ : a.M;
-        int o = 0, o1 = 0;
-        if (a.offsets) {
-            o = lane < n ? a.offsets[lane] : 0;
-            o1 = lane < n ? a.offsets[lane + 1] : 0;
-        } else if (lane == 0) {
-            o1 = WGRAD ? a.Kb * kQ : m_tiles * BM;
-        }
-        const bool ok = lane >= n || !a.offsets || (o >= 0 && o1 >= o && o1 <= limit && ((o | o1) & (BM - 1)) == 0);
-        const bool bad = !__all_sync(0xffffffffu, ok);
-        const int tiles = lane < n && !bad ? (WGRAD ? m_tiles : (o1 - o) / BM) : 0;
-        int incl = tiles;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, incl, d);
-            if (lane >= d) incl += v;
-        }
-        if (lane < n) {
-            ctl->offs[lane] = o;
-            ctl->offs[lane + 1] = o1;                 // (the neighbour writes the same number)
-            ctl->tstart[lane] = incl - tiles;
-            if (lane == n - 1) ctl->tstart[n] = incl;
-        }
-        if (lane == 0 && bad) set_status(a.status, UOE_ERR_DEVICE_INDEX);
+    if (warp == 1) {
+        if constexpr (PAIR) tmem_alloc_pair(&ctl->tmem_base, Cf::TMEM_COLS);
+        else tmem_alloc(&ctl->tmem_base, Cf::TMEM_COLS);
     }
+    pdl_wait();
+    const int m_tiles = (int)((a.M + Cf::TILE - 1) / Cf::TILE);
+    if (warp == 2) load_regions<WGRAD, Cf::TILE>(ctl->reg, a, m_tiles, lane);
     tc_fence_before();
     __syncthreads();
+    if constexpr (PAIR) cluster_sync_all();           // the other CTA's barriers exist before anything arrives on them
     tc_fence_after();
     const uint32_t tmem_base = ctl->tmem_base;
-    float* s_scales = (float*)((uint8_t*)ctl + Cf::CTL_BYTES);
     const int n_tiles = (a.N + BN - 1) / BN;
-    const int total = ctl->tstart[n] * n_tiles;
+    const int total = ctl->reg.tstart[n] * n_tiles;
 
-    // tile -> expert, first row of A and C, first block of the contraction and their number
-    auto locate = [&](int tile, int& e, int& row0, int& col0, int& kb0, int& kbs) {
+    // tile -> expert, first row of A and C in this CTA and where the expert's rows end, first block of the contraction and their number
+    struct Tile { int row0, row_end, col0, kb0, kbs; };
+    auto locate = [&](int tile, int& e) {
+        Tile t;
         const int rt = tile / n_tiles;
-        while (e + 1 < n && rt >= ctl->tstart[e + 1]) ++e;
-        row0 = (rt - ctl->tstart[e]) * BM + (WGRAD ? 0 : ctl->offs[e]);
-        col0 = (tile - rt * n_tiles) * BN;
-        kb0 = WGRAD ? ctl->offs[e] / kQ : 0;
-        kbs = WGRAD ? (ctl->offs[e + 1] - ctl->offs[e]) / kQ : a.Kb;
+        while (e + 1 < n && rt >= ctl->reg.tstart[e + 1]) ++e;
+        t.row0 = (rt - ctl->reg.tstart[e]) * Cf::TILE + rank * BM + (WGRAD ? 0 : ctl->reg.offs[e]);
+        t.row_end = (int)(WGRAD || ctl->reg.offs[e + 1] > a.M ? a.M : ctl->reg.offs[e + 1]);
+        t.col0 = (tile - rt * n_tiles) * BN;
+        t.kb0 = WGRAD ? ctl->reg.offs[e] / kQ : 0;
+        t.kbs = WGRAD ? (ctl->reg.offs[e + 1] - ctl->reg.offs[e]) / kQ : a.Kb;
+        return t;
     };
 
-    // Registers: 384 threads start with 168 each; the first warpgroup gives 128 of its up, the accumulating ones take 64 more
-    // (128 * 40 + 256 * 232 = 384 * 168).
-    if (warp >= 4) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+    // Registers: 512 threads start with 128 each (128 * 56 + 128 * 56 + 256 * 200 = 512 * 128).
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         constexpr int CW = Cf::CW;
-        const int quarter = warp & 3, half = (warp - 4) >> 2;
-        int acc = 0, e = 0, slot = 0;
-        uint32_t acc_phase = 0, slot_phase = 0;
-        bool stop = false;
-        for (int tile = blockIdx.x; tile < total && !stop; tile += gridDim.x) {
-            int row0, col0, kb0, kbs;
-            locate(tile, e, row0, col0, kb0, kbs);
-            const long long row = row0 + quarter * 32 + lane;
-            const int col = col0 + half * CW;
-            const bool row_ok = row < a.M;
+        const int quarter = warp & 3, half = (warp - 8) >> 2;
+        int acc = 0, e = 0;
+        uint32_t acc_phase = 0;
+        for (int tile = worker; tile < total; tile += workers) {
+            const Tile t = locate(tile, e);
             float sum[CW];
-#pragma unroll
-            for (int q = 0; q < CW; ++q) sum[q] = 0.f;
-            for (int kb = 0; kb < kbs; ++kb) {
-                if (!mbar_wait_warp_quick(&ctl->sfull[slot], slot_phase, abort_flag, a.status)) { stop = true; break; }
-                const float* sc = s_scales + slot * Cf::SCALES;
-                const float f = WGRAD ? sc[quarter * 32 + lane] : sc[quarter * 32 + lane] * sc[BM + half];
-                const float* s_sb = sc + BM + half * CW;
-                if (!mbar_wait_warp_quick(&ctl->tfull[acc], acc_phase, abort_flag, a.status)) { stop = true; break; }
+            if (t.kbs > 0) {
+                if (!mbar_wait_warp_quick(&ctl->tfull[acc], acc_phase, abort_flag, a.status)) break;
                 tc_fence_after();
                 const uint32_t taddr = tmem_base + acc * BN + half * CW + ((uint32_t)(quarter * 32) << 16);
-                // 32 columns at a time, two pieces on their way while two are added: a thread waits twice per block (one piece of
-                // 16 at a time, eight waits: 1390 cycles per block of 128 x 256 x 128 where the tensor cores take 540)
-                uint32_t v[2][32];
-                tmem_ld32(taddr, v[0]);
-                tmem_ld32(taddr + 32, v[1]);
-                auto add = [&](const uint32_t* w, int g) {
 #pragma unroll
-                    for (int q = 0; q < 32; q += 4) {
-                        if constexpr (WGRAD) {
-                            const float4 c = *(const float4*)(s_sb + g * 32 + q);
-                            sum[g * 32 + q] = fmaf(__uint_as_float(w[q]), f * c.x, sum[g * 32 + q]);
-                            sum[g * 32 + q + 1] = fmaf(__uint_as_float(w[q + 1]), f * c.y, sum[g * 32 + q + 1]);
-                            sum[g * 32 + q + 2] = fmaf(__uint_as_float(w[q + 2]), f * c.z, sum[g * 32 + q + 2]);
-                            sum[g * 32 + q + 3] = fmaf(__uint_as_float(w[q + 3]), f * c.w, sum[g * 32 + q + 3]);
-                        } else {
+                for (int g = 0; g < CW / 32; ++g) tmem_ld32(taddr + g * 32, (uint32_t*)sum + g * 32);
+                tmem_ld_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if constexpr (PAIR) mbar_arrive_cluster(map_to_cta(&ctl->tempty[acc], 0));
+                    else mbar_arrive(&ctl->tempty[acc]);
+                }
+                if (++acc == Cf::NACC) { acc = 0; acc_phase ^= 1; }
+            } else {
 #pragma unroll
-                            for (int u = 0; u < 4; ++u) sum[g * 32 + q + u] = fmaf(__uint_as_float(w[q + u]), f, sum[g * 32 + q + u]);
-                        }
-                    }
-                };
-                auto release = [&]() {                           // all of it is in registers: the accumulator is free
+                for (int q = 0; q < CW; ++q) sum[q] = 0.f;
+            }
+            const int row = t.row0 + quarter * 32 + lane, col = t.col0 + half * CW;
+            if (row < t.row_end && col < a.N) store_tile<CW, WGRAD, EPI>(a, sum, e, row, col);
+            __syncwarp();
+        }
+    } else if (warp >= 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        const uint32_t quarter = (uint32_t)((warp & 3) * 32) << 16;
+        constexpr int NB = WGRAD ? BN / 32 : (BN + kQ - 1) / kQ;      // scales of B per lane: its columns', or the column blocks'
+        constexpr int AHEAD = WGRAD ? 2 : 4;
+        int stage = 0, e = 0;
+        uint32_t phase = 0;
+        bool stop = false;
+        for (int tile = worker; tile < total && !stop; tile += workers) {
+            const Tile t = locate(tile, e);
+            const float* sa = a.sa + (size_t)t.kb0 * a.M + t.row0;
+            const float* sb = WGRAD ? a.sb + (size_t)t.kb0 * a.N + t.col0 : a.sb + ((size_t)e * a.Nb + t.col0 / kQ) * a.Kb;
+            float ra[AHEAD][4], rb[AHEAD][NB];
+            auto ask = [&](int kb, float* ra, float* rb) {            // scales of block kb (1 where there are no rows of this expert)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) ra[q] = kb < t.kbs && t.row0 + q * 32 + lane < t.row_end ? __ldg(sa + (size_t)kb * a.M + q * 32 + lane) : 1.f;
+#pragma unroll
+                for (int q = 0; q < NB; ++q) {
+                    if constexpr (WGRAD) rb[q] = kb < t.kbs && t.col0 + q * 32 + lane < a.N ? __ldg(sb + (size_t)kb * a.N + q * 32 + lane) : 1.f;
+                    else rb[q] = kb < t.kbs && t.col0 + q * kQ < a.N ? __ldg(sb + (size_t)q * a.Kb + kb) : 1.f;
+                }
+            };
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) ask(u, ra[u], rb[u]);
+            for (int kb0 = 0; kb0 < t.kbs && !stop; kb0 += AHEAD) {
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    if (kb0 + u >= t.kbs) break;
+                    uint32_t wa[4], wb[8];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) wa[q] = exponent_word(ra[u][q], a.status);
+#pragma unroll
+                    for (int q = 0; q < NB; ++q) rb[u][q] = __uint_as_float(exponent_word(rb[u][q], a.status));
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) wb[q] = __float_as_uint(rb[u][WGRAD ? q % NB : (q / 4) % NB]);
+                    ask(kb0 + u + AHEAD, ra[u], rb[u]);
+                    if (!mbar_wait_warp_quick(&ctl->empty[stage], phase ^ 1, abort_flag, a.status)) { stop = true; break; }
+                    tc_fence_after();
+                    const uint32_t sf = tmem_base + Cf::SF_COL + stage * Cf::SF_STRIDE + quarter;
+                    tmem_st4(sf, wa);
+                    if constexpr (BN == 256) tmem_st8(sf + Cf::SFB, wb);
+                    else tmem_st4(sf + Cf::SFB, wb);
+                    tmem_st_wait();
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&ctl->tempty[acc]);
-                };
-                tmem_ld_wait();
-                if constexpr (CW == 64) {
-                    release();
-                    add(v[0], 0);
-                    add(v[1], 1);
-                } else {
-                    add(v[0], 0);
-                    tmem_ld32(taddr + 64, v[0]);
-                    add(v[1], 1);
-                    tmem_ld32(taddr + 96, v[1]);
-                    tmem_ld_wait();
-                    release();
-                    add(v[0], 2);
-                    add(v[1], 3);
-                }
-                if constexpr (WGRAD) __syncwarp();
-                if (lane == 0) mbar_arrive(&ctl->sempty[slot]);
-                if (++acc == 2) { acc = 0; acc_phase ^= 1; }
-                if (++slot == kScaleSlots) { slot = 0; slot_phase ^= 1; }
-            }
-            if (stop) break;
-            if (!row_ok || col >= a.N) continue;
-            if constexpr (EPI == kFp8ActQuant) {
-                static_assert(EPI != kFp8ActQuant || (!WGRAD && CW == kQ), "a thread holds one block of the result");
-                uint32_t m = 0;
-#pragma unroll
-                for (int q = 0; q < CW; ++q) {
-                    if (a.bias && col + q < a.N) sum[q] += to_f32(a.bias[(size_t)e * a.N + col + q]);
-                    sum[q] = act_precise(sum[q], a.act);
-                    m = max(m, abs_bits(sum[q]));
-                }
-                const BlockScale b = block_scale(m);
-                a.qs[(size_t)(col / kQ) * a.M + row] = b.s;
-                uint8_t* o = a.q + (size_t)row * a.ldq + col;
-                const bool whole = sector_aligned(o);
-#pragma unroll
-                for (int q = 0; q < CW; q += 32) {
-                    uint32_t w[8];
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) w[u] = e4m3x4(sum[q + 4 * u], sum[q + 4 * u + 1], sum[q + 4 * u + 2], sum[q + 4 * u + 3], b.inv);
-                    st_sector(o + q, make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]), whole);
-                }
-            } else {
-                const size_t at = ((WGRAD ? (size_t)e * a.M : 0) + row) * a.N + col;
-                if (a.bias) {
-#pragma unroll
-                    for (int q = 0; q < CW; ++q)
-                        if (col + q < a.N) sum[q] += to_f32(a.bias[(size_t)e * a.N + col + q]);
-                }
-                if (a.out_bf16) {
-                    __nv_bfloat16* o = (__nv_bfloat16*)a.C + at;
-                    if (a.vec && col + CW <= a.N) {
-                        const bool whole = sector_aligned(o);
-#pragma unroll
-                        for (int q = 0; q < CW; q += 16) st_sector(o + q, pack16<__nv_bfloat16>(sum + q), pack16<__nv_bfloat16>(sum + q + 8), whole);
-                    } else {
-#pragma unroll
-                        for (int q = 0; q < CW; ++q)
-                            if (col + q < a.N) o[q] = __float2bfloat16_rn(sum[q]);
+                    if (lane == 0) {
+                        if constexpr (PAIR) mbar_arrive_cluster(map_to_cta(&ctl->full[stage], 0));
+                        else mbar_arrive(&ctl->full[stage]);
                     }
-                } else {
-                    float* o = (float*)a.C + at;
-                    if (a.vec && col + CW <= a.N) {
-                        const bool whole = sector_aligned(o);
-#pragma unroll
-                        for (int q = 0; q < CW; q += 8) st_sector(o + q, pack16<float>(sum + q), pack16<float>(sum + q + 4), whole);
-                    } else {
-#pragma unroll
-                        for (int q = 0; q < CW; ++q)
-                            if (col + q < a.N) o[q] = sum[q];
-                    }
+                    if (++stage == Cf::STAGES) { stage = 0; phase ^= 1; }
                 }
             }
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (warp == 0) {
             int stage = 0, e = 0;
             uint32_t phase = 0, issued = 0, issued_parity = 0;
             bool stop = false;
-            for (int tile = blockIdx.x; tile < total && !stop; tile += gridDim.x) {
-                int row0, col0, kb0, kbs;
-                locate(tile, e, row0, col0, kb0, kbs);
-                for (int kb = 0; kb < kbs; ++kb) {
+            for (int tile = worker; tile < total && !stop; tile += workers) {
+                const Tile t = locate(tile, e);
+                for (int kb = 0; kb < t.kbs; ++kb) {
                     if (!mbar_wait_warp_quick(&ctl->empty[stage], phase ^ 1, abort_flag, a.status)) { stop = true; break; }
                     if (lane == 0) {
                         uint8_t* st = smem + stage * Cf::STAGE;
-                        mbar_arrive_expect_tx(&ctl->full[stage], Cf::STAGE);
-                        tma_load_2d(st, &tmA, (kb0 + kb) * kQ, row0, &ctl->full[stage]);
-                        tma_load_3d(st + Cf::A_BYTES, &tmB, (kb0 + kb) * kQ, col0, WGRAD ? 0 : e, &ctl->full[stage]);
+                        const int k = (t.kb0 + kb) * kQ, row = min(t.row0, (int)a.M);        // (a block behind the rows: all zeros)
+                        if (rank == 0) mbar_arrive_expect_tx(&ctl->full[stage], CTAS * Cf::STAGE);
+                        if constexpr (PAIR) {
+                            const uint32_t full0 = map_to_cta(&ctl->full[stage], 0);
+                            tma_load_2d_pair(st, &tmA, k, row, full0);
+                            tma_load_3d_pair(st + Cf::A_BYTES, &tmB, k, t.col0 + rank * Cf::BN_CTA, WGRAD ? 0 : e, full0);
+                        } else {
+                            tma_load_2d(st, &tmA, k, row, &ctl->full[stage]);
+                            tma_load_3d(st + Cf::A_BYTES, &tmB, k, t.col0, WGRAD ? 0 : e, &ctl->full[stage]);
+                        }
                     }
                     __syncwarp();
                     issued |= 1u << stage;
@@ -298,77 +223,57 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                     if (++stage == Cf::STAGES) { stage = 0; phase ^= 1; }
                 }
             }
-            if (lane == 0 && *abort_flag)                 // copies in flight land before the CTA exits
+            if (lane == 0 && rank == 0 && *abort_flag)        // copies counted by this CTA's barriers land before it exits
                 for (int s = 0; s < Cf::STAGES; ++s)
                     if (issued & (1u << s)) mbar_wait(&ctl->full[s], (issued_parity >> s) & 1, abort_flag, a.status);
-        } else if (warp == 1) {
+        } else if (warp == 1 && rank == 0) {
             const uint32_t el = elect_one();
-            constexpr uint32_t idesc = instr_desc_e4m3(BM, BN);
+            constexpr uint32_t idesc = instr_desc_mxe4m3(PAIR ? 2 * BM : BM, BN);
             int stage = 0, acc = 0, e = 0;
             uint32_t phase = 0, acc_phase = 0;
             bool stop = false;
-            for (int tile = blockIdx.x; tile < total && !stop; tile += gridDim.x) {
-                int row0, col0, kb0, kbs;
-                locate(tile, e, row0, col0, kb0, kbs);
-                for (int kb = 0; kb < kbs; ++kb) {
-                    if (!mbar_wait_warp_quick(&ctl->tempty[acc], acc_phase ^ 1, abort_flag, a.status) ||
-                        !mbar_wait_warp_quick(&ctl->full[stage], phase, abort_flag, a.status)) { stop = true; break; }
+            for (int tile = worker; tile < total && !stop; tile += workers) {
+                const Tile t = locate(tile, e);
+                if (t.kbs == 0) continue;
+                if (!mbar_wait_warp_quick(&ctl->tempty[acc], acc_phase ^ 1, abort_flag, a.status)) break;
+                tc_fence_after();
+                for (int kb = 0; kb < t.kbs; ++kb) {
+                    if (!mbar_wait_warp_quick(&ctl->full[stage], phase, abort_flag, a.status)) { stop = true; break; }
                     tc_fence_after();
-                    const uint32_t st = smem_u32(smem + stage * Cf::STAGE);
+                    const uint32_t st = smem_u32(smem + stage * Cf::STAGE), sf = tmem_base + Cf::SF_COL + stage * Cf::SF_STRIDE;
 #pragma unroll
-                    for (int ks = 0; ks < 4; ++ks)
-                        mma_f8(el, tmem_base + acc * BN, smem_desc(st + ks * 32, 16, 1024), smem_desc(st + Cf::A_BYTES + ks * 32, 16, 1024), idesc, ks != 0);
-                    mma_commit(el, &ctl->empty[stage]);
-                    mma_commit(el, &ctl->tfull[acc]);
-                    if (++stage == Cf::STAGES) { stage = 0; phase ^= 1; }
-                    if (++acc == 2) { acc = 0; acc_phase ^= 1; }
-                }
-            }
-        } else if (warp == 2) {
-            int slot = 0, e = 0;
-            uint32_t phase = 0;
-            bool stop = false;
-            for (int tile = blockIdx.x; tile < total && !stop; tile += gridDim.x) {
-                int row0, col0, kb0, kbs;
-                locate(tile, e, row0, col0, kb0, kbs);
-                const float* sa = a.sa + (size_t)kb0 * a.M + row0;
-                const int rows = (int)(a.M - row0 < BM ? a.M - row0 : BM);
-                const float* sb = WGRAD ? a.sb + (size_t)kb0 * a.N + col0 : a.sb + ((size_t)e * a.Nb + col0 / kQ) * a.Kb;
-                const int cols = WGRAD ? min(a.N - col0, BN) : 0, nb = min(a.Nb - col0 / kQ, 2);
-                for (int kb = 0; kb < kbs; ++kb, sa += a.M) {
-                    if (!mbar_wait_warp_quick(&ctl->sempty[slot], phase ^ 1, abort_flag, a.status)) { stop = true; break; }
-                    const uint32_t dst = smem_u32(s_scales + slot * Cf::SCALES);
-#pragma unroll
-                    for (int r = lane; r < BM; r += 32) cp_async4(dst + 4 * r, sa + (r < rows ? r : 0), r < rows);
-                    if constexpr (WGRAD) {
-                        for (int c = lane; c < BN; c += 32) cp_async4(dst + 4 * (BM + c), sb + (c < cols ? c : 0), c < cols);
-                        sb += a.N;
-                    } else {      // a warp of either column half reads its own: with 128 columns they are the same block
-                        if (lane < 2) {
-                            const int b = BN == 256 ? lane : 0;
-                            cp_async4(dst + 4 * (BM + lane), sb + (size_t)(b < nb ? b : 0) * a.Kb + kb, b < nb);
-                        }
+                    for (int ks = 0; ks < 4; ++ks) {
+                        const uint64_t ad = smem_desc(st + ks * 32, 16, 1024), bd = smem_desc(st + Cf::A_BYTES + ks * 32, 16, 1024);
+                        if constexpr (PAIR) mma_mxf8_pair(el, tmem_base + acc * BN, ad, bd, idesc, sf, sf + Cf::SFB, (kb | ks) != 0);
+                        else mma_mxf8(el, tmem_base + acc * BN, ad, bd, idesc, sf, sf + Cf::SFB, (kb | ks) != 0);
                     }
-                    cp_async_arrive(&ctl->sfull[slot]);
-                    if (++slot == kScaleSlots) { slot = 0; phase ^= 1; }
+                    if constexpr (PAIR) mma_commit_pair(el, &ctl->empty[stage]);
+                    else mma_commit(el, &ctl->empty[stage]);
+                    if (++stage == Cf::STAGES) { stage = 0; phase ^= 1; }
                 }
+                if (stop) break;
+                if constexpr (PAIR) mma_commit_pair(el, &ctl->tfull[acc]);
+                else mma_commit(el, &ctl->tfull[acc]);
+                if (++acc == Cf::NACC) { acc = 0; acc_phase ^= 1; }
             }
-            asm volatile("cp.async.wait_all;" ::: "memory");      // none in flight when the CTA exits
         }
     }
     tc_fence_before();
     __syncthreads();
+    if constexpr (PAIR) cluster_sync_all();           // neither CTA leaves while the other may still arrive on its barriers or read its tiles
     if (warp == 1) {
         __syncwarp();
-        tmem_dealloc(tmem_base, Cf::TMEM_COLS);
+        if constexpr (PAIR) tmem_dealloc_pair(tmem_base, Cf::TMEM_COLS);
+        else tmem_dealloc(tmem_base, Cf::TMEM_COLS);
     }
 }
 
-template <int BN, bool WGRAD, int EPI>
+template <int BN, bool WGRAD, int EPI, bool PAIR>
 uoe_status launch_one(const Fp8Gemm& g, int* status, cudaStream_t s) {
-    using Cf = Cfg<BN>;
+    using Cf = Cfg<BN, PAIR>;
     static DeviceOnce once;
-    auto kern = fp8_gemm_kernel<BN, WGRAD, EPI>;
+    static DeviceValue pairs_cache;
+    auto kern = fp8_gemm_kernel<BN, WGRAD, EPI, PAIR>;
     const uoe_status st = smem_opt_in(once, kern, Cf::SMEM);
     if (st != UOE_OK) return st;
     const uint64_t Kp = (uint64_t)((g.K + kQ - 1) / kQ * kQ);
@@ -382,36 +287,47 @@ uoe_status launch_one(const Fp8Gemm& g, int* status, cudaStream_t s) {
     {
         const uint64_t dims[3] = {Kp, (uint64_t)g.N, (uint64_t)(g.wgrad ? 1 : g.n)};
         const uint64_t str[2] = {Kp, Kp * (uint64_t)g.N};
-        const uint32_t box[3] = {kQ, BN, 1};
+        const uint32_t box[3] = {kQ, Cf::BN_CTA, 1};
         if (!make_tmap(&tmB, g.B, 3, dims, str, box, CU_TENSOR_MAP_DATA_TYPE_UINT8)) return UOE_ERR_CUDA;
     }
-    Fp8Args a = {};
-    a.sa = g.sa; a.sb = g.sb; a.offsets = g.offsets;
-    a.n = g.n; a.N = g.N; a.Nb = q_blocks(g.N); a.M = g.M; a.Kb = (int)(Kp / kQ);
-    a.C = g.C; a.out_bf16 = g.out_bf16;
-    a.vec = ((size_t)g.N * (g.out_bf16 ? 2 : 4)) % 16 == 0 && aligned16(g.C);
-    a.bias = (const __nv_bfloat16*)g.bias; a.act = g.act;
-    a.q = (uint8_t*)g.q; a.qs = g.qs; a.ldq = q_pad(g.N);
-    a.status = status;
-    const long long m_tiles = (g.M + BM - 1) / BM, n_tiles = (g.N + BN - 1) / BN;
-    const long long tiles = m_tiles * n_tiles * (g.wgrad ? g.n : 1);
+    const Fp8Args a = fp8_args(g, status);
+    const long long tiles = ((g.M + Cf::TILE - 1) / Cf::TILE + (PAIR && !g.wgrad ? g.n : 0)) * ((g.N + BN - 1) / BN) * (g.wgrad ? g.n : 1);
     if (tiles > 0x3fffffffll) return UOE_ERR_UNSUPPORTED;
-    const int grid = (int)(tiles < sm_count() ? tiles : sm_count());
     ProfScope ps(g.label, s);
-    launch_k(kern, dim3(grid), dim3(Cf::THREADS), (size_t)Cf::SMEM, s, tmA, tmB, a);
+    if constexpr (PAIR) {
+        const int dev = current_device();
+        if (dev < 0) return UOE_ERR_CUDA;
+        if (!pairs_cache.has(dev)) {
+            int v = 0;
+            UOE_CUDA_OK(max_resident_pairs(kern, Cf::THREADS, Cf::SMEM, &v));
+            if (v < 1) return UOE_ERR_CUDA;
+            pairs_cache.set(dev, v);
+        }
+        const long long pairs = pairs_cache.get(dev);
+        launch_k_pairs(kern, dim3(2 * (unsigned)(tiles < pairs ? tiles : pairs)), dim3(Cf::THREADS), (size_t)Cf::SMEM, s, tmA, tmB, a);
+    } else {
+        launch_k(kern, dim3((unsigned)(tiles < sm_count() ? tiles : sm_count())), dim3(Cf::THREADS), (size_t)Cf::SMEM, s, tmA, tmB, a);
+    }
     UOE_LAUNCHED();
     return UOE_OK;
+}
+
+template <bool WGRAD, int EPI>
+uoe_status dispatch(const Fp8Gemm& g, int* status, cudaStream_t s) {
+    const long long cols256 = (g.N + 255) / 256, mats = g.wgrad ? g.n : 1;
+    if (g.N > 128 && (g.M + 255) / 256 * cols256 * mats >= sm_count()) return launch_one<256, WGRAD, EPI, true>(g, status, s);
+    if (EPI == kFp8ActQuant || (g.N > 128 && (g.M + 127) / 128 * cols256 * mats >= sm_count())) return launch_one<256, WGRAD, EPI, false>(g, status, s);
+    if constexpr (EPI != kFp8ActQuant) return launch_one<128, WGRAD, EPI, false>(g, status, s);
+    return UOE_ERR_UNSUPPORTED;
 }
 
 }  // namespace
 
 uoe_status launch_fp8_gemm(const Fp8Gemm& g, int* status, cudaStream_t s) {
     if (g.n > kMaxExperts) return UOE_ERR_UNSUPPORTED;
-    if (g.epi == kFp8ActQuant) return launch_one<256, false, kFp8ActQuant>(g, status, s);
-    const long long tiles256 = (g.M + BM - 1) / BM * ((g.N + 255) / 256) * (g.wgrad ? g.n : 1);
-    const bool wide = g.N > 128 && tiles256 >= sm_count();
-    if (g.wgrad) return wide ? launch_one<256, true, kFp8Store>(g, status, s) : launch_one<128, true, kFp8Store>(g, status, s);
-    return wide ? launch_one<256, false, kFp8Store>(g, status, s) : launch_one<128, false, kFp8Store>(g, status, s);
+    if (g.any_scale) return launch_fp8_gemm_any(g, status, s);
+    if (g.wgrad) return dispatch<true, kFp8Store>(g, status, s);
+    return g.epi == kFp8ActQuant ? dispatch<false, kFp8ActQuant>(g, status, s) : dispatch<false, kFp8Store>(g, status, s);
 }
 
 }  // namespace uoe
@@ -422,7 +338,7 @@ namespace {
 uoe_status fp8_check(const uoe_fp8_problem* p, const void* A, const float* sa, const void* B, const float* sb, const int32_t* offsets, const void* C,
                      const void* ws, size_t ws_bytes) {
     if (!p || p->n < 1 || p->M < 1 || p->N < 1 || p->K < 1) return UOE_ERR_INVALID_ARG;
-    if (p->dtype != UOE_F32 && p->dtype != UOE_BF16) return UOE_ERR_INVALID_ARG;
+    if ((p->dtype != UOE_F32 && p->dtype != UOE_BF16) || (p->flags & ~UOE_FP8_ANY_SCALE)) return UOE_ERR_INVALID_ARG;
     if (!A || !sa || !B || !sb || !C || !ws) return UOE_ERR_INVALID_ARG;
     if (!aligned16(A) || !aligned16(sa) || !aligned16(B) || !aligned16(sb) || !aligned16(C) || !aligned16(ws)) return UOE_ERR_INVALID_ARG;
     if (!offsets && p->n > 1) return UOE_ERR_INVALID_ARG;
@@ -442,6 +358,7 @@ extern "C" uoe_status uoe_fp8_gemm(const uoe_fp8_problem* p, const void* A, cons
     const uoe_status st = fp8_check(p, A, a_scale, W, w_scale, expert_offsets, C, ws, ws_bytes);
     if (st != UOE_OK) return st;
     Fp8Gemm g{A, a_scale, W, w_scale, expert_offsets, p->n, p->M, p->N, p->K, false, C, p->dtype == UOE_BF16};
+    g.any_scale = p->flags & UOE_FP8_ANY_SCALE;
     return launch_fp8_gemm(g, (int*)ws, (cudaStream_t)cuda_stream);
 }
 
@@ -451,6 +368,7 @@ extern "C" uoe_status uoe_fp8_wgrad(const uoe_fp8_problem* p, const void* A, con
     if (st != UOE_OK) return st;
     if (p->dtype != UOE_F32) return UOE_ERR_UNSUPPORTED;
     Fp8Gemm g{A, a_scale, B, b_scale, expert_offsets, p->n, p->M, p->N, p->K, true, dW, false};
+    g.any_scale = p->flags & UOE_FP8_ANY_SCALE;
     g.label = "fp8_wgrad";
     return launch_fp8_gemm(g, (int*)ws, (cudaStream_t)cuda_stream);
 }

@@ -1,0 +1,145 @@
+// What the kernels for products of 8-bit operands share: arguments, the experts' regions, what becomes of a tile's sums.
+#pragma once
+#include "fp8.cuh"
+
+namespace uoe {
+
+constexpr int kMaxExperts = 32;
+
+struct Fp8Args {
+    const float *sa, *sb;
+    const int* offsets;
+    int n, N, Nb;                     // columns of C, blocks of 128 of them
+    long long M;                      // rows of C (rows of the A operand)
+    int Kb;                           // blocks of the contraction (wgrad: in all regions together)
+    void* C;
+    int out_bf16, vec;                // vec: rows of C may be stored in 32-byte pieces
+    const __nv_bfloat16* bias;
+    int act;
+    uint8_t* q;
+    float* qs;
+    long long ldq;
+    int* status;
+};
+
+// phi with errors of float32 size (the result is compared with a rounding border of its own)
+__device__ __forceinline__ float act_precise(float h, int act) {
+    switch (act) {
+        case UOE_ACT_SILU: return __fdividef(h, 1.0f + __expf(-h));
+        case UOE_ACT_GELU_TANH: {
+            const float u = 0.79788456080286536f * (h + 0.044715f * h * h * h);
+            return __fdividef(h, 1.0f + __expf(-2.0f * u));             // h/2 (1 + tanh u)
+        }
+        default: return act_apply(h, act);
+    }
+}
+
+// First row (wgrad: position in the contraction) of every expert, and its first row tile.
+struct Regions {
+    int offs[kMaxExperts + 1];
+    int tstart[kMaxExperts + 1];
+};
+// By one warp.  Without offsets all rows are one expert's; wgrad: every expert has all row tiles of C.  Offsets that are no regions
+// (not ascending multiples of 128 within the operand) are reported, and there are no tiles.
+template <bool WGRAD, int TILE>
+__device__ __forceinline__ void load_regions(Regions& g, const Fp8Args& a, int m_tiles, int lane) {
+    const int n = a.n;
+    const long long limit = WGRAD ? (long long)a.Kb * kQ : a.M;
+    int o = 0, o1 = 0;
+    if (a.offsets) {
+        o = lane < n ? a.offsets[lane] : 0;
+        o1 = lane < n ? a.offsets[lane + 1] : 0;
+    } else if (lane == 0) {
+        o1 = WGRAD ? a.Kb * kQ : (int)((a.M + kQ - 1) / kQ * kQ);
+    }
+    const bool ok = lane >= n || !a.offsets || (o >= 0 && o1 >= o && o1 <= limit && ((o | o1) & (kQ - 1)) == 0);
+    const bool bad = !__all_sync(0xffffffffu, ok);
+    const int tiles = lane < n && !bad ? (WGRAD ? m_tiles : (o1 - o + TILE - 1) / TILE) : 0;
+    int incl = tiles;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += v;
+    }
+    if (lane < n) {
+        g.offs[lane] = o;
+        g.offs[lane + 1] = o1;                 // (the neighbour writes the same number)
+        g.tstart[lane] = incl - tiles;
+        if (lane == n - 1) g.tstart[n] = incl;
+    }
+    if (lane == 0 && bad) set_status(a.status, UOE_ERR_DEVICE_INDEX);
+}
+
+// One thread's CW sums of row `row`, columns col .. col + CW (within the rows and columns there are: row < M, col < N).
+template <int CW, bool WGRAD, int EPI>
+__device__ __forceinline__ void store_tile(const Fp8Args& a, float* sum, int e, long long row, int col) {
+    if constexpr (EPI == kFp8ActQuant) {
+        static_assert(EPI != kFp8ActQuant || (!WGRAD && CW == kQ), "a thread holds one block of the result");
+        uint32_t m = 0;
+#pragma unroll
+        for (int q = 0; q < CW; ++q) {
+            if (a.bias && col + q < a.N) sum[q] += to_f32(a.bias[(size_t)e * a.N + col + q]);
+            sum[q] = act_precise(sum[q], a.act);
+            m = max(m, abs_bits(sum[q]));
+        }
+        const BlockScale b = block_scale(m);
+        a.qs[(size_t)(col / kQ) * a.M + row] = b.s;
+        uint8_t* o = a.q + (size_t)row * a.ldq + col;
+        const bool whole = sector_aligned(o);
+#pragma unroll
+        for (int q = 0; q < CW; q += 32) {
+            uint32_t w[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) w[u] = e4m3x4(sum[q + 4 * u], sum[q + 4 * u + 1], sum[q + 4 * u + 2], sum[q + 4 * u + 3], b.inv);
+            st_sector(o + q, make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]), whole);
+        }
+    } else {
+        const size_t at = ((WGRAD ? (size_t)e * a.M : 0) + row) * a.N + col;
+        if (a.bias) {
+#pragma unroll
+            for (int q = 0; q < CW; ++q)
+                if (col + q < a.N) sum[q] += to_f32(a.bias[(size_t)e * a.N + col + q]);
+        }
+        if (a.out_bf16) {
+            __nv_bfloat16* o = (__nv_bfloat16*)a.C + at;
+            if (a.vec && col + CW <= a.N) {
+                const bool whole = sector_aligned(o);
+#pragma unroll
+                for (int q = 0; q < CW; q += 16) st_sector(o + q, pack16<__nv_bfloat16>(sum + q), pack16<__nv_bfloat16>(sum + q + 8), whole);
+            } else {
+#pragma unroll
+                for (int q = 0; q < CW; ++q)
+                    if (col + q < a.N) o[q] = __float2bfloat16_rn(sum[q]);
+            }
+        } else {
+            float* o = (float*)a.C + at;
+            if (a.vec && col + CW <= a.N) {
+                const bool whole = sector_aligned(o);
+#pragma unroll
+                for (int q = 0; q < CW; q += 8) st_sector(o + q, pack16<float>(sum + q), pack16<float>(sum + q + 4), whole);
+            } else {
+#pragma unroll
+                for (int q = 0; q < CW; ++q)
+                    if (col + q < a.N) o[q] = sum[q];
+            }
+        }
+    }
+}
+
+inline Fp8Args fp8_args(const Fp8Gemm& g, int* status) {
+    const uint64_t Kp = (uint64_t)((g.K + kQ - 1) / kQ * kQ);
+    Fp8Args a = {};
+    a.sa = g.sa; a.sb = g.sb; a.offsets = g.offsets;
+    a.n = g.n; a.N = g.N; a.Nb = q_blocks(g.N); a.M = g.M; a.Kb = (int)(Kp / kQ);
+    a.C = g.C; a.out_bf16 = g.out_bf16;
+    a.vec = ((size_t)g.N * (g.out_bf16 ? 2 : 4)) % 16 == 0 && aligned16(g.C);
+    a.bias = (const __nv_bfloat16*)g.bias; a.act = g.act;
+    a.q = (uint8_t*)g.q; a.qs = g.qs; a.ldq = q_pad(g.N);
+    a.status = status;
+    return a;
+}
+
+// Factors of any size: blocks' products added outside the tensor cores (fp8_gemm_any_tcgen05.cu).
+uoe_status launch_fp8_gemm_any(const Fp8Gemm& g, int* status, cudaStream_t s);
+
+}  // namespace uoe

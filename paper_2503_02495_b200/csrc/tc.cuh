@@ -139,6 +139,17 @@ __device__ __forceinline__ void mma_f8(uint32_t elected, uint32_t d_tmem, uint64
         "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
         :: "r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"((uint32_t)accumulate), "r"(elected) : "memory");
 }
+// the same with a power-of-two scale (one exponent byte) per row of A, per row of B and 32 of the contraction; the scales of a step
+// lie in TMEM: row r of 128 in lane r % 32 (and the three lanes 32 apart), column r / 32
+__device__ __forceinline__ void mma_mxf8(uint32_t elected, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                         uint32_t sfa_tmem, uint32_t sfb_tmem, bool accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "setp.ne.b32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%6], [%7], p;\n\t}"
+        :: "r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"((uint32_t)accumulate), "r"(elected), "r"(sfa_tmem), "r"(sfb_tmem) : "memory");
+}
 // The mbarrier gets one arrival when all MMAs issued so far by the elected lane have completed.
 __device__ __forceinline__ void mma_commit(uint32_t elected, uint64_t* bar) {
     asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
@@ -158,6 +169,16 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* v) {
           "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
         : "r"(taddr) : "memory");
 }
+// 32 lanes x 4 or 8 columns, register -> TMEM: thread t of the warp writes lane (base lane + t)
+__device__ __forceinline__ void tmem_st4(uint32_t taddr, const uint32_t* v) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};"
+                 :: "r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* v) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 :: "r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // ---- CTA pairs (cluster of two, tcgen05 cta_group::2) ------------------------------------------
@@ -217,6 +238,16 @@ __device__ __forceinline__ void mma_bf16_pair(uint32_t elected, uint32_t d_tmem,
         "@q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
         :: "r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"((uint32_t)accumulate), "r"(elected) : "memory");
 }
+// (block-scaled: each CTA's TMEM holds the scales of its own 128 rows of A and of all N rows of B)
+__device__ __forceinline__ void mma_mxf8_pair(uint32_t elected, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                              uint32_t sfa_tmem, uint32_t sfb_tmem, bool accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "setp.ne.b32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%6], [%7], p;\n\t}"
+        :: "r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"((uint32_t)accumulate), "r"(elected), "r"(sfa_tmem), "r"(sfb_tmem) : "memory");
+}
 // one arrival on the barrier at this offset in each CTA of the pair when all MMAs issued so far by the elected lane have
 // completed (two commits, one per CTA: the second names the other CTA's barrier by its cluster address)
 __device__ __forceinline__ void mma_commit_pair(uint32_t elected, uint64_t* bar) {
@@ -255,6 +286,11 @@ __host__ __device__ constexpr uint32_t instr_desc_bf16(int M, int N, bool a_mn_m
 // Instruction descriptor for kind::f8f6f4 with e4m3 A and B (formats 0), both K-major, fp32 D.
 __host__ __device__ constexpr uint32_t instr_desc_e4m3(int M, int N) {
     return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+// Instruction descriptor for kind::mxf8f6f4 with e4m3 A and B, both K-major, exponent-byte scales (bit 23), scale byte 0 of each word.
+__host__ __device__ constexpr uint32_t instr_desc_mxe4m3(int M, int N) {
+    return ((uint32_t)(N >> 3) << 17) | (1u << 23) | ((uint32_t)(M >> 4) << 24);
 }
 
 }  // namespace tc

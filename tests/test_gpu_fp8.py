@@ -3,8 +3,9 @@
 Quantisation is exact up to its one rounding, which both sides do on the same exact quotient: values and scales must be equal.
 Products: the operands are exact on both sides (e4m3 values times float32 scales, formed in float64 by the reference), so the kernel's
 error is its float32 arithmetic and the rounding of the result.  Per element of the sum: one product of two e4m3 values (exact in float32:
-2 x 4 bits), at most 128 additions in the tensor core and Kb additions outside it, two roundings of the scales' product.  With
-gamma = (128 + Kb + 4) 2^-23 (a tensor-core addition counted as truncating: one step of float32) the error is at most
+2 x 4 bits), at most 128 additions in the tensor core and Kb additions outside it, two roundings of the scales' product.  (With scales
+that are powers of two the tensor core adds all of K, 32 products a step.)  With gamma = (128 + 4 Kb + 4) 2^-23 (a tensor-core addition counted
+as truncating: one step of float32) the error is at most
 gamma * sum |a| |b|; bfloat16 results add half a step, 2^-8 / 2 ... counted as 2^-8 of the result.
 """
 import numpy as np
@@ -136,7 +137,7 @@ def _blk_values(q, s):
 
 
 def _gamma(Kb):
-    return (128 + Kb + 4) * 2.0 ** -23
+    return (128 + 4 * Kb + 4) * 2.0 ** -23
 
 
 def _regions(counts):
@@ -164,15 +165,17 @@ GEMMS = {
     "wide": dict(counts=[1000], N=1000, K=384),
     "long": dict(counts=[130], N=130, K=5000),
     "experts": dict(counts=[100, 0, 300, 1], slack=130, N=200, K=260),
+    "pairs": dict(counts=[5000, 128, 4100, 0, 3000, 129], slack=300, N=1030, K=640),
     "experts_wide_tiles": dict(counts=[2000, 3500, 129, 0, 4000], slack=1, N=1030, K=512),
     "all_empty": dict(counts=[0, 0, 0], slack=200, N=64, K=64),
     "thirty_two": dict(counts=[5] * 32, N=40, K=48),
 }
 
 
+@pytest.mark.parametrize("any_scale", [False, True])
 @pytest.mark.parametrize("out", ["bf16", "f32"])
 @pytest.mark.parametrize("name", list(GEMMS))
-def test_gemm(name, out):
+def test_gemm(name, out, any_scale):
     import paper_2503_02495_b200 as uoe
     c = GEMMS[name]
     n, N, K = len(c["counts"]), c["N"], c["K"]
@@ -185,12 +188,13 @@ def test_gemm(name, out):
     A, sa = uoe.uoe_fp8_quantize(x.cuda(), "rows")
     Wq, sw = uoe.uoe_fp8_quantize(W.cuda(), "blocks")
     g = torch.Generator().manual_seed(9)
-    sa *= (0.5 + torch.rand(sa.shape, generator=g)).cuda()          # scales need not be powers of two
-    sw *= (0.5 + torch.rand(sw.shape, generator=g)).cuda()
+    if any_scale:                                                   # scales that are no powers of two
+        sa *= (0.5 + torch.rand(sa.shape, generator=g)).cuda()
+        sw *= (0.5 + torch.rand(sw.shape, generator=g)).cuda()
     dt = torch.bfloat16 if out == "bf16" else torch.float32
     C = torch.full((M, N), -3.0, dtype=dt, device="cuda")
     offsets = torch.tensor(off, dtype=torch.int32, device="cuda") if n > 1 else None
-    prob = uoe.Fp8Problem(n=n, M=M, N=N, K=K, dtype=out)
+    prob = uoe.Fp8Problem(n=n, M=M, N=N, K=K, dtype=out, any_scale=any_scale)
     got = uoe.uoe_fp8_gemm(prob, A, sa, Wq, sw, offsets, C=C)
     a = _vec_values(A.cpu(), sa.cpu())
     bounds = off if n > 1 else [0, M]
@@ -206,13 +210,15 @@ WGRADS = {
     "one": dict(counts=[1], M=8, N=8),
     "odd": dict(counts=[130, 0, 400, 1], M=77, N=333),
     "wide": dict(counts=[3000, 1000, 2500], M=1100, N=600),
+    "pairs": dict(counts=[300, 0, 128, 500, 1000, 129, 1, 700], M=1300, N=1000),
     "many_tiles": dict(counts=[300, 0, 128, 500], M=1024, N=2304),
     "empty": dict(counts=[0, 0], M=40, N=24),
 }
 
 
+@pytest.mark.parametrize("any_scale", [False, True])
 @pytest.mark.parametrize("name", list(WGRADS))
-def test_wgrad(name):
+def test_wgrad(name, any_scale):
     import paper_2503_02495_b200 as uoe
     c = WGRADS[name]
     n, M, N = len(c["counts"]), c["M"], c["N"]
@@ -224,9 +230,10 @@ def test_wgrad(name):
     A, sa = uoe.uoe_fp8_quantize(x.cuda(), "cols")
     B, sb = uoe.uoe_fp8_quantize(dy.cuda(), "cols")
     g = torch.Generator().manual_seed(9)
-    sa *= (0.5 + torch.rand(sa.shape, generator=g)).cuda()
-    sb *= (0.5 + torch.rand(sb.shape, generator=g)).cuda()
-    prob = uoe.Fp8Problem(n=n, M=M, N=N, K=K, dtype="f32")
+    if any_scale:
+        sa *= (0.5 + torch.rand(sa.shape, generator=g)).cuda()
+        sb *= (0.5 + torch.rand(sb.shape, generator=g)).cuda()
+    prob = uoe.Fp8Problem(n=n, M=M, N=N, K=K, dtype="f32", any_scale=any_scale)
     dW = torch.full((n, M, N), -3.0, device="cuda")
     got = uoe.uoe_fp8_wgrad(prob, A, sa, B, sb, torch.tensor(off, dtype=torch.int32, device="cuda"), dW=dW)
     a, b = _vec_values(A.cpu(), sa.cpu()), _vec_values(B.cpu(), sb.cpu())
@@ -264,3 +271,20 @@ def test_a_row_with_a_nan_spoils_only_itself():
             got[70] = ref[70]
             assert torch.equal(got, ref)
         ref = got
+
+
+def test_a_scale_that_is_no_power_of_two_is_reported():
+    import paper_2503_02495_b200 as uoe
+    A, sa = uoe.uoe_fp8_quantize(_rand(1, 200, 300).cuda(), "rows")
+    W, sw = uoe.uoe_fp8_quantize(_rand(2, 1, 64, 300).cuda(), "blocks")
+    prob = uoe.Fp8Problem(n=1, M=200, N=64, K=300)
+    ref = uoe.uoe_fp8_gemm(prob, A, sa, W, sw)
+    for bad in (0.75, 0.0, -1.0, 2.0 ** -130):
+        s2 = sa.clone()
+        s2[1, 150] = bad
+        C, ws = torch.empty_like(ref), uoe.alloc_fp8_workspace(prob)
+        uoe.uoe_fp8_gemm(prob, A, s2, W, sw, C=C, ws=ws, check=False)
+        assert uoe.uoe_read_device_status(ws) == 8 and "power of two" in uoe.status_string(8)
+        assert torch.isnan(C[150]).all()
+        C[150] = ref[150]
+        assert torch.equal(C, ref)
