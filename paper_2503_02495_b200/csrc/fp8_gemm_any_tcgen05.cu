@@ -34,15 +34,6 @@ template <int BN> struct Cfg {
     static constexpr int SMEM = STAGES * STAGE + 1024 /* alignment */ + CTL_BYTES + kScaleSlots * SCALES * 4;
 };
 
-// four bytes, zero where `real` is false (the address is a valid one all the same)
-__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, bool real) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" :: "r"(dst), "l"(src), "r"(real ? 4 : 0) : "memory");
-}
-// one arrival of this thread on the barrier when all its copies so far have landed (counted in the barrier's 32)
-__device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
-    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" :: "r"(smem_u32(bar)) : "memory");
-}
-
 struct Ctl {
     uint64_t full[8], empty[8], tfull[2], tempty[2], sfull[kScaleSlots], sempty[kScaleSlots];
     uint32_t tmem_base;
@@ -235,15 +226,15 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                     if (!mbar_wait_warp_quick(&ctl->sempty[slot], phase ^ 1, abort_flag, a.status)) { stop = true; break; }
                     const uint32_t dst = smem_u32(s_scales + slot * Cf::SCALES);
 #pragma unroll
-                    for (int r = lane; r < BM; r += 32) cp_async4(dst + 4 * r, sa + (r < rows ? r : 0), r < rows);
+                    for (int r = lane; r < BM; r += 32)
+                        if (r < rows) cp_async4(dst + 4 * r, sa + r);
                     if constexpr (WGRAD) {
-                        for (int c = lane; c < BN; c += 32) cp_async4(dst + 4 * (BM + c), sb + (c < cols ? c : 0), c < cols);
+                        for (int c = lane; c < BN; c += 32)
+                            if (c < cols) cp_async4(dst + 4 * (BM + c), sb + c);
                         sb += a.N;
                     } else {      // a warp of either column half reads its own: with 128 columns they are the same block
-                        if (lane < 2) {
-                            const int b = BN == 256 ? lane : 0;
-                            cp_async4(dst + 4 * (BM + lane), sb + (size_t)(b < nb ? b : 0) * a.Kb + kb, b < nb);
-                        }
+                        const int b = BN == 256 ? lane : 0;
+                        if (lane < 2 && b < nb) cp_async4(dst + 4 * (BM + lane), sb + (size_t)b * a.Kb + kb);
                     }
                     cp_async_arrive(&ctl->sfull[slot]);
                     if (++slot == kScaleSlots) { slot = 0; phase ^= 1; }

@@ -8,8 +8,9 @@
 // kernel).  A persistent CTA (pair) per SM (two) walks the tiles, 128 x BN or, by a pair of CTAs (cta_group::2), 256 x 256:
 //   warp 0       TMA producer: a stage is one block of the contraction, 128 bytes of every row of A and of B (128-byte swizzle)
 //   warp 1       MMA issuer: four steps of 32 per stage
-//   warps 4..7   the stage's scales: float32 -> exponent byte, once for every lane quarter of TMEM (a warp each), four blocks ahead
-//                in registers.  A scale holds for the whole stage, so its byte fills the word and the steps need no index.
+//   warp 2       the scales of the blocks to come, by 4-byte asynchronous copies (their rows start anywhere) into a ring of their own
+//   warps 4..7   the stage's scales: float32 -> exponent byte -> TMEM, once for every lane quarter (a warp each).  A scale holds
+//                for the whole stage, so its byte fills the word and the four steps need no index.
 //   warps 8..15  write-out: a warp has 32 rows (its TMEM lane quarter) and half of the columns, all of them in registers before it
 //                gives the accumulator back (256 columns and the scales leave room for one accumulator: the next tile's products
 //                wait for these loads, not for the arithmetic and the stores)
@@ -25,6 +26,8 @@ using namespace tc;
 
 constexpr int BM = 128;
 
+constexpr int kScaleSlots = 8;
+
 template <int BN, bool PAIR> struct Cfg {
     static_assert(!PAIR || BN == 256, "a pair works 256 x 256");
     static constexpr int BN_CTA = PAIR ? BN / 2 : BN;                 // rows of B this CTA loads
@@ -35,26 +38,25 @@ template <int BN, bool PAIR> struct Cfg {
     static constexpr int CW = BN / 2;
     static constexpr int EPI_WARPS = 8, SCALE_WARPS = 4, THREADS = 128 + 128 + 32 * EPI_WARPS;
     static constexpr int TMEM_COLS = 512, SF_COL = 256, SF_STRIDE = 16, SFB = 8;      // scales of stage s: A at SF_COL + 16 s, B 8 behind
-    static constexpr int SMEM = STAGES * STAGE + 1024 /* alignment */ + 1024 /* control */;
+    static constexpr int SCALES = BM + BN;                            // floats of a block's scales: A's rows, then B's rows or blocks
+    static constexpr int SMEM = STAGES * STAGE + 1024 /* alignment */ + 1024 /* control */ + kScaleSlots * SCALES * 4;
 };
 
 struct Ctl {
-    uint64_t full[8], empty[8], tfull[2], tempty[2];
+    uint64_t full[8], empty[8], tfull[2], tempty[2], sfull[kScaleSlots], sempty[kScaleSlots];
     uint32_t tmem_base;
     int abort_flag;
     Regions reg;
 };
 static_assert(sizeof(Ctl) <= 1024, "control block");
 
-// The scale's exponent byte in all four bytes of a word; 0xff stands for NaN.
-__device__ __forceinline__ uint32_t exponent_word(float s, int* status) {
-    const uint32_t b = __float_as_uint(s);
-    uint32_t e = b >> 23;
-    if (((b & 0x7fffffu) != 0 || e - 1 >= 254u) && e != 255) {        // not a power of two
-        set_status(status, UOE_ERR_FP8_SCALE);
-        e = 255;
-    }
-    return e * 0x01010101u;
+// The scale's exponent byte in all four bytes of a word; 0xff, which stands for NaN, where it is no power of two (a scale that is NaN
+// itself is no news).  Without a branch: a look at the status word per scale cost 1000 cycles per block.
+__device__ __forceinline__ uint32_t exponent_word(float s, bool there, bool& bad) {
+    const uint32_t b = there ? __float_as_uint(s) : 0x3f800000u, e = b >> 23;
+    const bool pow2 = (b & 0x7fffffu) == 0 && e - 1 < 254u;
+    bad |= !pow2 && e != 255;
+    return __byte_perm(pow2 ? e : 255u, 0, 0);
 }
 
 template <int BN, bool WGRAD, int EPI, bool PAIR>
@@ -75,6 +77,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         // (a pair's products are issued by rank 0, on whose barriers both CTAs' copies, scales and write-outs arrive)
         for (int s = 0; s < Cf::STAGES; ++s) { mbar_init(&ctl->full[s], 1 + CTAS * Cf::SCALE_WARPS); mbar_init(&ctl->empty[s], 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(&ctl->tfull[i], 1); mbar_init(&ctl->tempty[i], CTAS * Cf::EPI_WARPS); }
+        for (int i = 0; i < kScaleSlots; ++i) { mbar_init(&ctl->sfull[i], 32); mbar_init(&ctl->sempty[i], Cf::SCALE_WARPS); }
         ctl->abort_flag = 0;
         fence_barrier_init();
         prefetch_tmap(&tmA);
@@ -92,6 +95,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     if constexpr (PAIR) cluster_sync_all();           // the other CTA's barriers exist before anything arrives on them
     tc_fence_after();
     const uint32_t tmem_base = ctl->tmem_base;
+    float* s_scales = (float*)((uint8_t*)ctl + 1024);
     const int n_tiles = (a.N + BN - 1) / BN;
     const int total = ctl->reg.tstart[n] * n_tiles;
 
@@ -129,7 +133,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) {
-                    if constexpr (PAIR) mbar_arrive_cluster(map_to_cta(&ctl->tempty[acc], 0));
+                    if constexpr (PAIR) mbar_arrive_cluster_relaxed(map_to_cta(&ctl->tempty[acc], 0));
                     else mbar_arrive(&ctl->tempty[acc]);
                 }
                 if (++acc == Cf::NACC) { acc = 0; acc_phase ^= 1; }
@@ -145,55 +149,45 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         const uint32_t quarter = (uint32_t)((warp & 3) * 32) << 16;
         constexpr int NB = WGRAD ? BN / 32 : (BN + kQ - 1) / kQ;      // scales of B per lane: its columns', or the column blocks'
-        constexpr int AHEAD = WGRAD ? 2 : 4;
-        int stage = 0, e = 0;
-        uint32_t phase = 0;
-        bool stop = false;
+        int stage = 0, e = 0, slot = 0;
+        uint32_t phase = 0, slot_phase = 0;
+        bool stop = false, bad = false;
         for (int tile = worker; tile < total && !stop; tile += workers) {
             const Tile t = locate(tile, e);
-            const float* sa = a.sa + (size_t)t.kb0 * a.M + t.row0;
-            const float* sb = WGRAD ? a.sb + (size_t)t.kb0 * a.N + t.col0 : a.sb + ((size_t)e * a.Nb + t.col0 / kQ) * a.Kb;
-            float ra[AHEAD][4], rb[AHEAD][NB];
-            auto ask = [&](int kb, float* ra, float* rb) {            // scales of block kb (1 where there are no rows of this expert)
+            const int rows = t.row_end - t.row0, cols = a.N - t.col0;
+            for (int kb = 0; kb < t.kbs; ++kb) {
+                if (!mbar_wait_warp_quick(&ctl->sfull[slot], slot_phase, abort_flag, a.status)) { stop = true; break; }
+                const float* sc = s_scales + slot * Cf::SCALES;
+                uint32_t wa[4], wn[NB], wb[8];                        // (1 where there are no rows of this expert, or no columns)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) ra[q] = kb < t.kbs && t.row0 + q * 32 + lane < t.row_end ? __ldg(sa + (size_t)kb * a.M + q * 32 + lane) : 1.f;
+                for (int q = 0; q < 4; ++q) wa[q] = exponent_word(sc[q * 32 + lane], lane < rows - q * 32, bad);
 #pragma unroll
                 for (int q = 0; q < NB; ++q) {
-                    if constexpr (WGRAD) rb[q] = kb < t.kbs && t.col0 + q * 32 + lane < a.N ? __ldg(sb + (size_t)kb * a.N + q * 32 + lane) : 1.f;
-                    else rb[q] = kb < t.kbs && t.col0 + q * kQ < a.N ? __ldg(sb + (size_t)q * a.Kb + kb) : 1.f;
+                    if constexpr (WGRAD) wn[q] = exponent_word(sc[BM + q * 32 + lane], lane < cols - q * 32, bad);
+                    else wn[q] = exponent_word(sc[BM + q], cols > q * kQ, bad);
                 }
-            };
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) ask(u, ra[u], rb[u]);
-            for (int kb0 = 0; kb0 < t.kbs && !stop; kb0 += AHEAD) {
-#pragma unroll
-                for (int u = 0; u < AHEAD; ++u) {
-                    if (kb0 + u >= t.kbs) break;
-                    uint32_t wa[4], wb[8];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) wa[q] = exponent_word(ra[u][q], a.status);
-#pragma unroll
-                    for (int q = 0; q < NB; ++q) rb[u][q] = __uint_as_float(exponent_word(rb[u][q], a.status));
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) wb[q] = __float_as_uint(rb[u][WGRAD ? q % NB : (q / 4) % NB]);
-                    ask(kb0 + u + AHEAD, ra[u], rb[u]);
-                    if (!mbar_wait_warp_quick(&ctl->empty[stage], phase ^ 1, abort_flag, a.status)) { stop = true; break; }
-                    tc_fence_after();
-                    const uint32_t sf = tmem_base + Cf::SF_COL + stage * Cf::SF_STRIDE + quarter;
-                    tmem_st4(sf, wa);
-                    if constexpr (BN == 256) tmem_st8(sf + Cf::SFB, wb);
-                    else tmem_st4(sf + Cf::SFB, wb);
-                    tmem_st_wait();
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) {
-                        if constexpr (PAIR) mbar_arrive_cluster(map_to_cta(&ctl->full[stage], 0));
-                        else mbar_arrive(&ctl->full[stage]);
-                    }
-                    if (++stage == Cf::STAGES) { stage = 0; phase ^= 1; }
+                for (int q = 0; q < 8; ++q) wb[q] = wn[WGRAD ? q % NB : (q / 4) % NB];
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&ctl->sempty[slot]);
+                if (++slot == kScaleSlots) { slot = 0; slot_phase ^= 1; }
+                if (!mbar_wait_warp_quick(&ctl->empty[stage], phase ^ 1, abort_flag, a.status)) { stop = true; break; }
+                tc_fence_after();
+                const uint32_t sf = tmem_base + Cf::SF_COL + stage * Cf::SF_STRIDE + quarter;
+                tmem_st4(sf, wa);
+                if constexpr (BN == 256) tmem_st8(sf + Cf::SFB, wb);
+                else tmem_st4(sf + Cf::SFB, wb);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if constexpr (PAIR) mbar_arrive_cluster_relaxed(map_to_cta(&ctl->full[stage], 0));
+                    else mbar_arrive(&ctl->full[stage]);
                 }
+                if (++stage == Cf::STAGES) { stage = 0; phase ^= 1; }
             }
         }
+        if (bad) set_status(a.status, UOE_ERR_FP8_SCALE);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (warp == 0) {
@@ -256,6 +250,33 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 else mma_commit(el, &ctl->tfull[acc]);
                 if (++acc == Cf::NACC) { acc = 0; acc_phase ^= 1; }
             }
+        } else if (warp == 2) {
+            int slot = 0, e = 0;
+            uint32_t phase = 0;
+            bool stop = false;
+            for (int tile = worker; tile < total && !stop; tile += workers) {
+                const Tile t = locate(tile, e);
+                const float* sa = a.sa + (size_t)t.kb0 * a.M + t.row0;
+                const float* sb = WGRAD ? a.sb + (size_t)t.kb0 * a.N + t.col0 : a.sb + ((size_t)e * a.Nb + t.col0 / kQ) * a.Kb;
+                for (int kb = 0; kb < t.kbs; ++kb, sa += a.M) {
+                    if (!mbar_wait_warp_quick(&ctl->sempty[slot], phase ^ 1, abort_flag, a.status)) { stop = true; break; }
+                    const uint32_t dst = smem_u32(s_scales + slot * Cf::SCALES);
+#pragma unroll
+                    for (int r = lane; r < BM; r += 32)
+                        if (t.row0 + r < t.row_end) cp_async4(dst + 4 * r, sa + r);
+                    if constexpr (WGRAD) {
+#pragma unroll
+                        for (int c = lane; c < BN; c += 32)
+                            if (t.col0 + c < a.N) cp_async4(dst + 4 * (BM + c), sb + c);
+                        sb += a.N;
+                    } else {
+                        if (lane < BN / kQ && t.col0 + lane * kQ < a.N) cp_async4(dst + 4 * (BM + lane), sb + (size_t)lane * a.Kb + kb);
+                    }
+                    cp_async_arrive(&ctl->sfull[slot]);
+                    if (++slot == kScaleSlots) { slot = 0; phase ^= 1; }
+                }
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");      // none in flight when the CTA exits
         }
     }
     tc_fence_before();

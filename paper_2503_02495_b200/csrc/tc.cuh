@@ -66,6 +66,15 @@ __device__ __forceinline__ bool mbar_wait_warp_quick(uint64_t* bar, uint32_t par
     return __all_sync(0xffffffffu, mbar_try_wait(bar, parity)) || mbar_wait_warp(bar, parity, abort_flag, status);
 }
 
+// ---- small asynchronous copies ------------------------------------------------------------------
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" :: "r"(dst), "l"(src) : "memory");
+}
+// one arrival of this thread on the barrier when all its copies so far have landed (counted in the barrier's number)
+__device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" :: "r"(smem_u32(bar)) : "memory");
+}
+
 // ---- TMA --------------------------------------------------------------------------------------
 __device__ __forceinline__ void prefetch_tmap(const CUtensorMap* m) {
     asm volatile("prefetch.tensormap [%0];" :: "l"(m) : "memory");
@@ -203,6 +212,11 @@ __device__ __forceinline__ uint32_t map_to_cta(const void* p, uint32_t rank) {
 }
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(cluster_addr) : "memory");
+}
+// The same without release: for hand-overs of TMEM, whose order is that of tcgen05.wait and tcgen05.fence and not of memory.  (A release at
+// cluster scope waits for every store the thread has under way; once per 128 of the contraction that is 2000 cycles each.)
+__device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t cluster_addr) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" :: "r"(cluster_addr) : "memory");
 }
 // tensor loads into this CTA's shared memory whose bytes are counted by a barrier of either CTA of the pair
 __device__ __forceinline__ void tma_load_2d_pair(void* dst, const CUtensorMap* m, int c0, int c1, uint32_t bar_cluster_addr) {
