@@ -8,9 +8,8 @@
 // kernel).  A persistent CTA (pair) per SM (two) walks the tiles, 128 x BN or, by a pair of CTAs (cta_group::2), 256 x 256:
 //   warp 0       TMA producer: a stage is one block of the contraction, 128 bytes of every row of A and of B (128-byte swizzle)
 //   warp 1       MMA issuer: four steps of 32 per stage
-//   warp 2       the scales of the blocks to come, by 4-byte asynchronous copies (their rows start anywhere) into a ring of their own
-//   warps 4..7   the stage's scales: float32 -> exponent byte -> TMEM, once for every lane quarter (a warp each).  A scale holds
-//                for the whole stage, so its byte fills the word and the four steps need no index.
+//   warps 4..7   the stages' scales in turn: float32 -> exponent byte -> shared memory, in the order in which the issuer's copies put
+//                them into TMEM.  A scale holds for the whole stage, so its byte fills the word and the four steps need no index.
 //   warps 8..15  write-out: a warp has 32 rows (its TMEM lane quarter) and half of the columns, all of them in registers before it
 //                gives the accumulator back (256 columns and the scales leave room for one accumulator: the next tile's products
 //                wait for these loads, not for the arithmetic and the stores)
@@ -26,8 +25,6 @@ using namespace tc;
 
 constexpr int BM = 128;
 
-constexpr int kScaleSlots = 8;
-
 template <int BN, bool PAIR> struct Cfg {
     static_assert(!PAIR || BN == 256, "a pair works 256 x 256");
     static constexpr int BN_CTA = PAIR ? BN / 2 : BN;                 // rows of B this CTA loads
@@ -36,14 +33,14 @@ template <int BN, bool PAIR> struct Cfg {
     static constexpr int STAGES = BN_CTA == 256 ? 4 : 6;
     static constexpr int NACC = BN == 256 ? 1 : 2;
     static constexpr int CW = BN / 2;
-    static constexpr int EPI_WARPS = 8, SCALE_WARPS = 4, THREADS = 128 + 128 + 32 * EPI_WARPS;
+    static constexpr int EPI_WARPS = 8, THREADS = 128 + 128 + 32 * EPI_WARPS;
     static constexpr int TMEM_COLS = 512, SF_COL = 256, SF_STRIDE = 16, SFB = 8;      // scales of stage s: A at SF_COL + 16 s, B 8 behind
-    static constexpr int SCALES = BM + BN;                            // floats of a block's scales: A's rows, then B's rows or blocks
-    static constexpr int SMEM = STAGES * STAGE + 1024 /* alignment */ + 1024 /* control */ + kScaleSlots * SCALES * 4;
+    static constexpr int SF_BYTES = 512 + 4 * BN;                     // a stage's scale words: A's 128 rows, then B's BN
+    static constexpr int SMEM = STAGES * (STAGE + SF_BYTES) + 1024 /* alignment */ + 1024 /* control */;
 };
 
 struct Ctl {
-    uint64_t full[8], empty[8], tfull[2], tempty[2], sfull[kScaleSlots], sempty[kScaleSlots];
+    uint64_t full[8], empty[8], tfull[2], tempty[2];
     uint32_t tmem_base;
     int abort_flag;
     Regions reg;
@@ -75,9 +72,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     constexpr int CTAS = PAIR ? 2 : 1;
     if (threadIdx.x == 0) {
         // (a pair's products are issued by rank 0, on whose barriers both CTAs' copies, scales and write-outs arrive)
-        for (int s = 0; s < Cf::STAGES; ++s) { mbar_init(&ctl->full[s], 1 + CTAS * Cf::SCALE_WARPS); mbar_init(&ctl->empty[s], 1); }
+        for (int s = 0; s < Cf::STAGES; ++s) { mbar_init(&ctl->full[s], 1 + CTAS); mbar_init(&ctl->empty[s], 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(&ctl->tfull[i], 1); mbar_init(&ctl->tempty[i], CTAS * Cf::EPI_WARPS); }
-        for (int i = 0; i < kScaleSlots; ++i) { mbar_init(&ctl->sfull[i], 32); mbar_init(&ctl->sempty[i], Cf::SCALE_WARPS); }
         ctl->abort_flag = 0;
         fence_barrier_init();
         prefetch_tmap(&tmA);
@@ -95,7 +91,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     if constexpr (PAIR) cluster_sync_all();           // the other CTA's barriers exist before anything arrives on them
     tc_fence_after();
     const uint32_t tmem_base = ctl->tmem_base;
-    float* s_scales = (float*)((uint8_t*)ctl + 1024);
+    uint8_t* s_sf = (uint8_t*)ctl + 1024;
     const int n_tiles = (a.N + BN - 1) / BN;
     const int total = ctl->reg.tstart[n] * n_tiles;
 
@@ -147,45 +143,56 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         }
     } else if (warp >= 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-        const uint32_t quarter = (uint32_t)((warp & 3) * 32) << 16;
         constexpr int NB = WGRAD ? BN / 32 : (BN + kQ - 1) / kQ;      // scales of B per lane: its columns', or the column blocks'
-        int stage = 0, e = 0, slot = 0;
-        uint32_t phase = 0, slot_phase = 0;
+        // The blocks of all this CTA's tiles are one sequence, and the four warps take turns: what a block costs is a chain (loads,
+        // a wait for the stage, the release), four of which run at a time.
+        int stage = 0, e = 0, turn = 0;
+        uint32_t phase = 0;
         bool stop = false, bad = false;
         for (int tile = worker; tile < total && !stop; tile += workers) {
             const Tile t = locate(tile, e);
             const int rows = t.row_end - t.row0, cols = a.N - t.col0;
-            for (int kb = 0; kb < t.kbs; ++kb) {
-                if (!mbar_wait_warp_quick(&ctl->sfull[slot], slot_phase, abort_flag, a.status)) { stop = true; break; }
-                const float* sc = s_scales + slot * Cf::SCALES;
-                uint32_t wa[4], wn[NB], wb[8];                        // (1 where there are no rows of this expert, or no columns)
+            const float* sa = a.sa + (size_t)t.kb0 * a.M + t.row0;
+            const float* sb = WGRAD ? a.sb + (size_t)t.kb0 * a.N + t.col0 : a.sb + ((size_t)e * a.Nb + t.col0 / kQ) * a.Kb;
+            float ra[4], rb[NB];                                      // (whatever is there where there are no rows of this expert, or no columns)
+            auto ask = [&](int kb) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) wa[q] = exponent_word(sc[q * 32 + lane], lane < rows - q * 32, bad);
+                for (int q = 0; q < 4; ++q)
+                    if (lane < rows - q * 32) ra[q] = __ldg(sa + (size_t)kb * a.M + q * 32 + lane);
 #pragma unroll
                 for (int q = 0; q < NB; ++q) {
-                    if constexpr (WGRAD) wn[q] = exponent_word(sc[BM + q * 32 + lane], lane < cols - q * 32, bad);
-                    else wn[q] = exponent_word(sc[BM + q], cols > q * kQ, bad);
+                    if constexpr (WGRAD) { if (lane < cols - q * 32) rb[q] = __ldg(sb + (size_t)kb * a.N + q * 32 + lane); }
+                    else if (cols > q * kQ) rb[q] = __ldg(sb + (size_t)q * a.Kb + kb);
                 }
+            };
+            const int first = ((warp & 3) - turn) & 3;                // this warp's first block of the tile
+            if (first < t.kbs) ask(first);
+            for (int kb = 0; kb < t.kbs; ++kb) {
+                if (((kb - first) & 3) == 0) {
+                    uint32_t wa[4], wn[NB], wb[8];
 #pragma unroll
-                for (int q = 0; q < 8; ++q) wb[q] = wn[WGRAD ? q % NB : (q / 4) % NB];
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&ctl->sempty[slot]);
-                if (++slot == kScaleSlots) { slot = 0; slot_phase ^= 1; }
-                if (!mbar_wait_warp_quick(&ctl->empty[stage], phase ^ 1, abort_flag, a.status)) { stop = true; break; }
-                tc_fence_after();
-                const uint32_t sf = tmem_base + Cf::SF_COL + stage * Cf::SF_STRIDE + quarter;
-                tmem_st4(sf, wa);
-                if constexpr (BN == 256) tmem_st8(sf + Cf::SFB, wb);
-                else tmem_st4(sf + Cf::SFB, wb);
-                tmem_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    if constexpr (PAIR) mbar_arrive_cluster_relaxed(map_to_cta(&ctl->full[stage], 0));
-                    else mbar_arrive(&ctl->full[stage]);
+                    for (int q = 0; q < 4; ++q) wa[q] = exponent_word(ra[q], lane < rows - q * 32, bad);
+#pragma unroll
+                    for (int q = 0; q < NB; ++q) wn[q] = exponent_word(rb[q], WGRAD ? lane < cols - q * 32 : cols > q * kQ, bad);
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) wb[q] = wn[WGRAD ? q % NB : (q / 4) % NB];
+                    if (kb + 4 < t.kbs) ask(kb + 4);
+                    if (!mbar_wait_warp_quick(&ctl->empty[stage], phase ^ 1, abort_flag, a.status)) { stop = true; break; }
+                    uint8_t* sf = s_sf + stage * Cf::SF_BYTES + lane * 16;
+                    *(uint4*)sf = make_uint4(wa[0], wa[1], wa[2], wa[3]);
+                    *(uint4*)(sf + 512) = make_uint4(wb[0], wb[1], wb[2], wb[3]);
+                    if constexpr (BN == 256) *(uint4*)(sf + 1024) = make_uint4(wb[4], wb[5], wb[6], wb[7]);
+                    // (every lane's words are in place for the copy, which reads this SM's shared memory, once its fence is behind it)
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if constexpr (PAIR) mbar_arrive_cluster_relaxed(map_to_cta(&ctl->full[stage], 0));
+                        else mbar_arrive(&ctl->full[stage]);
+                    }
                 }
                 if (++stage == Cf::STAGES) { stage = 0; phase ^= 1; }
             }
+            turn += t.kbs;
         }
         if (bad) set_status(a.status, UOE_ERR_FP8_SCALE);
     } else {
@@ -235,6 +242,13 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                     if (!mbar_wait_warp_quick(&ctl->full[stage], phase, abort_flag, a.status)) { stop = true; break; }
                     tc_fence_after();
                     const uint32_t st = smem_u32(smem + stage * Cf::STAGE), sf = tmem_base + Cf::SF_COL + stage * Cf::SF_STRIDE;
+                    const uint32_t ss = smem_u32(s_sf + stage * Cf::SF_BYTES);
+#pragma unroll
+                    for (int q = 0; q < 1 + BN / 128; ++q) {
+                        const uint32_t to = q == 0 ? sf : sf + Cf::SFB + 4 * (q - 1);
+                        if constexpr (PAIR) scales_to_tmem_pair(el, to, smem_desc_rows16(ss + 512 * q));
+                        else scales_to_tmem(el, to, smem_desc_rows16(ss + 512 * q));
+                    }
 #pragma unroll
                     for (int ks = 0; ks < 4; ++ks) {
                         const uint64_t ad = smem_desc(st + ks * 32, 16, 1024), bd = smem_desc(st + Cf::A_BYTES + ks * 32, 16, 1024);
@@ -250,33 +264,6 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 else mma_commit(el, &ctl->tfull[acc]);
                 if (++acc == Cf::NACC) { acc = 0; acc_phase ^= 1; }
             }
-        } else if (warp == 2) {
-            int slot = 0, e = 0;
-            uint32_t phase = 0;
-            bool stop = false;
-            for (int tile = worker; tile < total && !stop; tile += workers) {
-                const Tile t = locate(tile, e);
-                const float* sa = a.sa + (size_t)t.kb0 * a.M + t.row0;
-                const float* sb = WGRAD ? a.sb + (size_t)t.kb0 * a.N + t.col0 : a.sb + ((size_t)e * a.Nb + t.col0 / kQ) * a.Kb;
-                for (int kb = 0; kb < t.kbs; ++kb, sa += a.M) {
-                    if (!mbar_wait_warp_quick(&ctl->sempty[slot], phase ^ 1, abort_flag, a.status)) { stop = true; break; }
-                    const uint32_t dst = smem_u32(s_scales + slot * Cf::SCALES);
-#pragma unroll
-                    for (int r = lane; r < BM; r += 32)
-                        if (t.row0 + r < t.row_end) cp_async4(dst + 4 * r, sa + r);
-                    if constexpr (WGRAD) {
-#pragma unroll
-                        for (int c = lane; c < BN; c += 32)
-                            if (t.col0 + c < a.N) cp_async4(dst + 4 * (BM + c), sb + c);
-                        sb += a.N;
-                    } else {
-                        if (lane < BN / kQ && t.col0 + lane * kQ < a.N) cp_async4(dst + 4 * (BM + lane), sb + (size_t)lane * a.Kb + kb);
-                    }
-                    cp_async_arrive(&ctl->sfull[slot]);
-                    if (++slot == kScaleSlots) { slot = 0; phase ^= 1; }
-                }
-            }
-            asm volatile("cp.async.wait_all;" ::: "memory");      // none in flight when the CTA exits
         }
     }
     tc_fence_before();

@@ -159,6 +159,16 @@ __device__ __forceinline__ void mma_mxf8(uint32_t elected, uint32_t d_tmem, uint
         "@q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%6], [%7], p;\n\t}"
         :: "r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"((uint32_t)accumulate), "r"(elected), "r"(sfa_tmem), "r"(sfb_tmem) : "memory");
 }
+// Scales, shared memory -> TMEM: 32 rows of 16 bytes, one behind the other, to 32 lanes x 4 columns, once for every lane quarter.  Done in
+// order with the MMAs that the same lane issues, and counted by the same commits.  (Pairs: each CTA's own shared memory to its own TMEM.)
+__device__ __forceinline__ void scales_to_tmem(uint32_t elected, uint32_t taddr, uint64_t desc) {
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t"
+                 "@q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" :: "r"(taddr), "l"(desc), "r"(elected) : "memory");
+}
+__device__ __forceinline__ void scales_to_tmem_pair(uint32_t elected, uint32_t taddr, uint64_t desc) {
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t"
+                 "@q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t}" :: "r"(taddr), "l"(desc), "r"(elected) : "memory");
+}
 // The mbarrier gets one arrival when all MMAs issued so far by the elected lane have completed.
 __device__ __forceinline__ void mma_commit(uint32_t elected, uint64_t* bar) {
     asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
@@ -178,16 +188,6 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* v) {
           "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
         : "r"(taddr) : "memory");
 }
-// 32 lanes x 4 or 8 columns, register -> TMEM: thread t of the warp writes lane (base lane + t)
-__device__ __forceinline__ void tmem_st4(uint32_t taddr, const uint32_t* v) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};"
-                 :: "r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
-}
-__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* v) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
-                 :: "r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
-}
-__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // ---- CTA pairs (cluster of two, tcgen05 cta_group::2) ------------------------------------------
@@ -213,8 +213,9 @@ __device__ __forceinline__ uint32_t map_to_cta(const void* p, uint32_t rank) {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(cluster_addr) : "memory");
 }
-// The same without release: for hand-overs of TMEM, whose order is that of tcgen05.wait and tcgen05.fence and not of memory.  (A release at
-// cluster scope waits for every store the thread has under way; once per 128 of the contraction that is 2000 cycles each.)
+// The same without release: for hand-overs whose data is not the generic proxy's to order (TMEM, behind tcgen05.wait and tcgen05.fence;
+// shared memory that only the writing SM's asynchronous copies read, behind fence.proxy.async).  A release at cluster scope waits for
+// everything the thread has under way: 2000 cycles, where a hand-over is due every 500.
 __device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" :: "r"(cluster_addr) : "memory");
 }
@@ -287,6 +288,11 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t saddr, uint32_t lbo_bytes
     d |= (uint64_t)1 << 46;
     d |= (uint64_t)2 << 61;
     return d;
+}
+
+// The same without swizzle, for rows of 16 bytes (eight of them, 128 bytes, are a core matrix; the next one follows).
+__device__ __forceinline__ uint64_t smem_desc_rows16(uint32_t saddr) {
+    return (uint64_t)((saddr & 0x3FFFF) >> 4) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
 }
 
 // Instruction descriptor for kind::f16 with bf16 A and B, fp32 D, M x N tile:
