@@ -78,6 +78,7 @@ enum {
     UOE_FLAG_DYNAMIC_C = 8,    /* uoe_route: two-stage routing (Eq. 15-16): every chosen expert of a sample takes
                                   min(c, c_b) patches, c_b = the largest number of patches any expert receives when
                                   each patch goes to its k best experts; the remaining slots are unused (-1) */
+    UOE_FLAG_FP8_ANY_SCALE = 32, /* uoe_mlp_forward_fp8: the weights' scales may be any float32 numbers, not powers of two only */
     UOE_FLAG_GENERAL_PATH = 16 /* take the general routed path even for the two single-mode cases below (same results;
                                   for verification and for measuring what the special cases save) */
 };
@@ -95,7 +96,7 @@ enum {
  */
 
 typedef enum { UOE_OP_ROUTE = 0, UOE_OP_MLP_FWD = 1, UOE_OP_MLP_BWD = 2, UOE_OP_SMHA_FWD = 3, UOE_OP_SMHA_BWD = 4,
-               UOE_OP_BALANCE_BWD = 5 } uoe_op;
+               UOE_OP_BALANCE_BWD = 5, UOE_OP_MLP_FWD_FP8 = 6, UOE_OP_MLP_TOKENS = 7 } uoe_op;
 
 /* One Union-of-Experts block.  L must equal m * l_p; rows t >= L_valid of every sample are padding
  * (they take no part in routing means, are masked as attention keys (Eq. 41), and y = x there).
@@ -310,6 +311,19 @@ uoe_status uoe_fp8_gemm(const uoe_fp8_problem* prob, const void* A, const float*
 uoe_status uoe_fp8_wgrad(const uoe_fp8_problem* prob, const void* A, const float* a_scale, const void* B, const float* b_scale,
                          const int32_t* expert_offsets, float* dW, void* ws, size_t ws_bytes, void* cuda_stream);
 
+/*
+ * UoME forward on 8-bit weights: uoe_mlp_forward with the expert products of uoe_fp8_gemm.
+ *   W1 [n, d_e, dp], w1_scale and W2 [n, d, d_ep], w2_scale: UOE_FP8_BLOCKS_T of W1 [n, d, d_e] and W2 [n, d_e, d] (dp, d_ep: d, d_e
+ *   rounded up to UOE_FP8_BLOCK); scales other than powers of two only with UOE_FLAG_FP8_ANY_SCALE.
+ * The rows that enter a product are quantised as UOE_FP8_ROWS, a scale per row and 128 columns: the routed rows of x, and
+ * phi( ... + b1) in float32.  Products, biases and phi are float32; the experts' outputs are bfloat16 before the weighted sum.
+ * bfloat16 problems only (x, biases and y).  Everything else as for uoe_mlp_forward; workspace: UOE_OP_MLP_FWD_FP8.
+ */
+uoe_status uoe_mlp_forward_fp8(const uoe_problem* prob, const void* x, const void* W1, const float* w1_scale, const void* W2,
+                               const float* w2_scale, const void* b1, const void* b2, const int32_t* expert_idx,
+                               const int32_t* patch_idx, const float* gate, const int32_t* expert_offsets, void* y /* [B,L,d] */,
+                               void* ws, size_t ws_bytes, void* cuda_stream);
+
 /* Device arrays written by a router (shapes as for uoe_route).  A set is complete or absent as a whole. */
 typedef struct {
     int32_t* expert_idx;      /* [B,k] */
@@ -346,6 +360,22 @@ uoe_status uoe_block_forward(const uoe_problem* att, const uoe_problem* mlp, con
                              const void* Wr_mlp, const void* W1, const void* W2,
                              const uoe_routing* r_att, const uoe_routing* r_mlp, void* u, void* y,
                              void* saved_h, float* lse, void* ws, size_t ws_bytes, void* cuda_stream);
+
+/*
+ * A UoME layer for a few tokens, as in decoding: router and experts in two kernels, the same result as uoe_route followed by
+ * uoe_mlp_forward on a problem whose samples are one token each (L = m = c = 1, B <= 64 tokens; UOE_ERR_UNSUPPORTED otherwise):
+ *   y[b] = x[b] + sum over the k chosen experts i of token b  gate[b,i] * ( phi( x[b] W1[i] + b1[i] ) W2[i] + b2[i] )
+ * with gate = p_samp^2 (UOE_FLAG_GATE: P_samp times the gate of the token's one patch) or 1, and the residual by UOE_FLAG_RESIDUAL.  Every
+ * chosen expert's weights are read once.
+ *   Weights in prob->dtype as for uoe_mlp_forward (w1_scale = w2_scale = NULL), or, for bfloat16 problems, 8-bit as for
+ *   uoe_mlp_forward_fp8 with any float32 scales; x and the hidden rows stay bfloat16 there (the products are exact in float32).
+ *   r: host pointer to device arrays that receive the router's outputs, or NULL.    y: distinct from x.
+ *   A token that holds a NaN gets the first k experts.
+ * Workspace: UOE_OP_MLP_TOKENS.
+ */
+uoe_status uoe_mlp_tokens(const uoe_problem* prob, const void* x /* [B,1,d] */, const void* W_r, const void* W1, const float* w1_scale,
+                          const void* W2, const float* w2_scale, const void* b1, const void* b2, const uoe_routing* r,
+                          void* y /* [B,1,d] */, void* ws, size_t ws_bytes, void* cuda_stream);
 
 /*
  * uoe_route without a workspace argument and without any allocation.  (The paper has no counterpart;

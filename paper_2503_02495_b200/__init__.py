@@ -10,4 +10,5 @@ from .binding import (  # noqa: F401
     UOE_OP_SMHA_BWD,
     UOE_ROW_ALIGN, alloc_block_workspace, uoe_block_forward, uoe_block_workspace_bytes,
     Fp8Problem, alloc_fp8_workspace, uoe_fp8_gemm, uoe_fp8_quantize, uoe_fp8_wgrad, uoe_fp8_workspace_bytes, UOE_FP8_BLOCK,
+    uoe_mlp_forward_fp8, uoe_mlp_tokens, UOE_OP_MLP_FWD_FP8, UOE_OP_MLP_TOKENS,
 )

@@ -21,7 +21,8 @@ UOE_F32, UOE_BF16 = 0, 1
 ACTS = {"gelu_erf": 0, "gelu_tanh": 1, "silu": 2, "identity": 3}
 UOE_FLAG_RESIDUAL, UOE_FLAG_GATE, UOE_FLAG_CAUSAL, UOE_FLAG_DYNAMIC_C, UOE_FLAG_GENERAL_PATH = 1, 2, 4, 8, 16
 UOE_OP_ROUTE, UOE_OP_MLP_FWD, UOE_OP_MLP_BWD, UOE_OP_SMHA_FWD, UOE_OP_SMHA_BWD = 0, 1, 2, 3, 4
-UOE_OP_BALANCE_BWD = 5
+UOE_OP_BALANCE_BWD, UOE_OP_MLP_FWD_FP8, UOE_OP_MLP_TOKENS = 5, 6, 7
+UOE_FLAG_FP8_ANY_SCALE = 32
 UOE_FP8_BLOCK, UOE_FP8_ANY_SCALE = 128, 1
 FP8_LAYOUTS = {"rows": 0, "cols": 1, "blocks": 2, "blocks_t": 3}
 
@@ -87,11 +88,12 @@ class Problem:
     dynamic_c: bool = False
     d_rope: int = 0
     general_path: bool = False      # UOE_FLAG_GENERAL_PATH: no single-mode shortcuts (same results)
+    fp8_any_scale: bool = False     # UOE_FLAG_FP8_ANY_SCALE: 8-bit weights whose scales are not powers of two
 
     def c_struct(self) -> _Problem:
         flags = (UOE_FLAG_RESIDUAL if self.residual else 0) | (UOE_FLAG_GATE if self.gate else 0) | \
                 (UOE_FLAG_CAUSAL if self.causal else 0) | (UOE_FLAG_DYNAMIC_C if self.dynamic_c else 0) | \
-                (UOE_FLAG_GENERAL_PATH if self.general_path else 0)
+                (UOE_FLAG_GENERAL_PATH if self.general_path else 0) | (UOE_FLAG_FP8_ANY_SCALE if self.fp8_any_scale else 0)
         return _Problem(self.B, self.L, self.L_valid, self.d, self.n, self.k, self.m, self.c, self.d_e, self.H,
                         self.d_h, UOE_BF16 if self.dtype == "bf16" else UOE_F32, ACTS[self.act], flags, self.d_rope)
 
@@ -145,6 +147,10 @@ def _load():
     for f in (lib.uoe_fp8_gemm, lib.uoe_fp8_wgrad):
         f.restype = ctypes.c_int
         f.argtypes = [p8, vp, f32p, vp, f32p, i32p, vp, vp, sz, vp]
+    lib.uoe_mlp_forward_fp8.restype = ctypes.c_int
+    lib.uoe_mlp_forward_fp8.argtypes = [pp, vp, vp, f32p, vp, f32p, vp, vp, i32p, i32p, f32p, i32p, vp, vp, sz, vp]
+    lib.uoe_mlp_tokens.restype = ctypes.c_int
+    lib.uoe_mlp_tokens.argtypes = [pp, vp, vp, vp, f32p, vp, f32p, vp, vp, ctypes.POINTER(_Routing), vp, vp, sz, vp]
     lib.uoe_block_workspace_bytes.restype = sz
     lib.uoe_block_workspace_bytes.argtypes = [pp, pp]
     lib.uoe_block_forward.restype = ctypes.c_int
@@ -483,6 +489,50 @@ def uoe_fp8_wgrad(prob: Fp8Problem, A, a_scale, B, b_scale, expert_offsets=None,
     if check:
         _check(uoe_read_device_status(ws), "uoe_fp8_wgrad (device)")
     return dW
+
+
+def _fp8_weights(prob: Problem, W1, s1, W2, s2):
+    blk = lambda v: -(-v // UOE_FP8_BLOCK)
+    db, eb = blk(prob.d), blk(prob.d_e)
+    _fp8_operand(W1, s1, (prob.n, prob.d_e, db * UOE_FP8_BLOCK), (prob.n, eb, db))
+    _fp8_operand(W2, s2, (prob.n, prob.d, eb * UOE_FP8_BLOCK), (prob.n, db, eb))
+
+
+def uoe_mlp_forward_fp8(prob: Problem, x, W1, s1, W2, s2, r: Routing, b1=None, b2=None, y=None, ws=None, check: bool = True):
+    """uoe_mlp_forward on 8-bit weights: (W1, s1), (W2, s2) = uoe_fp8_quantize(W1 [n,d,d_e], "blocks_t"), (W2 [n,d_e,d], "blocks_t")."""
+    for t in (x, b1, b2):
+        _contig(t, prob.torch_dtype)
+    _fp8_weights(prob, W1, s1, W2, s2)
+    y = y if y is not None else torch.empty_like(x)
+    ws = ws if ws is not None else alloc_workspace(prob, UOE_OP_MLP_FWD_FP8, x.device)
+    st = _lib.uoe_mlp_forward_fp8(ctypes.byref(prob.c_struct()), _ptr(x), _ptr(W1), _ptr(s1), _ptr(W2), _ptr(s2), _ptr(b1), _ptr(b2),
+                                  _ptr(r.expert_idx), _ptr(r.patch_idx), _ptr(r.gate), _ptr(r.expert_offsets), _ptr(y), _ptr(ws),
+                                  ws.numel(), _stream())
+    _check(st, "uoe_mlp_forward_fp8")
+    if check:
+        _check(uoe_read_device_status(ws), "uoe_mlp_forward_fp8 (device)")
+    return y
+
+
+def uoe_mlp_tokens(prob: Problem, x, W_r, W1, W2, s1=None, s2=None, b1=None, b2=None, r: Routing | None = None, y=None, ws=None,
+                   check: bool = True):
+    """Router, experts and combine of a UoME layer for up to 64 tokens x [B,1,d] (or [B,d]) in two kernels; prob has L = m = c = 1.
+    Weights in the problem's type, or 8-bit with their scales s1, s2 as for uoe_mlp_forward_fp8.  Fills r when given."""
+    for t in (x, W_r, b1, b2):
+        _contig(t, prob.torch_dtype)
+    if s1 is None:
+        _contig(W1, prob.torch_dtype)
+        _contig(W2, prob.torch_dtype)
+    else:
+        _fp8_weights(prob, W1, s1, W2, s2)
+    y = y if y is not None else torch.empty_like(x)
+    ws = ws if ws is not None else alloc_workspace(prob, UOE_OP_MLP_TOKENS, x.device)
+    st = _lib.uoe_mlp_tokens(ctypes.byref(prob.c_struct()), _ptr(x), _ptr(W_r), _ptr(W1), _ptr(s1), _ptr(W2), _ptr(s2), _ptr(b1), _ptr(b2),
+                             _routing_struct(r), _ptr(y), _ptr(ws), ws.numel(), _stream())
+    _check(st, "uoe_mlp_tokens")
+    if check:
+        _check(uoe_read_device_status(ws), "uoe_mlp_tokens (device)")
+    return y
 
 
 def uoe_block_workspace_bytes(att: Problem | None, mlp: Problem | None) -> int:

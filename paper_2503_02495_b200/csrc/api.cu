@@ -70,6 +70,8 @@ extern "C" size_t uoe_workspace_bytes(const uoe_problem* prob, int op) {
         case UOE_OP_SMHA_FWD: return D.H > 0 ? smha_fwd_workspace_bytes(D) : 0;
         case UOE_OP_SMHA_BWD: return D.H > 0 ? smha_bwd_workspace_bytes(D) : 0;
         case UOE_OP_BALANCE_BWD: return balance_bwd_workspace_bytes(D);
+        case UOE_OP_MLP_FWD_FP8: return D.d_e > 0 && D.bf16 ? mlp_fp8_workspace_bytes(D) : 0;
+        case UOE_OP_MLP_TOKENS: return D.d_e > 0 ? mlp_tokens_workspace_bytes(D) : 0;
         default: return 0;
     }
 }

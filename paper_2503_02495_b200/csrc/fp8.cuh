@@ -40,6 +40,18 @@ __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d, f
     return inv == 0.f ? 0u : lo | (hi << 16);
 }
 
+// phi with errors of float32 size (the result is compared with a rounding border of its own)
+__device__ __forceinline__ float act_precise(float h, int act) {
+    switch (act) {
+        case UOE_ACT_SILU: return __fdividef(h, 1.0f + __expf(-h));
+        case UOE_ACT_GELU_TANH: {
+            const float u = 0.79788456080286536f * (h + 0.044715f * h * h * h);
+            return __fdividef(h, 1.0f + __expf(-2.0f * u));             // h/2 (1 + tanh u)
+        }
+        default: return act_apply(h, act);
+    }
+}
+
 // x [rows of C elements] -> q [rows, Cp], scale [Cp / 128, rows]: every row by itself.  With map.on() row r of the output is the
 // token that routed row r holds (zeros on padding rows and unused slots), and only rows below offsets[n] are written.
 uoe_status launch_quantize_rows(const void* x, bool bf16, int G, long long rows, int C, void* q, float* scale, const SrcMap& map,

@@ -22,18 +22,6 @@ struct Fp8Args {
     int* status;
 };
 
-// phi with errors of float32 size (the result is compared with a rounding border of its own)
-__device__ __forceinline__ float act_precise(float h, int act) {
-    switch (act) {
-        case UOE_ACT_SILU: return __fdividef(h, 1.0f + __expf(-h));
-        case UOE_ACT_GELU_TANH: {
-            const float u = 0.79788456080286536f * (h + 0.044715f * h * h * h);
-            return __fdividef(h, 1.0f + __expf(-2.0f * u));             // h/2 (1 + tanh u)
-        }
-        default: return act_apply(h, act);
-    }
-}
-
 // First row (wgrad: position in the contraction) of every expert, and its first row tile.
 struct Regions {
     int offs[kMaxExperts + 1];

@@ -1,0 +1,669 @@
+// uoe_mlp_tokens: router, experts and combine of a UoME layer for a few tokens (every row of x is a sample of one token: Eq. 21-22
+// choose its experts, Eq. 38-40 follow) in two kernels.
+//
+// Bound by the weights of the chosen experts, each read once: one token per row tile of 128 would leave the tensor cores waiting for
+// memory all the same, so the products run on mma.sync fragments that come straight from global memory, without a pass through
+// shared memory.  Up to 32 tokens (one or two 16-row fragments) share a weight fragment.
+//   first_layer_kernel   routes, then a = phi(x W1 + b1) for every (chosen expert, 64 hidden columns): clusters of S CTAs walk these tiles,
+//                        the S * 8 warps of a cluster split the contraction, their sums meet in distributed shared memory
+//   second_layer_kernel  routes again (a few KB from L2, instead of a wait for the first kernel), asks for its weights (L2 prefetch)
+//                        while the first kernel runs, then y = x + sum over experts gate (a W2 + b2): a cluster per 64 columns of y, its
+//                        warps split the contraction over all chosen experts' hidden columns in one line
+// The router's sums are cut into 8 pieces of d whatever the cluster size, so that both kernels choose the same experts.
+// Sums are added in an order that depends on sizes alone.
+//
+// Fragments (m16n8k16: a lane g * 4 + t holds k = 2t, 2t+1, 2t+8, 2t+9 of row g of A and column g of B).  The order of k inside a step is
+// free as long as both operands have the same one: slots 2t, 2t+1, 2t+8, 2t+9 hold k = 4t .. 4t+3.
+//   bfloat16 weights [K, N]   a lane loads 16 bytes, columns 8g .. 8g+7, of rows 4t .. 4t+3 (a warp: 16 whole 128-byte lines) and pairs the
+//                             rows' halves: fragment j holds columns 8g + j
+//   8-bit weights [N, Kp]     a lane loads 16 bytes of k, 16t .. 16t+15, of row 8j + g: four steps of fragment j.  e4m3 -> half -> float
+//                             -> bfloat16 is exact; the block's scale multiplies the float32 sums of 64 of the contraction
+//   float32 weights [K, N]    float32 multiply-adds, eight tokens at a time
+#include "fp8.cuh"
+#include "tc.cuh"
+
+namespace uoe {
+namespace {
+
+using namespace tc;
+
+constexpr int kTok = 32;            // tokens of a group (a z slice of the grid)
+constexpr int kMaxTokens = 64;
+constexpr int kCols = 64;           // columns of a tile
+constexpr int kWarps = 8, kThreads = 32 * kWarps;
+constexpr int kPieces = 8;          // of d, in the router's sums
+enum { kBf16 = 0, kFp8 = 1, kF32 = 2 };
+
+struct TokArgs {
+    const void *x, *Wr, *W1, *W2, *b1, *b2;
+    const float *s1, *s2;
+    void *a, *y;                    // a [groups, n, kTok, d_e]: hidden rows by place in the group's list of chosen experts
+    RoutingPtrs r;                  // all null, or all to be written
+    int T, d, d_e, n, k, act, use_gate, residual;
+};
+
+template <int WT> struct Elem { using T = __nv_bfloat16; };
+template <> struct Elem<kF32> { using T = float; };
+
+struct Routed {                     // shared memory: what the router says about this group's tokens
+    uint32_t mask[kTok];            // chosen experts
+    float p[kTok][32];              // sample gate (Eq. 21)
+    uint32_t any;                   // experts that some token chose
+};
+
+__device__ __forceinline__ float ld_cluster(const float* p, uint32_t rank) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(map_to_cta(p, rank)) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ void mma16(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// e4m3 pair (low half of v) -> bfloat16 pair, exact
+__device__ __forceinline__ uint32_t bf16x2_of_e4m3x2(uint32_t v) {
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)v, __NV_E4M3);
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+    return pack_bf16x2(f.x, f.y);
+}
+
+// Sums over this CTA's pieces of d: part[piece / S][token * n + expert], pieces rank, rank + S, ...
+template <int WT, int MT>
+__device__ void router_pieces(const TokArgs& a, int t0, int Tn, int rank, int S, float* red /* [8][Tn * n] */, float* part) {
+    using T = typename Elem<WT>::T;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int d = a.d, n = a.n, len = ((d + kPieces - 1) / kPieces + 15) / 16 * 16;
+    const T* x = (const T*)a.x + (size_t)t0 * d;
+    const T* Wr = (const T*)a.Wr;
+    for (int p = rank; p < kPieces; p += S) {
+        const int k0 = p * len, k1 = min(d, k0 + len);
+        if constexpr (WT == kF32) {
+            // a warp per (token, expert)
+            for (int q = warp; q < Tn * n; q += kWarps) {
+                const int tok = q / n, i = q - tok * n;
+                float s = 0.f;
+                for (int kk = k0 + lane; kk < k1; kk += 32) s = fmaf(x[(size_t)tok * d + kk], Wr[(size_t)kk * n + i], s);
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+                if (lane == 0) part[(p / S) * Tn * n + q] = s;
+            }
+        } else {
+            const int J = (n + 7) / 8;                 // fragment j: experts g * J + j
+            float c[MT][4][4];
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) c[m][j][u] = 0.f;
+#pragma unroll 4
+            for (int kk = k0 + warp * 16; kk < k1; kk += kWarps * 16) {
+                const int kt = kk + 4 * t;
+                uint32_t af[MT][4];
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint2 v = make_uint2(0, 0);
+                        const int row = m * 16 + h * 8 + g;
+                        if (row < Tn && kt < k1) v = *(const uint2*)(x + (size_t)row * d + kt);
+                        af[m][h] = v.x; af[m][2 + h] = v.y;
+                    }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (j >= J) break;
+                    const int i = g * J + j;
+                    uint32_t w[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) w[r] = i < n && kt < k1 ? *(const uint16_t*)(Wr + (size_t)(kt + r) * n + i) : 0u;
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) mma16(c[m][j], af[m], w[0] | (w[1] << 16), w[2] | (w[3] << 16));
+                }
+            }
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const int row = m * 16 + (u >> 1) * 8 + g, i = (2 * t + (u & 1)) * J + j;
+                        if (j < J && row < Tn && i < n) red[warp * Tn * n + row * n + i] = c[m][j][u];
+                    }
+            __syncthreads();
+            for (int q = threadIdx.x; q < Tn * n; q += kThreads) {
+                float s = 0.f;
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) s += red[w * Tn * n + q];
+                part[(p / S) * Tn * n + q] = s;
+            }
+            __syncthreads();
+        }
+    }
+}
+
+// Eq. 21-22 for the group's tokens, the same in every CTA.
+template <int WT, int MT>
+__device__ void route_tokens(const TokArgs& a, int t0, int Tn, int rank, int S, float* red, float* part, Routed& R) {
+    router_pieces<WT, MT>(a, t0, Tn, rank, S, red, part);
+    if (threadIdx.x == 0) R.any = 0;
+    cluster_sync_all();                                // every CTA's pieces are there
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = a.n;
+    uint32_t any = 0;
+    for (int tok = warp; tok < Tn; tok += kWarps) {
+        float v = -INFINITY;
+        if (lane < n) {
+            v = 0.f;
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) v += ld_cluster(part + (p / S) * Tn * n + tok * n + lane, p % S);
+        }
+        float mx = v;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        const float e = lane < n ? expf(v - mx) : 0.f;
+        float sum = e;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        const float ps = (lane < n ? e : 1.f) / sum;
+        // (a token that holds a NaN has no order: it gets the first k experts, as many as every other)
+        const float key = ps == ps ? ps : -1.f;
+        int rank_i = 0;
+        for (int i = 0; i < n; ++i) {
+            const float w = __shfl_sync(0xffffffffu, key, i);
+            rank_i += (w > key) || (w == key && i < lane);
+        }
+        const uint32_t m = __ballot_sync(0xffffffffu, lane < n && rank_i < a.k);
+        R.p[tok][lane] = lane < n ? ps : 0.f;
+        if (lane == 0) R.mask[tok] = m;
+        any |= m;
+    }
+    if (lane == 0 && any) atomicOr(&R.any, any);
+    __syncthreads();
+}
+
+__device__ __forceinline__ int nth_bit(uint32_t m, int i) {
+    for (; i > 0; --i) m &= m - 1;
+    return __ffs(m) - 1;
+}
+
+// One warp: c[m][j] += A[rows, k0 .. k1) W[k0 .. k1, columns], fragments of columns as in the file's head.  A [Tn rows, ld], W the
+// expert's matrix, its first column c0 of N.  scale: 8-bit weights only, [K / 128] of this column block.
+template <int WT, int MT>
+__device__ __forceinline__ void accumulate(float (*c)[8][4], const __nv_bfloat16* A, int ld, int Tn, const void* W, const float* scale, int c0, int N, int K,
+                                           int k0, int k1) {
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    if constexpr (WT == kBf16) {
+        constexpr int U = 2;                           // steps of 16 in flight: 4 KB of weights per warp
+        const __nv_bfloat16* w0 = (const __nv_bfloat16*)W + c0 + 8 * g;
+        const bool col_ok = c0 + 8 * g < N;
+        for (int kk = k0; kk < k1; kk += 16 * U) {
+            uint4 w[U][4];
+            uint2 x[U][MT][2];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int kt = kk + 16 * u + 4 * t;
+                const bool ok = kt < k1;               // (K and the cuts are multiples of 4)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) w[u][r] = ok && col_ok ? ld_stream16(w0 + (size_t)(kt + r) * N) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int row = m * 16 + h * 8 + g;
+                        x[u][m][h] = ok && row < Tn ? *(const uint2*)(A + (size_t)row * ld + kt) : make_uint2(0, 0);
+                    }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint32_t* r0 = (const uint32_t*)&w[u][0];
+                const uint32_t* r1 = (const uint32_t*)&w[u][1];
+                const uint32_t* r2 = (const uint32_t*)&w[u][2];
+                const uint32_t* r3 = (const uint32_t*)&w[u][3];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t sel = j & 1 ? 0x7632 : 0x5410;
+                    const uint32_t b0 = __byte_perm(r0[j >> 1], r1[j >> 1], sel), b1 = __byte_perm(r2[j >> 1], r3[j >> 1], sel);
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) {
+                        const uint32_t af[4] = {x[u][m][0].x, x[u][m][1].x, x[u][m][0].y, x[u][m][1].y};
+                        mma16(c[m][j], af, b0, b1);
+                    }
+                }
+            }
+        }
+    } else {
+        const size_t Kp = (size_t)(K + kQ - 1) / kQ * kQ;
+        const uint8_t* w0 = (const uint8_t*)W + (size_t)(c0 + g) * Kp + 16 * t;
+        for (int kk = k0; kk < k1; kk += 64) {         // (cuts are multiples of 64)
+            uint4 w[8];
+            uint4 x[MT][2][2];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = c0 + 8 * j + g < N ? ld_stream16(w0 + (size_t)8 * j * Kp + kk) : make_uint4(0, 0, 0, 0);
+            const float s = __ldg(scale + kk / kQ);
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        const int row = m * 16 + h * 8 + g, kt = kk + 16 * t + 8 * q;
+                        x[m][h][q] = row < Tn && kt < K ? *(const uint4*)(A + (size_t)row * ld + kt) : make_uint4(0, 0, 0, 0);
+                    }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t* wj = (const uint32_t*)&w[j];
+                float p[MT][4];
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) p[m][u] = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {          // k = 16 t + 4 i .. + 3
+                    const uint32_t b0 = bf16x2_of_e4m3x2(wj[i] & 0xffff), b1 = bf16x2_of_e4m3x2(wj[i] >> 16);
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) {
+                        const uint32_t* lo = (const uint32_t*)&x[m][0][i >> 1];
+                        const uint32_t* hi = (const uint32_t*)&x[m][1][i >> 1];
+                        const uint32_t af[4] = {lo[2 * (i & 1)], hi[2 * (i & 1)], lo[2 * (i & 1) + 1], hi[2 * (i & 1) + 1]};
+                        mma16(p[m], af, b0, b1);
+                    }
+                }
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) c[m][j][u] = fmaf(s, p[m][u], c[m][j][u]);
+            }
+        }
+    }
+}
+
+// Column of the tile that element u of fragment j is in.
+template <int WT>
+__device__ __forceinline__ int col_of(int j, int u, int t) {
+    return WT == kBf16 ? 8 * (2 * t + (u & 1)) + j : 8 * j + 2 * t + (u & 1);
+}
+
+// float32: a half warp takes every other row of W, a lane four columns; eight tokens per pass over the weights.  Adds weight(tok) times the
+// product to red[tok][col] of this warp (first: sets it).
+template <typename Weight>
+__device__ void accumulate_f32(float* red, const float* A, int ld, int Tn, const float* W, int c0, int N, int k0, int k1, bool first, Weight weight) {
+    const int lane = threadIdx.x & 31, h = lane >> 4, col = 4 * (lane & 15);
+    const bool col_ok = c0 + col < N;
+    for (int tb = 0; tb < Tn; tb += 8) {
+        float4 s[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] = make_float4(0, 0, 0, 0);
+#pragma unroll 4
+        for (int kk = k0 + h; kk < k1; kk += 2) {
+            const uint4 v = col_ok ? ld_stream16(W + (size_t)kk * N + c0 + col) : make_uint4(0, 0, 0, 0);
+            const float4 w = make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float q = tb + i < Tn ? A[(size_t)(tb + i) * ld + kk] : 0.f;
+                s[i].x = fmaf(q, w.x, s[i].x); s[i].y = fmaf(q, w.y, s[i].y); s[i].z = fmaf(q, w.z, s[i].z); s[i].w = fmaf(q, w.w, s[i].w);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (tb + i >= Tn) break;
+            float f[4] = {s[i].x, s[i].y, s[i].z, s[i].w};
+#pragma unroll
+            for (int u = 0; u < 4; ++u) f[u] += __shfl_xor_sync(0xffffffffu, f[u], 16);
+            float wt;
+            const bool on = weight(tb + i, wt);
+            if (h == 0) {
+                float* o = red + (tb + i) * kCols + col;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) o[u] = (first ? 0.f : o[u]) + (on ? wt * f[u] : 0.f);
+            }
+        }
+    }
+}
+
+// Cut of `units` pieces of work among `workers`: worker w's [lo, hi).
+__device__ __forceinline__ void cut(int units, int workers, int w, int& lo, int& hi) {
+    lo = (int)((long long)units * w / workers);
+    hi = (int)((long long)units * (w + 1) / workers);
+}
+template <int WT> __device__ __forceinline__ constexpr int unit_len() { return WT == kFp8 ? 64 : 16; }
+
+struct Smem {                       // dynamic shared memory, sizes in floats
+    float *red, *cta, *part;
+    Routed* R;
+    __device__ Smem(uint8_t* base, int Tn, int n, int S) {
+        red = (float*)base;
+        cta = red + kWarps * Tn * (n > kCols ? n : kCols);
+        part = cta + 2 * Tn * kCols;
+        R = (Routed*)(part + (kPieces / S) * Tn * n);
+    }
+    static size_t bytes(int Tn, int n, int S) {
+        return sizeof(float) * ((size_t)kWarps * Tn * (n > kCols ? n : kCols) + 2 * Tn * kCols + (size_t)(kPieces / S) * Tn * n) + sizeof(Routed);
+    }
+};
+
+// This CTA's sums of a tile (its warps' parts added in order) into its buffer `cta`, visible to the whole cluster.
+__device__ __forceinline__ void meet(const float* red, float* cta, int Tn) {
+    __syncthreads();
+    for (int q = threadIdx.x; q < Tn * kCols; q += kThreads) {
+        float s = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) s += red[w * Tn * kCols + q];
+        cta[q] = s;
+    }
+    cluster_sync_all();
+}
+
+template <int WT, int MT>
+__global__ void __launch_bounds__(kThreads, MT == 1 ? 2 : 1)
+first_layer_kernel(const TokArgs a, int S) {
+    using T = typename Elem<WT>::T;
+    extern __shared__ __align__(16) uint8_t smem_raw[];
+    const int rank = (int)cluster_ctarank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int t0 = blockIdx.z * kTok, Tn = min(kTok, a.T - t0);
+    Smem sm(smem_raw, Tn, a.n, S);
+    pdl_wait();
+    // Only now: when the second kernel starts, everything in front of this one is complete, and it may read the inputs at once.
+    pdl_trigger();
+    route_tokens<WT, MT>(a, t0, Tn, rank, S, sm.red, sm.part, *sm.R);
+    const Routed& R = *sm.R;
+    const int cluster = blockIdx.x / S, clusters = gridDim.x / S;
+    if (cluster == 0 && rank == 0 && a.r.expert_idx) {
+        for (int tok = warp; tok < Tn; tok += kWarps) {
+            const uint32_t m = R.mask[tok];
+            const size_t b = t0 + tok;
+            if (lane < a.n) a.r.p_samp[b * a.n + lane] = a.r.p_patch[b * a.n + lane] = R.p[tok][lane];
+            if ((m >> lane) & 1) {
+                const int s = __popc(m & ((1u << lane) - 1u));
+                a.r.expert_idx[b * a.k + s] = lane;
+                a.r.patch_idx[b * a.k + s] = 0;
+                a.r.gate[b * a.k + s] = a.use_gate ? R.p[tok][lane] * R.p[tok][lane] : 1.f;
+            }
+        }
+    }
+    const int tiles_n = (a.d_e + kCols - 1) / kCols, tiles = __popc(R.any) * tiles_n;
+    const T* x = (const T*)a.x + (size_t)t0 * a.d;
+    T* out = (T*)a.a + (size_t)blockIdx.z * a.n * kTok * a.d_e;
+    int lo, hi, buf = 0;
+    cut((a.d + unit_len<WT>() - 1) / unit_len<WT>(), S * kWarps, rank * kWarps + warp, lo, hi);
+    const int k0 = lo * unit_len<WT>(), k1 = min(a.d, hi * unit_len<WT>());
+    for (int tile = cluster; tile < tiles; tile += clusters) {
+        const int slot = tile / tiles_n, c0 = (tile - slot * tiles_n) * kCols, e = nth_bit(R.any, slot);
+        float* red = sm.red + warp * Tn * kCols;
+        if constexpr (WT == kF32) {
+            accumulate_f32(red, (const float*)x, a.d, Tn, (const float*)a.W1 + (size_t)e * a.d * a.d_e, c0, a.d_e, k0, k1, true,
+                           [](int, float& w) { w = 1.f; return true; });
+        } else {
+            float c[MT][8][4];
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) c[m][j][u] = 0.f;
+            const size_t Kp = (size_t)(a.d + kQ - 1) / kQ * kQ;
+            const void* W = WT == kFp8 ? (const void*)((const uint8_t*)a.W1 + (size_t)e * a.d_e * Kp) : (const void*)((const T*)a.W1 + (size_t)e * a.d * a.d_e);
+            const float* sc = WT == kFp8 ? a.s1 + ((size_t)e * ((a.d_e + kQ - 1) / kQ) + c0 / kQ) * (Kp / kQ) : nullptr;
+            accumulate<WT, MT>(c, (const __nv_bfloat16*)x, a.d, Tn, W, sc, c0, a.d_e, a.d, k0, k1);
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const int row = m * 16 + (u >> 1) * 8 + g;
+                        if (row < Tn) red[row * kCols + col_of<WT>(j, u, t)] = c[m][j][u];
+                    }
+        }
+        float* cta = sm.cta + buf * Tn * kCols;
+        meet(sm.red, cta, Tn);
+        for (int q = rank * kThreads + threadIdx.x; q < Tn * kCols; q += S * kThreads) {
+            const int tok = q / kCols, col = c0 + q % kCols;
+            if (col >= a.d_e || !((R.mask[tok] >> e) & 1)) continue;
+            float h = 0.f;
+            for (int s = 0; s < S; ++s) h += ld_cluster(cta + q, s);
+            if (a.b1) h += to_f32(((const T*)a.b1)[(size_t)e * a.d_e + col]);
+            // (bfloat16: half a step, 2^-9 of the value, like the hidden rows of uoe_mlp_forward)
+            out[((size_t)slot * kTok + tok) * a.d_e + col] = (T)act_precise(h, a.act);
+        }
+        buf ^= 1;
+    }
+    cluster_sync_all();            // nobody's shared memory goes while another CTA may read it
+}
+
+template <int WT, int MT>
+__global__ void __launch_bounds__(kThreads, MT == 1 ? 2 : 1)
+second_layer_kernel(const TokArgs a, int S) {
+    using T = typename Elem<WT>::T;
+    extern __shared__ __align__(16) uint8_t smem_raw[];
+    const int rank = (int)cluster_ctarank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int t0 = blockIdx.z * kTok, Tn = min(kTok, a.T - t0);
+    Smem sm(smem_raw, Tn, a.n, S);
+    pdl_trigger();
+    route_tokens<WT, MT>(a, t0, Tn, rank, S, sm.red, sm.part, *sm.R);
+    const Routed& R = *sm.R;
+    const int c0 = blockIdx.x / S * kCols;
+    constexpr int UL = unit_len<WT>();
+    const int per = (a.d_e + UL - 1) / UL;             // units of one expert
+    int lo, hi;
+    cut(__popc(R.any) * per, S * kWarps, rank * kWarps + warp, lo, hi);
+    const size_t Kp = (size_t)(a.d_e + kQ - 1) / kQ * kQ;
+    auto weights = [&](int e) -> const void* {
+        if constexpr (WT == kFp8) return (const uint8_t*)a.W2 + (size_t)e * a.d * Kp;
+        else return (const T*)a.W2 + (size_t)e * a.d_e * a.d;
+    };
+    for (int u = lo; u < hi;) {                        // this warp's weights on their way to L2 while the first kernel runs
+        const int slot = u / per, k0 = (u - slot * per) * UL, n_u = min(hi - u, per - (u - slot * per)), k1 = min(a.d_e, k0 + n_u * UL);
+        const int e = nth_bit(R.any, slot);
+        if constexpr (WT == kFp8) {
+            for (int q = lane; q < kCols * ((k1 - k0 + kQ - 1) / kQ); q += 32) {
+                const int row = c0 + q % kCols;
+                if (row < a.d) asm volatile("prefetch.global.L2 [%0];" :: "l"((const uint8_t*)weights(e) + (size_t)row * Kp + k0 + q / kCols * kQ));
+            }
+        } else {
+            constexpr int LINES = kCols * sizeof(T) / 128;
+            for (int q = lane; q < (k1 - k0) * LINES; q += 32) {
+                const int col = c0 + q % LINES * (128 / (int)sizeof(T));
+                if (col < a.d) asm volatile("prefetch.global.L2 [%0];" :: "l"((const T*)weights(e) + (size_t)(k0 + q / LINES) * a.d + col));
+            }
+        }
+        u += n_u;
+    }
+    pdl_wait();
+    if (blockIdx.x == 0 && blockIdx.z == 0 && warp == 0 && a.r.expert_offsets) {      // Eq. 23, from every group's choices
+        int cnt = 0;
+        for (int q0 = 0; q0 < a.T * a.k; q0 += 32) {
+            const int v = q0 + lane < a.T * a.k ? __ldcg(a.r.expert_idx + q0 + lane) : -1;
+            for (int j = 0; j < 32; ++j) cnt += __shfl_sync(0xffffffffu, v, j) == lane;
+        }
+        const int rows = lane < a.n ? (cnt + UOE_ROW_ALIGN - 1) / UOE_ROW_ALIGN * UOE_ROW_ALIGN : 0;
+        int incl = rows;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += v;
+        }
+        if (lane < a.n) a.r.expert_offsets[lane + 1] = incl;
+        if (lane == 0) a.r.expert_offsets[0] = 0;
+    }
+    const T* hid = (const T*)a.a + (size_t)blockIdx.z * a.n * kTok * a.d_e;
+    float* red = sm.red + warp * Tn * kCols;
+    auto weight = [&](int tok, int e, float& w) {      // combine weight of (token, expert); false: not chosen
+        const float p = R.p[tok][e];
+        w = a.use_gate ? p * p : 1.f;
+        return ((R.mask[tok] >> e) & 1) != 0;
+    };
+    if constexpr (WT == kF32) {
+        for (int q = lane; q < Tn * kCols; q += 32) red[q] = 0.f;
+        __syncwarp();
+    }
+    float tot[MT][8][4];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) tot[m][j][u] = 0.f;
+    for (int u = lo; u < hi;) {
+        const int slot = u / per, k0 = (u - slot * per) * UL, n_u = min(hi - u, per - (u - slot * per)), k1 = min(a.d_e, k0 + n_u * UL);
+        const int e = nth_bit(R.any, slot);
+        const T* A = hid + (size_t)slot * kTok * a.d_e;
+        if constexpr (WT == kF32) {
+            accumulate_f32(red, (const float*)A, a.d_e, Tn, (const float*)weights(e), c0, a.d, k0, k1, false,
+                           [&](int tok, float& w) { return weight(tok, e, w); });
+        } else {
+            float c[MT][8][4];
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) c[m][j][v] = 0.f;
+            const float* sc = WT == kFp8 ? a.s2 + ((size_t)e * ((a.d + kQ - 1) / kQ) + c0 / kQ) * (Kp / kQ) : nullptr;
+            accumulate<WT, MT>(c, (const __nv_bfloat16*)A, a.d_e, Tn, weights(e), sc, c0, a.d, a.d_e, k0, k1);
+            // the tokens that chose this expert take its sums (the hidden rows of the others were never written)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int row = m * 16 + h * 8 + g;
+                    float w = 0.f;
+                    if (row < Tn && weight(row, e, w)) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            tot[m][j][2 * h] = fmaf(w, c[m][j][2 * h], tot[m][j][2 * h]);
+                            tot[m][j][2 * h + 1] = fmaf(w, c[m][j][2 * h + 1], tot[m][j][2 * h + 1]);
+                        }
+                    }
+                }
+        }
+        u += n_u;
+    }
+    if constexpr (WT != kF32) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int row = m * 16 + (u >> 1) * 8 + g;
+                    if (row < Tn) red[row * kCols + col_of<WT>(j, u, t)] = tot[m][j][u];
+                }
+    }
+    meet(sm.red, sm.cta, Tn);
+    for (int q = rank * kThreads + threadIdx.x; q < Tn * kCols; q += S * kThreads) {
+        const int tok = q / kCols, col = c0 + q % kCols;
+        if (col >= a.d) continue;
+        float s = 0.f;
+        for (int r = 0; r < S; ++r) s += ld_cluster(sm.cta + q, r);
+        if (a.b2) {
+            for (uint32_t m = R.mask[tok]; m; m &= m - 1) {
+                const int e = __ffs(m) - 1;
+                float w;
+                weight(tok, e, w);
+                s = fmaf(w, to_f32(((const T*)a.b2)[(size_t)e * a.d + col]), s);
+            }
+        }
+        const size_t at = (size_t)(t0 + tok) * a.d + col;
+        if (a.residual) s += to_f32(((const T*)a.x)[at]);
+        ((T*)a.y)[at] = (T)s;
+    }
+    cluster_sync_all();
+}
+
+template <typename... KArgs, typename... Args>
+cudaError_t launch_clusters(void (*kern)(KArgs...), dim3 grid, int S, size_t smem, cudaStream_t s, Args&&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = S;
+    at[1].val.clusterDim.y = 1;
+    at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
+}
+
+constexpr int kMaxSmem = 160 * 1024;
+
+// CTAs of a cluster: as many as leave every warp a unit of the contraction, and no more than the SMs hold (two CTAs each).
+int split_of(int units, long long tiles) {
+    int S = 8;
+    while (S > 1 && (units < S * kWarps || tiles * S > 2ll * sm_count())) S >>= 1;
+    return S;
+}
+
+template <int WT, int MT>
+uoe_status launch_layers(const TokArgs& a, cudaStream_t s) {
+    static DeviceOnce once1, once2;
+    uoe_status st = smem_opt_in(once1, first_layer_kernel<WT, MT>, kMaxSmem);
+    if (st == UOE_OK) st = smem_opt_in(once2, second_layer_kernel<WT, MT>, kMaxSmem);
+    if (st != UOE_OK) return st;
+    const int groups = (a.T + kTok - 1) / kTok, Tn = a.T < kTok ? a.T : kTok;
+    constexpr int UL = WT == kFp8 ? 64 : 16;
+    const long long chosen = a.n < (long long)Tn * a.k ? a.n : (long long)Tn * a.k;      // experts at most
+    {
+        const long long tiles = chosen * ((a.d_e + kCols - 1) / kCols);
+        const int S = split_of((a.d + UL - 1) / UL, 1);
+        long long clusters = 2ll * sm_count() / (S * groups);
+        if (clusters < 1) clusters = 1;
+        if (clusters > tiles) clusters = tiles;
+        ProfScope ps("tokens_first", s);
+        launch_clusters(first_layer_kernel<WT, MT>, dim3((unsigned)(clusters * S), 1, groups), S, Smem::bytes(Tn, a.n, S), s, a, S);
+        UOE_LAUNCHED();
+    }
+    {
+        const long long tiles = (a.d + kCols - 1) / kCols;
+        const int S = split_of((int)(a.k * ((a.d_e + UL - 1) / UL)), tiles * groups);
+        ProfScope ps("tokens_second", s);
+        launch_clusters(second_layer_kernel<WT, MT>, dim3((unsigned)(tiles * S), 1, groups), S, Smem::bytes(Tn, a.n, S), s, a, S);
+        UOE_LAUNCHED();
+    }
+    return UOE_OK;
+}
+
+template <int WT>
+uoe_status launch_tokens(const TokArgs& a, cudaStream_t s) {
+    return a.T <= 16 ? launch_layers<WT, 1>(a, s) : launch_layers<WT, 2>(a, s);
+}
+
+}  // namespace
+
+size_t mlp_tokens_workspace_bytes(const Dims& D) {
+    if (D.L != 1 || D.B > kMaxTokens) return 0;
+    return align_up(kStatusBytes + (size_t)((D.B + kTok - 1) / kTok) * D.n * kTok * D.d_e * D.esize, 1024);
+}
+
+}  // namespace uoe
+
+using namespace uoe;
+
+extern "C" uoe_status uoe_mlp_tokens(const uoe_problem* prob, const void* x, const void* W_r, const void* W1, const float* w1_scale,
+                                     const void* W2, const float* w2_scale, const void* b1, const void* b2, const uoe_routing* r, void* y,
+                                     void* ws, size_t ws_bytes, void* cuda_stream) {
+    Dims D;
+    const uoe_status st = make_dims(prob, D);
+    if (st != UOE_OK) return st;
+    if (D.d_e < 1 || !x || !W_r || !W1 || !W2 || !y || !ws || (w1_scale == nullptr) != (w2_scale == nullptr)) return UOE_ERR_INVALID_ARG;
+    for (const void* p : {x, W_r, W1, W2, (const void*)w1_scale, (const void*)w2_scale, b1, b2, (const void*)y, (const void*)ws})
+        if (p && !aligned16(p)) return UOE_ERR_INVALID_ARG;
+    if (x == y) return UOE_ERR_INVALID_ARG;
+    if (r && (!r->expert_idx || !r->patch_idx || !r->gate || !r->p_samp || !r->p_patch || !r->expert_offsets)) return UOE_ERR_INVALID_ARG;
+    if (D.L != 1 || D.B > kMaxTokens || (D.d_e * D.esize) % 16 != 0 || (w1_scale && !D.bf16)) return UOE_ERR_UNSUPPORTED;
+    if (ws_bytes < mlp_tokens_workspace_bytes(D)) return UOE_ERR_WORKSPACE;
+    TokArgs a = {};
+    a.x = x; a.Wr = W_r; a.W1 = W1; a.W2 = W2; a.b1 = b1; a.b2 = b2; a.s1 = w1_scale; a.s2 = w2_scale;
+    a.a = (char*)ws + kStatusBytes; a.y = y;
+    if (r) a.r = RoutingPtrs{r->expert_idx, r->patch_idx, r->gate, r->p_samp, r->p_patch, r->expert_offsets};
+    a.T = D.B; a.d = D.d; a.d_e = D.d_e; a.n = D.n; a.k = D.k; a.act = prob->act;
+    a.use_gate = (prob->flags & UOE_FLAG_GATE) != 0; a.residual = (prob->flags & UOE_FLAG_RESIDUAL) != 0;
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    if (!D.bf16) return launch_tokens<kF32>(a, s);
+    return w1_scale ? launch_tokens<kFp8>(a, s) : launch_tokens<kBf16>(a, s);
+}
