@@ -52,6 +52,21 @@ __device__ __forceinline__ float act_precise(float h, int act) {
     }
 }
 
+// The same for N values, chosen once.
+template <int N>
+__device__ __forceinline__ void act_precise_n(float* f, int act) {
+    if (act == UOE_ACT_SILU) {
+#pragma unroll
+        for (int q = 0; q < N; ++q) f[q] = act_precise(f[q], UOE_ACT_SILU);
+    } else if (act == UOE_ACT_GELU_TANH) {
+#pragma unroll
+        for (int q = 0; q < N; ++q) f[q] = act_precise(f[q], UOE_ACT_GELU_TANH);
+    } else if (act == UOE_ACT_GELU_ERF) {
+#pragma unroll
+        for (int q = 0; q < N; ++q) f[q] = act_precise(f[q], UOE_ACT_GELU_ERF);
+    }
+}
+
 // x [rows of C elements] -> q [rows, Cp], scale [Cp / 128, rows]: every row by itself.  With map.on() row r of the output is the
 // token that routed row r holds (zeros on padding rows and unused slots), and only rows below offsets[n] are written.
 uoe_status launch_quantize_rows(const void* x, bool bf16, int G, long long rows, int C, void* q, float* scale, const SrcMap& map,

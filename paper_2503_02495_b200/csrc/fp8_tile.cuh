@@ -64,12 +64,14 @@ __device__ __forceinline__ void store_tile(const Fp8Args& a, float* sum, int e, 
     if constexpr (EPI == kFp8ActQuant) {
         static_assert(EPI != kFp8ActQuant || (!WGRAD && CW == kQ), "a thread holds one block of the result");
         uint32_t m = 0;
+        if (a.bias) {
 #pragma unroll
-        for (int q = 0; q < CW; ++q) {
-            if (a.bias && col + q < a.N) sum[q] += to_f32(a.bias[(size_t)e * a.N + col + q]);
-            sum[q] = act_precise(sum[q], a.act);
-            m = max(m, abs_bits(sum[q]));
+            for (int q = 0; q < CW; ++q)
+                if (col + q < a.N) sum[q] += to_f32(a.bias[(size_t)e * a.N + col + q]);
         }
+        act_precise_n<CW>(sum, a.act);
+#pragma unroll
+        for (int q = 0; q < CW; ++q) m = max(m, abs_bits(sum[q]));
         const BlockScale b = block_scale(m);
         a.qs[(size_t)(col / kQ) * a.M + row] = b.s;
         uint8_t* o = a.q + (size_t)row * a.ldq + col;

@@ -4,12 +4,14 @@
 // Bound by the weights of the chosen experts, each read once: one token per row tile of 128 would leave the tensor cores waiting for
 // memory all the same, so the products run on mma.sync fragments that come straight from global memory, without a pass through
 // shared memory.  Up to 32 tokens (one or two 16-row fragments) share a weight fragment.
-//   first_layer_kernel   routes, then a = phi(x W1 + b1) for every (chosen expert, 64 hidden columns): clusters of S CTAs walk these tiles,
-//                        the S * 8 warps of a cluster split the contraction, their sums meet in distributed shared memory
-//   second_layer_kernel  routes again (a few KB from L2, instead of a wait for the first kernel), asks for its weights (L2 prefetch)
-//                        while the first kernel runs, then y = x + sum over experts gate (a W2 + b2): a cluster per 64 columns of y, its
-//                        warps split the contraction over all chosen experts' hidden columns in one line
-// The router's sums are cut into 8 pieces of d whatever the cluster size, so that both kernels choose the same experts.
+//   first_layer_kernel   routes, then a = phi(x W1 + b1) for every (chosen expert, 64 hidden columns)
+//   second_layer_kernel  routes again (a few KB from L2, instead of a wait for the first kernel), then y = x + sum over experts
+//                        gate (a W2 + b2) for every 64 columns of y, the contraction running over all chosen experts' hidden columns in one line
+// Both run in clusters of eight CTAs, which share the router's work (an eighth of d each; cut finer by warp, the same cut in both kernels
+// and at every size, so that both choose the same experts) and, S CTAs to a tile, the contraction of a tile, whose sums meet in
+// distributed shared memory.  S is the largest split that leaves no more than two CTAs per SM.
+// As soon as the experts are known a CTA asks for all the weights it will read, and for its share of the second layer's, by prefetches to
+// L2: memory is busy from there on to the end, whatever the two kernels' loads wait for.
 // Sums are added in an order that depends on sizes alone.
 //
 // Fragments (m16n8k16: a lane g * 4 + t holds k = 2t, 2t+1, 2t+8, 2t+9 of row g of A and column g of B).  The order of k inside a step is
@@ -31,7 +33,7 @@ constexpr int kTok = 32;            // tokens of a group (a z slice of the grid)
 constexpr int kMaxTokens = 64;
 constexpr int kCols = 64;           // columns of a tile
 constexpr int kWarps = 8, kThreads = 32 * kWarps;
-constexpr int kPieces = 8;          // of d, in the router's sums
+constexpr int kCluster = 8;         // CTAs; the router's sums have as many pieces
 enum { kBf16 = 0, kFp8 = 1, kF32 = 2 };
 
 struct TokArgs {
@@ -57,6 +59,9 @@ __device__ __forceinline__ float ld_cluster(const float* p, uint32_t rank) {
     return v;
 }
 
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+
 __device__ __forceinline__ void mma16(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
@@ -69,16 +74,16 @@ __device__ __forceinline__ uint32_t bf16x2_of_e4m3x2(uint32_t v) {
     return pack_bf16x2(f.x, f.y);
 }
 
-// Sums over this CTA's pieces of d: part[piece / S][token * n + expert], pieces rank, rank + S, ...
+// Sums over this CTA's piece of d: part[token * n + expert].
 template <int WT, int MT>
-__device__ void router_pieces(const TokArgs& a, int t0, int Tn, int rank, int S, float* red /* [8][Tn * n] */, float* part) {
+__device__ void router_piece(const TokArgs& a, int t0, int Tn, int rank, float* red /* [8][Tn * n] */, float* part) {
     using T = typename Elem<WT>::T;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int d = a.d, n = a.n, len = ((d + kPieces - 1) / kPieces + 15) / 16 * 16;
+    const int d = a.d, n = a.n, len = ((d + kCluster - 1) / kCluster + 15) / 16 * 16;
     const T* x = (const T*)a.x + (size_t)t0 * d;
     const T* Wr = (const T*)a.Wr;
-    for (int p = rank; p < kPieces; p += S) {
-        const int k0 = p * len, k1 = min(d, k0 + len);
+    const int k0 = rank * len, k1 = min(d, k0 + len);
+    {
         if constexpr (WT == kF32) {
             // a warp per (token, expert)
             for (int q = warp; q < Tn * n; q += kWarps) {
@@ -87,7 +92,7 @@ __device__ void router_pieces(const TokArgs& a, int t0, int Tn, int rank, int S,
                 for (int kk = k0 + lane; kk < k1; kk += 32) s = fmaf(x[(size_t)tok * d + kk], Wr[(size_t)kk * n + i], s);
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-                if (lane == 0) part[(p / S) * Tn * n + q] = s;
+                if (lane == 0) part[q] = s;
             }
         } else {
             const int J = (n + 7) / 8;                 // fragment j: experts g * J + j
@@ -136,19 +141,18 @@ __device__ void router_pieces(const TokArgs& a, int t0, int Tn, int rank, int S,
                 float s = 0.f;
 #pragma unroll
                 for (int w = 0; w < kWarps; ++w) s += red[w * Tn * n + q];
-                part[(p / S) * Tn * n + q] = s;
+                part[q] = s;
             }
-            __syncthreads();
         }
     }
 }
 
 // Eq. 21-22 for the group's tokens, the same in every CTA.
 template <int WT, int MT>
-__device__ void route_tokens(const TokArgs& a, int t0, int Tn, int rank, int S, float* red, float* part, Routed& R) {
-    router_pieces<WT, MT>(a, t0, Tn, rank, S, red, part);
+__device__ void route_tokens(const TokArgs& a, int t0, int Tn, int rank, float* red, float* part, Routed& R) {
+    router_piece<WT, MT>(a, t0, Tn, rank, red, part);
     if (threadIdx.x == 0) R.any = 0;
-    cluster_sync_all();                                // every CTA's pieces are there
+    cluster_sync_all();                                // every CTA's piece is there
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = a.n;
     uint32_t any = 0;
     for (int tok = warp; tok < Tn; tok += kWarps) {
@@ -156,7 +160,7 @@ __device__ void route_tokens(const TokArgs& a, int t0, int Tn, int rank, int S, 
         if (lane < n) {
             v = 0.f;
 #pragma unroll
-            for (int p = 0; p < kPieces; ++p) v += ld_cluster(part + (p / S) * Tn * n + tok * n + lane, p % S);
+            for (int p = 0; p < kCluster; ++p) v += ld_cluster(part + tok * n + lane, p);
         }
         float mx = v;
 #pragma unroll
@@ -179,6 +183,7 @@ __device__ void route_tokens(const TokArgs& a, int t0, int Tn, int rank, int S, 
         any |= m;
     }
     if (lane == 0 && any) atomicOr(&R.any, any);
+    cluster_arrive();                                  // done with the others' pieces (cluster_wait follows before the next meeting, or the end)
     __syncthreads();
 }
 
@@ -326,20 +331,18 @@ __device__ __forceinline__ void cut(int units, int workers, int w, int& lo, int&
     lo = (int)((long long)units * w / workers);
     hi = (int)((long long)units * (w + 1) / workers);
 }
-template <int WT> __device__ __forceinline__ constexpr int unit_len() { return WT == kFp8 ? 64 : 16; }
+template <int WT> __host__ __device__ constexpr int unit_len() { return WT == kFp8 ? 64 : 16; }
 
 struct Smem {                       // dynamic shared memory, sizes in floats
     float *red, *cta, *part;
     Routed* R;
-    __device__ Smem(uint8_t* base, int Tn, int n, int S) {
+    __device__ Smem(uint8_t* base, int Tn, int n) {
         red = (float*)base;
-        cta = red + kWarps * Tn * (n > kCols ? n : kCols);
-        part = cta + 2 * Tn * kCols;
-        R = (Routed*)(part + (kPieces / S) * Tn * n);
+        cta = red + kWarps * Tn * kCols;               // (n <= 32: the router's partial sums fit as well)
+        part = cta + Tn * kCols;
+        R = (Routed*)(part + Tn * n);
     }
-    static size_t bytes(int Tn, int n, int S) {
-        return sizeof(float) * ((size_t)kWarps * Tn * (n > kCols ? n : kCols) + 2 * Tn * kCols + (size_t)(kPieces / S) * Tn * n) + sizeof(Routed);
-    }
+    static size_t bytes(int Tn, int n) { return sizeof(float) * ((size_t)(kWarps + 1) * Tn * kCols + (size_t)Tn * n) + sizeof(Routed); }
 };
 
 // This CTA's sums of a tile (its warps' parts added in order) into its buffer `cta`, visible to the whole cluster.
@@ -351,7 +354,37 @@ __device__ __forceinline__ void meet(const float* red, float* cta, int Tn) {
         for (int w = 0; w < kWarps; ++w) s += red[w * Tn * kCols + q];
         cta[q] = s;
     }
+    cluster_wait();
     cluster_sync_all();
+}
+
+// One warp: its part [k0, k1) of an expert's matrix and the tile's columns on their way to L2.
+template <int WT>
+__device__ __forceinline__ void prefetch_tile(const void* W, int c0, int N, int K, int k0, int k1) {
+    const int lane = threadIdx.x & 31;
+    if constexpr (WT == kFp8) {
+        const size_t Kp = (size_t)(K + kQ - 1) / kQ * kQ;
+        for (int q = lane; q < kCols * ((k1 - k0 + kQ - 1) / kQ); q += 32) {
+            const int row = c0 + q % kCols;
+            if (row < N) asm volatile("prefetch.global.L2 [%0];" :: "l"((const uint8_t*)W + (size_t)row * Kp + k0 + q / kCols * kQ));
+        }
+    } else {
+        using T = typename Elem<WT>::T;
+        constexpr int LINES = kCols * sizeof(T) / 128;
+        for (int q = lane; q < (k1 - k0) * LINES; q += 32) {
+            const int col = c0 + q % LINES * (128 / (int)sizeof(T));
+            if (col < N) asm volatile("prefetch.global.L2 [%0];" :: "l"((const T*)W + (size_t)(k0 + q / LINES) * N + col));
+        }
+    }
+}
+// Part `part` of `parts` of an expert's whole matrix of `bytes` bytes, by one warp.
+__device__ __forceinline__ void prefetch_share(const void* W, size_t bytes, int part, int parts) {
+    const size_t lines = (bytes + 127) / 128, lo = lines * part / parts, hi = lines * (part + 1) / parts;
+    for (size_t q = lo + (threadIdx.x & 31); q < hi; q += 32) asm volatile("prefetch.global.L2 [%0];" :: "l"((const uint8_t*)W + q * 128));
+}
+template <int WT>
+__device__ __forceinline__ size_t matrix_bytes(int K, int N) {
+    return WT == kFp8 ? (size_t)N * ((K + kQ - 1) / kQ * kQ) : (size_t)K * N * sizeof(typename Elem<WT>::T);
 }
 
 template <int WT, int MT>
@@ -361,14 +394,27 @@ first_layer_kernel(const TokArgs a, int S) {
     extern __shared__ __align__(16) uint8_t smem_raw[];
     const int rank = (int)cluster_ctarank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int t0 = blockIdx.z * kTok, Tn = min(kTok, a.T - t0);
-    Smem sm(smem_raw, Tn, a.n, S);
+    Smem sm(smem_raw, Tn, a.n);
     pdl_wait();
     // Only now: when the second kernel starts, everything in front of this one is complete, and it may read the inputs at once.
     pdl_trigger();
-    route_tokens<WT, MT>(a, t0, Tn, rank, S, sm.red, sm.part, *sm.R);
+    route_tokens<WT, MT>(a, t0, Tn, rank, sm.red, sm.part, *sm.R);
     const Routed& R = *sm.R;
-    const int cluster = blockIdx.x / S, clusters = gridDim.x / S;
-    if (cluster == 0 && rank == 0 && a.r.expert_idx) {
+    const int tiles_n = (a.d_e + kCols - 1) / kCols, tiles = __popc(R.any) * tiles_n;
+    const int tile = blockIdx.x / S, kr = rank % S, first = rank - kr;        // this CTA's tile, its place among the tile's CTAs, the first of them
+    const bool live = tile < tiles;
+    const int slot = live ? tile / tiles_n : 0, c0 = (tile - slot * tiles_n) * kCols, e = nth_bit(R.any, slot);
+    int lo, hi;
+    cut((a.d + unit_len<WT>() - 1) / unit_len<WT>(), S * kWarps, kr * kWarps + warp, lo, hi);
+    const int k0 = lo * unit_len<WT>(), k1 = min(a.d, hi * unit_len<WT>());
+    const void* W = (const uint8_t*)a.W1 + (size_t)e * matrix_bytes<WT>(a.d, a.d_e);
+    if (live) {
+        prefetch_tile<WT>(W, c0, a.d_e, a.d, k0, k1);
+        // the second layer's weights of the same expert: the tile's warps share them with those of the expert's other tiles
+        prefetch_share((const uint8_t*)a.W2 + (size_t)e * matrix_bytes<WT>(a.d_e, a.d), matrix_bytes<WT>(a.d_e, a.d),
+                       ((tile - slot * tiles_n) * S + kr) * kWarps + warp, tiles_n * S * kWarps);
+    }
+    if (blockIdx.x == 0 && a.r.expert_idx) {
         for (int tok = warp; tok < Tn; tok += kWarps) {
             const uint32_t m = R.mask[tok];
             const size_t b = t0 + tok;
@@ -381,18 +427,12 @@ first_layer_kernel(const TokArgs a, int S) {
             }
         }
     }
-    const int tiles_n = (a.d_e + kCols - 1) / kCols, tiles = __popc(R.any) * tiles_n;
     const T* x = (const T*)a.x + (size_t)t0 * a.d;
     T* out = (T*)a.a + (size_t)blockIdx.z * a.n * kTok * a.d_e;
-    int lo, hi, buf = 0;
-    cut((a.d + unit_len<WT>() - 1) / unit_len<WT>(), S * kWarps, rank * kWarps + warp, lo, hi);
-    const int k0 = lo * unit_len<WT>(), k1 = min(a.d, hi * unit_len<WT>());
-    for (int tile = cluster; tile < tiles; tile += clusters) {
-        const int slot = tile / tiles_n, c0 = (tile - slot * tiles_n) * kCols, e = nth_bit(R.any, slot);
-        float* red = sm.red + warp * Tn * kCols;
+    float* red = sm.red + warp * Tn * kCols;
+    if (live) {
         if constexpr (WT == kF32) {
-            accumulate_f32(red, (const float*)x, a.d, Tn, (const float*)a.W1 + (size_t)e * a.d * a.d_e, c0, a.d_e, k0, k1, true,
-                           [](int, float& w) { w = 1.f; return true; });
+            accumulate_f32(red, (const float*)x, a.d, Tn, (const float*)W, c0, a.d_e, k0, k1, true, [](int, float& w) { w = 1.f; return true; });
         } else {
             float c[MT][8][4];
 #pragma unroll
@@ -401,9 +441,7 @@ first_layer_kernel(const TokArgs a, int S) {
                 for (int j = 0; j < 8; ++j)
 #pragma unroll
                     for (int u = 0; u < 4; ++u) c[m][j][u] = 0.f;
-            const size_t Kp = (size_t)(a.d + kQ - 1) / kQ * kQ;
-            const void* W = WT == kFp8 ? (const void*)((const uint8_t*)a.W1 + (size_t)e * a.d_e * Kp) : (const void*)((const T*)a.W1 + (size_t)e * a.d * a.d_e);
-            const float* sc = WT == kFp8 ? a.s1 + ((size_t)e * ((a.d_e + kQ - 1) / kQ) + c0 / kQ) * (Kp / kQ) : nullptr;
+            const float* sc = WT == kFp8 ? a.s1 + ((size_t)e * ((a.d_e + kQ - 1) / kQ) + c0 / kQ) * ((a.d + kQ - 1) / kQ) : nullptr;
             accumulate<WT, MT>(c, (const __nv_bfloat16*)x, a.d, Tn, W, sc, c0, a.d_e, a.d, k0, k1);
 #pragma unroll
             for (int m = 0; m < MT; ++m)
@@ -415,18 +453,18 @@ first_layer_kernel(const TokArgs a, int S) {
                         if (row < Tn) red[row * kCols + col_of<WT>(j, u, t)] = c[m][j][u];
                     }
         }
-        float* cta = sm.cta + buf * Tn * kCols;
-        meet(sm.red, cta, Tn);
-        for (int q = rank * kThreads + threadIdx.x; q < Tn * kCols; q += S * kThreads) {
+    }
+    meet(sm.red, sm.cta, Tn);
+    if (live) {
+        for (int q = kr * kThreads + threadIdx.x; q < Tn * kCols; q += S * kThreads) {
             const int tok = q / kCols, col = c0 + q % kCols;
             if (col >= a.d_e || !((R.mask[tok] >> e) & 1)) continue;
             float h = 0.f;
-            for (int s = 0; s < S; ++s) h += ld_cluster(cta + q, s);
+            for (int s = 0; s < S; ++s) h += ld_cluster(sm.cta + q, first + s);
             if (a.b1) h += to_f32(((const T*)a.b1)[(size_t)e * a.d_e + col]);
             // (bfloat16: half a step, 2^-9 of the value, like the hidden rows of uoe_mlp_forward)
             out[((size_t)slot * kTok + tok) * a.d_e + col] = (T)act_precise(h, a.act);
         }
-        buf ^= 1;
     }
     cluster_sync_all();            // nobody's shared memory goes while another CTA may read it
 }
@@ -438,37 +476,17 @@ second_layer_kernel(const TokArgs a, int S) {
     extern __shared__ __align__(16) uint8_t smem_raw[];
     const int rank = (int)cluster_ctarank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int t0 = blockIdx.z * kTok, Tn = min(kTok, a.T - t0);
-    Smem sm(smem_raw, Tn, a.n, S);
+    Smem sm(smem_raw, Tn, a.n);
     pdl_trigger();
-    route_tokens<WT, MT>(a, t0, Tn, rank, S, sm.red, sm.part, *sm.R);
+    route_tokens<WT, MT>(a, t0, Tn, rank, sm.red, sm.part, *sm.R);
     const Routed& R = *sm.R;
-    const int c0 = blockIdx.x / S * kCols;
+    const int c0 = blockIdx.x / S * kCols, kr = rank % S, first = rank - kr;
+    const bool live = c0 < a.d;                        // (the grid is whole clusters)
     constexpr int UL = unit_len<WT>();
     const int per = (a.d_e + UL - 1) / UL;             // units of one expert
     int lo, hi;
-    cut(__popc(R.any) * per, S * kWarps, rank * kWarps + warp, lo, hi);
-    const size_t Kp = (size_t)(a.d_e + kQ - 1) / kQ * kQ;
-    auto weights = [&](int e) -> const void* {
-        if constexpr (WT == kFp8) return (const uint8_t*)a.W2 + (size_t)e * a.d * Kp;
-        else return (const T*)a.W2 + (size_t)e * a.d_e * a.d;
-    };
-    for (int u = lo; u < hi;) {                        // this warp's weights on their way to L2 while the first kernel runs
-        const int slot = u / per, k0 = (u - slot * per) * UL, n_u = min(hi - u, per - (u - slot * per)), k1 = min(a.d_e, k0 + n_u * UL);
-        const int e = nth_bit(R.any, slot);
-        if constexpr (WT == kFp8) {
-            for (int q = lane; q < kCols * ((k1 - k0 + kQ - 1) / kQ); q += 32) {
-                const int row = c0 + q % kCols;
-                if (row < a.d) asm volatile("prefetch.global.L2 [%0];" :: "l"((const uint8_t*)weights(e) + (size_t)row * Kp + k0 + q / kCols * kQ));
-            }
-        } else {
-            constexpr int LINES = kCols * sizeof(T) / 128;
-            for (int q = lane; q < (k1 - k0) * LINES; q += 32) {
-                const int col = c0 + q % LINES * (128 / (int)sizeof(T));
-                if (col < a.d) asm volatile("prefetch.global.L2 [%0];" :: "l"((const T*)weights(e) + (size_t)(k0 + q / LINES) * a.d + col));
-            }
-        }
-        u += n_u;
-    }
+    cut(live ? __popc(R.any) * per : 0, S * kWarps, kr * kWarps + warp, lo, hi);
+    auto weights = [&](int e) { return (const void*)((const uint8_t*)a.W2 + (size_t)e * matrix_bytes<WT>(a.d_e, a.d)); };
     pdl_wait();
     if (blockIdx.x == 0 && blockIdx.z == 0 && warp == 0 && a.r.expert_offsets) {      // Eq. 23, from every group's choices
         int cnt = 0;
@@ -519,7 +537,7 @@ second_layer_kernel(const TokArgs a, int S) {
                 for (int j = 0; j < 8; ++j)
 #pragma unroll
                     for (int v = 0; v < 4; ++v) c[m][j][v] = 0.f;
-            const float* sc = WT == kFp8 ? a.s2 + ((size_t)e * ((a.d + kQ - 1) / kQ) + c0 / kQ) * (Kp / kQ) : nullptr;
+            const float* sc = WT == kFp8 ? a.s2 + ((size_t)e * ((a.d + kQ - 1) / kQ) + c0 / kQ) * ((a.d_e + kQ - 1) / kQ) : nullptr;
             accumulate<WT, MT>(c, (const __nv_bfloat16*)A, a.d_e, Tn, weights(e), sc, c0, a.d, a.d_e, k0, k1);
             // the tokens that chose this expert take its sums (the hidden rows of the others were never written)
 #pragma unroll
@@ -551,11 +569,11 @@ second_layer_kernel(const TokArgs a, int S) {
                 }
     }
     meet(sm.red, sm.cta, Tn);
-    for (int q = rank * kThreads + threadIdx.x; q < Tn * kCols; q += S * kThreads) {
+    for (int q = kr * kThreads + threadIdx.x; q < Tn * kCols; q += S * kThreads) {
         const int tok = q / kCols, col = c0 + q % kCols;
         if (col >= a.d) continue;
         float s = 0.f;
-        for (int r = 0; r < S; ++r) s += ld_cluster(sm.cta + q, r);
+        for (int r = 0; r < S; ++r) s += ld_cluster(sm.cta + q, first + r);
         if (a.b2) {
             for (uint32_t m = R.mask[tok]; m; m &= m - 1) {
                 const int e = __ffs(m) - 1;
@@ -572,7 +590,7 @@ second_layer_kernel(const TokArgs a, int S) {
 }
 
 template <typename... KArgs, typename... Args>
-cudaError_t launch_clusters(void (*kern)(KArgs...), dim3 grid, int S, size_t smem, cudaStream_t s, Args&&... args) {
+cudaError_t launch_clusters(void (*kern)(KArgs...), dim3 grid, size_t smem, cudaStream_t s, Args&&... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(kThreads);
@@ -582,7 +600,7 @@ cudaError_t launch_clusters(void (*kern)(KArgs...), dim3 grid, int S, size_t sme
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = S;
+    at[1].val.clusterDim.x = kCluster;
     at[1].val.clusterDim.y = 1;
     at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
@@ -592,9 +610,9 @@ cudaError_t launch_clusters(void (*kern)(KArgs...), dim3 grid, int S, size_t sme
 
 constexpr int kMaxSmem = 160 * 1024;
 
-// CTAs of a cluster: as many as leave every warp a unit of the contraction, and no more than the SMs hold (two CTAs each).
+// CTAs of a tile: the largest split that leaves every warp a unit of the contraction and no more than two CTAs per SM.
 int split_of(int units, long long tiles) {
-    int S = 8;
+    int S = kCluster;
     while (S > 1 && (units < S * kWarps || tiles * S > 2ll * sm_count())) S >>= 1;
     return S;
 }
@@ -606,23 +624,21 @@ uoe_status launch_layers(const TokArgs& a, cudaStream_t s) {
     if (st == UOE_OK) st = smem_opt_in(once2, second_layer_kernel<WT, MT>, kMaxSmem);
     if (st != UOE_OK) return st;
     const int groups = (a.T + kTok - 1) / kTok, Tn = a.T < kTok ? a.T : kTok;
-    constexpr int UL = WT == kFp8 ? 64 : 16;
+    constexpr int UL = unit_len<WT>();
     const long long chosen = a.n < (long long)Tn * a.k ? a.n : (long long)Tn * a.k;      // experts at most
+    auto grid = [&](long long tiles, int S) { return dim3((unsigned)((tiles * S + kCluster - 1) / kCluster * kCluster), 1, groups); };
     {
         const long long tiles = chosen * ((a.d_e + kCols - 1) / kCols);
-        const int S = split_of((a.d + UL - 1) / UL, 1);
-        long long clusters = 2ll * sm_count() / (S * groups);
-        if (clusters < 1) clusters = 1;
-        if (clusters > tiles) clusters = tiles;
+        const int S = split_of((a.d + UL - 1) / UL, tiles * groups);
         ProfScope ps("tokens_first", s);
-        launch_clusters(first_layer_kernel<WT, MT>, dim3((unsigned)(clusters * S), 1, groups), S, Smem::bytes(Tn, a.n, S), s, a, S);
+        launch_clusters(first_layer_kernel<WT, MT>, grid(tiles, S), Smem::bytes(Tn, a.n), s, a, S);
         UOE_LAUNCHED();
     }
     {
         const long long tiles = (a.d + kCols - 1) / kCols;
         const int S = split_of((int)(a.k * ((a.d_e + UL - 1) / UL)), tiles * groups);
         ProfScope ps("tokens_second", s);
-        launch_clusters(second_layer_kernel<WT, MT>, dim3((unsigned)(tiles * S), 1, groups), S, Smem::bytes(Tn, a.n, S), s, a, S);
+        launch_clusters(second_layer_kernel<WT, MT>, grid(tiles, S), Smem::bytes(Tn, a.n), s, a, S);
         UOE_LAUNCHED();
     }
     return UOE_OK;
