@@ -10,16 +10,16 @@
 // Both run in clusters of eight CTAs, which share the router's work (an eighth of d each; cut finer by warp, the same cut in both kernels
 // and at every size, so that both choose the same experts) and, S CTAs to a tile, the contraction of a tile, whose sums meet in
 // distributed shared memory.  S is the largest split that leaves no more than two CTAs per SM.
-// As soon as the experts are known a CTA asks for all the weights it will read, and for its share of the second layer's, by prefetches to
-// L2: memory is busy from there on to the end, whatever the two kernels' loads wait for.
 // Sums are added in an order that depends on sizes alone.
 //
-// Fragments (m16n8k16: a lane g * 4 + t holds k = 2t, 2t+1, 2t+8, 2t+9 of row g of A and column g of B).  The order of k inside a step is
-// free as long as both operands have the same one: slots 2t, 2t+1, 2t+8, 2t+9 hold k = 4t .. 4t+3.
+// Fragments (m16n8k16): the weights are the 16-row operand (two fragments of 8 columns), the tokens the 8-column one, so up to eight tokens cost
+// one instruction per 16 columns and step.  A lane g * 4 + t holds k = 2t, 2t+1, 2t+8, 2t+9 of rows g and g + 8 of the one and of column g of
+// the other; the order of k inside a step is free as long as both have the same one: those slots hold k = 4t .. 4t+3.
 //   bfloat16 weights [K, N]   a lane loads 16 bytes, columns 8g .. 8g+7, of rows 4t .. 4t+3 (a warp: 16 whole 128-byte lines) and pairs the
 //                             rows' halves: fragment j holds columns 8g + j
-//   8-bit weights [N, Kp]     a lane loads 16 bytes of k, 16t .. 16t+15, of row 8j + g: four steps of fragment j.  e4m3 -> half -> float
-//                             -> bfloat16 is exact; the block's scale multiplies the float32 sums of 64 of the contraction
+//   8-bit weights [N, Kp]     a lane loads 16 bytes of k, 16t .. 16t+15, of row 8j + g: four steps of fragment j.  As half they are
+//                             exact (one instruction a pair; to bfloat16 it takes four); the activations become half by a power of two per
+//                             token and 64 of the contraction, which with the block's scale multiplies the float32 sums of those 64
 //   float32 weights [K, N]    float32 multiply-adds, eight tokens at a time
 #include "fp8.cuh"
 #include "tc.cuh"
@@ -63,15 +63,17 @@ __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
 __device__ __forceinline__ void mma16(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// e4m3 pair (low half of v) -> bfloat16 pair, exact
-__device__ __forceinline__ uint32_t bf16x2_of_e4m3x2(uint32_t v) {
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)v, __NV_E4M3);
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-    return pack_bf16x2(f.x, f.y);
+__device__ __forceinline__ void mma16_half(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// four e4m3 bytes -> two half pairs, exact
+__device__ __forceinline__ void halves_of_e4m3(uint32_t v, uint32_t& lo, uint32_t& hi) {
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}" : "=r"(lo), "=r"(hi) : "r"(v));
 }
 
 // Sums over this CTA's piece of d: part[token * n + expert].
@@ -192,19 +194,19 @@ __device__ __forceinline__ int nth_bit(uint32_t m, int i) {
     return __ffs(m) - 1;
 }
 
-// One warp: c[m][j] += A[rows, k0 .. k1) W[k0 .. k1, columns], fragments of columns as in the file's head.  A [Tn rows, ld], W the
-// expert's matrix, its first column c0 of N.  scale: 8-bit weights only, [K / 128] of this column block.
-template <int WT, int MT>
-__device__ __forceinline__ void accumulate(float (*c)[8][4], const __nv_bfloat16* A, int ld, int Tn, const void* W, const float* scale, int c0, int N, int K,
+// One warp: c[q][i] += the products of A's rows (tokens) 8 q .. 8 q + 7 with W[k0 .. k1, columns of fragments 2 i and 2 i + 1].  A [Tn rows, ld];
+// W the expert's matrix, its first column c0 of N.  scale: 8-bit weights only, [K / 128] of this column block.
+template <int WT, int G>
+__device__ __forceinline__ void accumulate(float (*c)[4][4], const __nv_bfloat16* A, int ld, int Tn, const void* W, const float* scale, int c0, int N, int K,
                                            int k0, int k1) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     if constexpr (WT == kBf16) {
-        constexpr int U = 2;                           // steps of 16 in flight: 4 KB of weights per warp
+        constexpr int U = G == 1 ? 4 : 2;              // steps of 16 in flight: 8 or 4 KB of weights per warp
         const __nv_bfloat16* w0 = (const __nv_bfloat16*)W + c0 + 8 * g;
         const bool col_ok = c0 + 8 * g < N;
         for (int kk = k0; kk < k1; kk += 16 * U) {
             uint4 w[U][4];
-            uint2 x[U][MT][2];
+            uint2 x[U][G];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int kt = kk + 16 * u + 4 * t;
@@ -212,12 +214,7 @@ __device__ __forceinline__ void accumulate(float (*c)[8][4], const __nv_bfloat16
 #pragma unroll
                 for (int r = 0; r < 4; ++r) w[u][r] = ok && col_ok ? ld_stream16(w0 + (size_t)(kt + r) * N) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-                for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int row = m * 16 + h * 8 + g;
-                        x[u][m][h] = ok && row < Tn ? *(const uint2*)(A + (size_t)row * ld + kt) : make_uint2(0, 0);
-                    }
+                for (int q = 0; q < G; ++q) x[u][q] = ok && 8 * q + g < Tn ? *(const uint2*)(A + (size_t)(8 * q + g) * ld + kt) : make_uint2(0, 0);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -226,68 +223,98 @@ __device__ __forceinline__ void accumulate(float (*c)[8][4], const __nv_bfloat16
                 const uint32_t* r2 = (const uint32_t*)&w[u][2];
                 const uint32_t* r3 = (const uint32_t*)&w[u][3];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const uint32_t sel = j & 1 ? 0x7632 : 0x5410;
-                    const uint32_t b0 = __byte_perm(r0[j >> 1], r1[j >> 1], sel), b1 = __byte_perm(r2[j >> 1], r3[j >> 1], sel);
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t f[4] = {__byte_perm(r0[i], r1[i], 0x5410), __byte_perm(r0[i], r1[i], 0x7632),
+                                           __byte_perm(r2[i], r3[i], 0x5410), __byte_perm(r2[i], r3[i], 0x7632)};
 #pragma unroll
-                    for (int m = 0; m < MT; ++m) {
-                        const uint32_t af[4] = {x[u][m][0].x, x[u][m][1].x, x[u][m][0].y, x[u][m][1].y};
-                        mma16(c[m][j], af, b0, b1);
-                    }
+                    for (int q = 0; q < G; ++q) mma16(c[q][i], f, x[u][q].x, x[u][q].y);
                 }
             }
         }
     } else {
+        constexpr int U = G == 1 ? 2 : 1;              // units of 64 in flight
         const size_t Kp = (size_t)(K + kQ - 1) / kQ * kQ;
         const uint8_t* w0 = (const uint8_t*)W + (size_t)(c0 + g) * Kp + 16 * t;
-        for (int kk = k0; kk < k1; kk += 64) {         // (cuts are multiples of 64)
-            uint4 w[8];
-            uint4 x[MT][2][2];
+        for (int kb = k0; kb < k1; kb += 64 * U) {     // (cuts are multiples of 64)
+            uint4 w[U][8], x[U][G][2];
+            float s[U];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] = c0 + 8 * j + g < N ? ld_stream16(w0 + (size_t)8 * j * Kp + kk) : make_uint4(0, 0, 0, 0);
-            const float s = __ldg(scale + kk / kQ);
+            for (int u = 0; u < U; ++u) {
+                const int kk = kb + 64 * u;
+                const bool ok = kk < k1;
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+                for (int j = 0; j < 8; ++j) w[u][j] = ok && c0 + 8 * j + g < N ? ld_stream16(w0 + (size_t)8 * j * Kp + kk) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int q = 0; q < G; ++q)
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        const int row = m * 16 + h * 8 + g, kt = kk + 16 * t + 8 * q;
-                        x[m][h][q] = row < Tn && kt < K ? *(const uint4*)(A + (size_t)row * ld + kt) : make_uint4(0, 0, 0, 0);
+                    for (int h = 0; h < 2; ++h) {
+                        const int kt = kk + 16 * t + 8 * h;
+                        x[u][q][h] = ok && 8 * q + g < Tn && kt < K ? *(const uint4*)(A + (size_t)(8 * q + g) * ld + kt) : make_uint4(0, 0, 0, 0);
                     }
+                s[u] = ok ? __ldg(scale + kk / kQ) : 0.f;
+            }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t* wj = (const uint32_t*)&w[j];
-                float p[MT][4];
+            for (int u = 0; u < U; ++u) {
+                // A token's 64 values as half: times a power of two that brings the largest of them to [2^14, 2^15), exact but for what lies
+                // 2^-29 below it (an error of 2^-40 of the largest, where the float32 sums have 2^-24); the power goes back in with the block's scale
+                float back[G][2];                      // of tokens 2 t and 2 t + 1
 #pragma unroll
-                for (int m = 0; m < MT; ++m)
+                for (int q = 0; q < G; ++q) {
+                    uint32_t* v = (uint32_t*)&x[u][q][0];
+                    uint32_t top = 0;
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) p[m][u] = 0.f;
+                    for (int i = 0; i < 8; ++i) top = __vmaxu2(top, v[i] & 0x7fff7fffu);
+                    top = max(top >> 16, top & 0xffffu) << 16;          // float bits of the largest magnitude
+                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                    // (a token with an infinity or NaN keeps it: half has both.  Factors within the floats' normal range.)
+                    const uint32_t e = min(max(top >> 23, 16u), 254u);
+                    const float f = __uint_as_float((268u - e) << 23);  // 2^(14 - (e - 127))
+                    const float r = s[u] * __uint_as_float((e - 14u) << 23);
+                    back[q][0] = __shfl_sync(0xffffffffu, r, 8 * t);
+                    back[q][1] = __shfl_sync(0xffffffffu, r, 8 * t + 4);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {          // k = 16 t + 4 i .. + 3
-                    const uint32_t b0 = bf16x2_of_e4m3x2(wj[i] & 0xffff), b1 = bf16x2_of_e4m3x2(wj[i] >> 16);
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) {
-                        const uint32_t* lo = (const uint32_t*)&x[m][0][i >> 1];
-                        const uint32_t* hi = (const uint32_t*)&x[m][1][i >> 1];
-                        const uint32_t af[4] = {lo[2 * (i & 1)], hi[2 * (i & 1)], lo[2 * (i & 1) + 1], hi[2 * (i & 1) + 1]};
-                        mma16(p[m], af, b0, b1);
+                    for (int i = 0; i < 8; ++i) {
+                        const __half2 p = __floats2half2_rn(__uint_as_float(v[i] << 16) * f, __uint_as_float(v[i] & 0xffff0000u) * f);
+                        v[i] = *reinterpret_cast<const uint32_t*>(&p);
                     }
                 }
 #pragma unroll
-                for (int m = 0; m < MT; ++m)
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t* wa = (const uint32_t*)&w[u][2 * i];
+                    const uint32_t* wb = (const uint32_t*)&w[u][2 * i + 1];
+                    float p[G][4];
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) c[m][j][u] = fmaf(s, p[m][u], c[m][j][u]);
+                    for (int q = 0; q < G; ++q)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) p[q][v] = 0.f;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {      // k = 16 t + 4 k .. + 3
+                        uint32_t f[4];
+                        halves_of_e4m3(wa[k], f[0], f[2]);
+                        halves_of_e4m3(wb[k], f[1], f[3]);
+#pragma unroll
+                        for (int q = 0; q < G; ++q) {
+                            const uint32_t* xv = (const uint32_t*)&x[u][q][0];
+                            mma16_half(p[q], f, xv[2 * k], xv[2 * k + 1]);
+                        }
+                    }
+#pragma unroll
+                    for (int q = 0; q < G; ++q)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) c[q][i][v] = fmaf(back[q][v & 1], p[q][v], c[q][i][v]);
+                }
             }
         }
     }
 }
 
-// Column of the tile that element u of fragment j is in.
+// Column of the tile, and token, of sum v of c[q][i].
 template <int WT>
-__device__ __forceinline__ int col_of(int j, int u, int t) {
-    return WT == kBf16 ? 8 * (2 * t + (u & 1)) + j : 8 * j + 2 * t + (u & 1);
+__device__ __forceinline__ int col_of(int i, int v, int g) {
+    return WT == kBf16 ? 8 * g + 2 * i + (v >> 1) : 8 * (2 * i + (v >> 1)) + g;
 }
+__device__ __forceinline__ int token_of_sum(int q, int v, int t) { return 8 * q + 2 * t + (v & 1); }
 
 // float32: a half warp takes every other row of W, a lane four columns; eight tokens per pass over the weights.  Adds weight(tok) times the
 // product to red[tok][col] of this warp (first: sets it).
@@ -358,37 +385,13 @@ __device__ __forceinline__ void meet(const float* red, float* cta, int Tn) {
     cluster_sync_all();
 }
 
-// One warp: its part [k0, k1) of an expert's matrix and the tile's columns on their way to L2.
-template <int WT>
-__device__ __forceinline__ void prefetch_tile(const void* W, int c0, int N, int K, int k0, int k1) {
-    const int lane = threadIdx.x & 31;
-    if constexpr (WT == kFp8) {
-        const size_t Kp = (size_t)(K + kQ - 1) / kQ * kQ;
-        for (int q = lane; q < kCols * ((k1 - k0 + kQ - 1) / kQ); q += 32) {
-            const int row = c0 + q % kCols;
-            if (row < N) asm volatile("prefetch.global.L2 [%0];" :: "l"((const uint8_t*)W + (size_t)row * Kp + k0 + q / kCols * kQ));
-        }
-    } else {
-        using T = typename Elem<WT>::T;
-        constexpr int LINES = kCols * sizeof(T) / 128;
-        for (int q = lane; q < (k1 - k0) * LINES; q += 32) {
-            const int col = c0 + q % LINES * (128 / (int)sizeof(T));
-            if (col < N) asm volatile("prefetch.global.L2 [%0];" :: "l"((const T*)W + (size_t)(k0 + q / LINES) * N + col));
-        }
-    }
-}
-// Part `part` of `parts` of an expert's whole matrix of `bytes` bytes, by one warp.
-__device__ __forceinline__ void prefetch_share(const void* W, size_t bytes, int part, int parts) {
-    const size_t lines = (bytes + 127) / 128, lo = lines * part / parts, hi = lines * (part + 1) / parts;
-    for (size_t q = lo + (threadIdx.x & 31); q < hi; q += 32) asm volatile("prefetch.global.L2 [%0];" :: "l"((const uint8_t*)W + q * 128));
-}
 template <int WT>
 __device__ __forceinline__ size_t matrix_bytes(int K, int N) {
     return WT == kFp8 ? (size_t)N * ((K + kQ - 1) / kQ * kQ) : (size_t)K * N * sizeof(typename Elem<WT>::T);
 }
 
-template <int WT, int MT>
-__global__ void __launch_bounds__(kThreads, MT == 1 ? 2 : 1)
+template <int WT, int G>
+__global__ void __launch_bounds__(kThreads, G < 4 ? 2 : 1)
 first_layer_kernel(const TokArgs a, int S) {
     using T = typename Elem<WT>::T;
     extern __shared__ __align__(16) uint8_t smem_raw[];
@@ -398,7 +401,7 @@ first_layer_kernel(const TokArgs a, int S) {
     pdl_wait();
     // Only now: when the second kernel starts, everything in front of this one is complete, and it may read the inputs at once.
     pdl_trigger();
-    route_tokens<WT, MT>(a, t0, Tn, rank, sm.red, sm.part, *sm.R);
+    route_tokens<WT, (G + 1) / 2>(a, t0, Tn, rank, sm.red, sm.part, *sm.R);
     const Routed& R = *sm.R;
     const int tiles_n = (a.d_e + kCols - 1) / kCols, tiles = __popc(R.any) * tiles_n;
     const int tile = blockIdx.x / S, kr = rank % S, first = rank - kr;        // this CTA's tile, its place among the tile's CTAs, the first of them
@@ -408,12 +411,6 @@ first_layer_kernel(const TokArgs a, int S) {
     cut((a.d + unit_len<WT>() - 1) / unit_len<WT>(), S * kWarps, kr * kWarps + warp, lo, hi);
     const int k0 = lo * unit_len<WT>(), k1 = min(a.d, hi * unit_len<WT>());
     const void* W = (const uint8_t*)a.W1 + (size_t)e * matrix_bytes<WT>(a.d, a.d_e);
-    if (live) {
-        prefetch_tile<WT>(W, c0, a.d_e, a.d, k0, k1);
-        // the second layer's weights of the same expert: the tile's warps share them with those of the expert's other tiles
-        prefetch_share((const uint8_t*)a.W2 + (size_t)e * matrix_bytes<WT>(a.d_e, a.d), matrix_bytes<WT>(a.d_e, a.d),
-                       ((tile - slot * tiles_n) * S + kr) * kWarps + warp, tiles_n * S * kWarps);
-    }
     if (blockIdx.x == 0 && a.r.expert_idx) {
         for (int tok = warp; tok < Tn; tok += kWarps) {
             const uint32_t m = R.mask[tok];
@@ -434,24 +431,16 @@ first_layer_kernel(const TokArgs a, int S) {
         if constexpr (WT == kF32) {
             accumulate_f32(red, (const float*)x, a.d, Tn, (const float*)W, c0, a.d_e, k0, k1, true, [](int, float& w) { w = 1.f; return true; });
         } else {
-            float c[MT][8][4];
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) c[m][j][u] = 0.f;
+            float c[G][4][4] = {};
             const float* sc = WT == kFp8 ? a.s1 + ((size_t)e * ((a.d_e + kQ - 1) / kQ) + c0 / kQ) * ((a.d + kQ - 1) / kQ) : nullptr;
-            accumulate<WT, MT>(c, (const __nv_bfloat16*)x, a.d, Tn, W, sc, c0, a.d_e, a.d, k0, k1);
+            accumulate<WT, G>(c, (const __nv_bfloat16*)x, a.d, Tn, W, sc, c0, a.d_e, a.d, k0, k1);
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+            for (int q = 0; q < G; ++q)
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const int row = m * 16 + (u >> 1) * 8 + g;
-                        if (row < Tn) red[row * kCols + col_of<WT>(j, u, t)] = c[m][j][u];
-                    }
+                    for (int v = 0; v < 4; ++v)
+                        if (token_of_sum(q, v, t) < Tn) red[token_of_sum(q, v, t) * kCols + col_of<WT>(i, v, g)] = c[q][i][v];
         }
     }
     meet(sm.red, sm.cta, Tn);
@@ -469,8 +458,8 @@ first_layer_kernel(const TokArgs a, int S) {
     cluster_sync_all();            // nobody's shared memory goes while another CTA may read it
 }
 
-template <int WT, int MT>
-__global__ void __launch_bounds__(kThreads, MT == 1 ? 2 : 1)
+template <int WT, int G>
+__global__ void __launch_bounds__(kThreads, G < 4 ? 2 : 1)
 second_layer_kernel(const TokArgs a, int S) {
     using T = typename Elem<WT>::T;
     extern __shared__ __align__(16) uint8_t smem_raw[];
@@ -478,7 +467,7 @@ second_layer_kernel(const TokArgs a, int S) {
     const int t0 = blockIdx.z * kTok, Tn = min(kTok, a.T - t0);
     Smem sm(smem_raw, Tn, a.n);
     pdl_trigger();
-    route_tokens<WT, MT>(a, t0, Tn, rank, sm.red, sm.part, *sm.R);
+    route_tokens<WT, (G + 1) / 2>(a, t0, Tn, rank, sm.red, sm.part, *sm.R);
     const Routed& R = *sm.R;
     const int c0 = blockIdx.x / S * kCols, kr = rank % S, first = rank - kr;
     const bool live = c0 < a.d;                        // (the grid is whole clusters)
@@ -515,13 +504,7 @@ second_layer_kernel(const TokArgs a, int S) {
         for (int q = lane; q < Tn * kCols; q += 32) red[q] = 0.f;
         __syncwarp();
     }
-    float tot[MT][8][4];
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-            for (int u = 0; u < 4; ++u) tot[m][j][u] = 0.f;
+    float tot[G][4][4] = {};
     for (int u = lo; u < hi;) {
         const int slot = u / per, k0 = (u - slot * per) * UL, n_u = min(hi - u, per - (u - slot * per)), k1 = min(a.d_e, k0 + n_u * UL);
         const int e = nth_bit(R.any, slot);
@@ -530,27 +513,21 @@ second_layer_kernel(const TokArgs a, int S) {
             accumulate_f32(red, (const float*)A, a.d_e, Tn, (const float*)weights(e), c0, a.d, k0, k1, false,
                            [&](int tok, float& w) { return weight(tok, e, w); });
         } else {
-            float c[MT][8][4];
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) c[m][j][v] = 0.f;
+            float c[G][4][4] = {};
             const float* sc = WT == kFp8 ? a.s2 + ((size_t)e * ((a.d + kQ - 1) / kQ) + c0 / kQ) * ((a.d_e + kQ - 1) / kQ) : nullptr;
-            accumulate<WT, MT>(c, (const __nv_bfloat16*)A, a.d_e, Tn, weights(e), sc, c0, a.d, a.d_e, k0, k1);
+            accumulate<WT, G>(c, (const __nv_bfloat16*)A, a.d_e, Tn, weights(e), sc, c0, a.d, a.d_e, k0, k1);
             // the tokens that chose this expert take its sums (the hidden rows of the others were never written)
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+            for (int q = 0; q < G; ++q)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int row = m * 16 + h * 8 + g;
+                    const int tok = token_of_sum(q, h, t);
                     float w = 0.f;
-                    if (row < Tn && weight(row, e, w)) {
+                    if (tok < Tn && weight(tok, e, w)) {
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            tot[m][j][2 * h] = fmaf(w, c[m][j][2 * h], tot[m][j][2 * h]);
-                            tot[m][j][2 * h + 1] = fmaf(w, c[m][j][2 * h + 1], tot[m][j][2 * h + 1]);
+                        for (int i = 0; i < 4; ++i) {
+                            tot[q][i][h] = fmaf(w, c[q][i][h], tot[q][i][h]);
+                            tot[q][i][2 + h] = fmaf(w, c[q][i][2 + h], tot[q][i][2 + h]);
                         }
                     }
                 }
@@ -559,14 +536,12 @@ second_layer_kernel(const TokArgs a, int S) {
     }
     if constexpr (WT != kF32) {
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int q = 0; q < G; ++q)
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const int row = m * 16 + (u >> 1) * 8 + g;
-                    if (row < Tn) red[row * kCols + col_of<WT>(j, u, t)] = tot[m][j][u];
-                }
+                for (int v = 0; v < 4; ++v)
+                    if (token_of_sum(q, v, t) < Tn) red[token_of_sum(q, v, t) * kCols + col_of<WT>(i, v, g)] = tot[q][i][v];
     }
     meet(sm.red, sm.cta, Tn);
     for (int q = kr * kThreads + threadIdx.x; q < Tn * kCols; q += S * kThreads) {
@@ -617,11 +592,11 @@ int split_of(int units, long long tiles) {
     return S;
 }
 
-template <int WT, int MT>
+template <int WT, int G>
 uoe_status launch_layers(const TokArgs& a, cudaStream_t s) {
     static DeviceOnce once1, once2;
-    uoe_status st = smem_opt_in(once1, first_layer_kernel<WT, MT>, kMaxSmem);
-    if (st == UOE_OK) st = smem_opt_in(once2, second_layer_kernel<WT, MT>, kMaxSmem);
+    uoe_status st = smem_opt_in(once1, first_layer_kernel<WT, G>, kMaxSmem);
+    if (st == UOE_OK) st = smem_opt_in(once2, second_layer_kernel<WT, G>, kMaxSmem);
     if (st != UOE_OK) return st;
     const int groups = (a.T + kTok - 1) / kTok, Tn = a.T < kTok ? a.T : kTok;
     constexpr int UL = unit_len<WT>();
@@ -631,14 +606,14 @@ uoe_status launch_layers(const TokArgs& a, cudaStream_t s) {
         const long long tiles = chosen * ((a.d_e + kCols - 1) / kCols);
         const int S = split_of((a.d + UL - 1) / UL, tiles * groups);
         ProfScope ps("tokens_first", s);
-        launch_clusters(first_layer_kernel<WT, MT>, grid(tiles, S), Smem::bytes(Tn, a.n), s, a, S);
+        launch_clusters(first_layer_kernel<WT, G>, grid(tiles, S), Smem::bytes(Tn, a.n), s, a, S);
         UOE_LAUNCHED();
     }
     {
         const long long tiles = (a.d + kCols - 1) / kCols;
         const int S = split_of((int)(a.k * ((a.d_e + UL - 1) / UL)), tiles * groups);
         ProfScope ps("tokens_second", s);
-        launch_clusters(second_layer_kernel<WT, MT>, grid(tiles, S), Smem::bytes(Tn, a.n), s, a, S);
+        launch_clusters(second_layer_kernel<WT, G>, grid(tiles, S), Smem::bytes(Tn, a.n), s, a, S);
         UOE_LAUNCHED();
     }
     return UOE_OK;
@@ -646,7 +621,8 @@ uoe_status launch_layers(const TokArgs& a, cudaStream_t s) {
 
 template <int WT>
 uoe_status launch_tokens(const TokArgs& a, cudaStream_t s) {
-    return a.T <= 16 ? launch_layers<WT, 1>(a, s) : launch_layers<WT, 2>(a, s);
+    if (a.T <= 8) return launch_layers<WT, 1>(a, s);
+    return a.T <= 16 ? launch_layers<WT, 2>(a, s) : launch_layers<WT, 4>(a, s);
 }
 
 }  // namespace
