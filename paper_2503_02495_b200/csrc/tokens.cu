@@ -5,11 +5,11 @@
 // memory all the same, so the products run on mma.sync fragments that come straight from global memory, without a pass through
 // shared memory.  Up to 32 tokens (one or two 16-row fragments) share a weight fragment.
 //   first_layer_kernel   routes, then a = phi(x W1 + b1) for every (chosen expert, 64 hidden columns)
-//   second_layer_kernel  routes again (a few KB from L2, instead of a wait for the first kernel), then y = x + sum over experts
-//                        gate (a W2 + b2) for every 64 columns of y, the contraction running over all chosen experts' hidden columns in one line
-// Both run in clusters of eight CTAs, which share the router's work (an eighth of d each; cut finer by warp, the same cut in both kernels
-// and at every size, so that both choose the same experts) and, S CTAs to a tile, the contraction of a tile, whose sums meet in
-// distributed shared memory.  S is the largest split that leaves no more than two CTAs per SM.
+//   second_layer_kernel  y = x + sum over experts gate (a W2 + b2) for every 64 columns of y, the contraction running over all chosen
+//                        experts' hidden columns in one line
+// Both run in clusters of eight CTAs.  The first kernel's share the router's work, an eighth of d each, and every cluster routes for itself
+// (a few KB from L2, instead of a third kernel).  S CTAs of a cluster share a tile's contraction, and their sums meet in distributed shared
+// memory; S is the largest split that leaves no more than two CTAs per SM.
 // Sums are added in an order that depends on sizes alone.
 //
 // Fragments (m16n8k16): the weights are the 16-row operand (two fragments of 8 columns), the tokens the 8-column one, so up to eight tokens cost
@@ -39,6 +39,7 @@ enum { kBf16 = 0, kFp8 = 1, kF32 = 2 };
 struct TokArgs {
     const void *x, *Wr, *W1, *W2, *b1, *b2;
     const float *s1, *s2;
+    struct Routed* routed;          // [groups]: what the first kernel's router says, for the second
     void *a, *y;                    // a [groups, n, kTok, d_e]: hidden rows by place in the group's list of chosen experts
     RoutingPtrs r;                  // all null, or all to be written
     int T, d, d_e, n, k, act, use_gate, residual;
@@ -47,7 +48,7 @@ struct TokArgs {
 template <int WT> struct Elem { using T = __nv_bfloat16; };
 template <> struct Elem<kF32> { using T = float; };
 
-struct Routed {                     // shared memory: what the router says about this group's tokens
+struct Routed {                     // what the router says about a group's tokens
     uint32_t mask[kTok];            // chosen experts
     float p[kTok][32];              // sample gate (Eq. 21)
     uint32_t any;                   // experts that some token chose
@@ -185,7 +186,7 @@ __device__ void route_tokens(const TokArgs& a, int t0, int Tn, int rank, float* 
         any |= m;
     }
     if (lane == 0 && any) atomicOr(&R.any, any);
-    cluster_arrive();                                  // done with the others' pieces (cluster_wait follows before the next meeting, or the end)
+    cluster_arrive();                                  // done with the others' pieces (cluster_wait follows before the next meeting)
     __syncthreads();
 }
 
@@ -202,22 +203,26 @@ __device__ __forceinline__ void accumulate(float (*c)[4][4], const __nv_bfloat16
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     if constexpr (WT == kBf16) {
         constexpr int U = G == 1 ? 4 : 2;              // steps of 16 in flight: 8 or 4 KB of weights per warp
-        const __nv_bfloat16* w0 = (const __nv_bfloat16*)W + c0 + 8 * g;
-        const bool col_ok = c0 + 8 * g < N;
+        // (columns past the matrix are other columns again, whose sums nobody takes; rows of k past the cut are other rows, times zero)
+        const __nv_bfloat16* w0 = (const __nv_bfloat16*)W + min(c0 + 8 * g, N - 8);
         for (int kk = k0; kk < k1; kk += 16 * U) {
             uint4 w[U][4];
             uint2 x[U][G];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int kt = kk + 16 * u + 4 * t;
-                const bool ok = kt < k1;               // (K and the cuts are multiples of 4)
+                if (kk + 16 * u >= k1) break;
+                const int kt = kk + 16 * u + 4 * t, kc = min(kt, k1 - 4);             // (K and the cuts are multiples of 4)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) w[u][r] = ok && col_ok ? ld_stream16(w0 + (size_t)(kt + r) * N) : make_uint4(0, 0, 0, 0);
+                for (int r = 0; r < 4; ++r) w[u][r] = ld_stream16(w0 + (size_t)(kc + r) * N);
 #pragma unroll
-                for (int q = 0; q < G; ++q) x[u][q] = ok && 8 * q + g < Tn ? *(const uint2*)(A + (size_t)(8 * q + g) * ld + kt) : make_uint2(0, 0);
+                for (int q = 0; q < G; ++q) {
+                    x[u][q] = *(const uint2*)(A + (size_t)min(8 * q + g, Tn - 1) * ld + kc);
+                    if (kt >= k1) x[u][q] = make_uint2(0, 0);
+                }
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
+                if (kk + 16 * u >= k1) break;
                 const uint32_t* r0 = (const uint32_t*)&w[u][0];
                 const uint32_t* r1 = (const uint32_t*)&w[u][1];
                 const uint32_t* r2 = (const uint32_t*)&w[u][2];
@@ -232,35 +237,37 @@ __device__ __forceinline__ void accumulate(float (*c)[4][4], const __nv_bfloat16
             }
         }
     } else {
-        constexpr int U = G == 1 ? 2 : 1;              // units of 64 in flight
-        const size_t Kp = (size_t)(K + kQ - 1) / kQ * kQ;
-        const uint8_t* w0 = (const uint8_t*)W + (size_t)(c0 + g) * Kp + 16 * t;
-        for (int kb = k0; kb < k1; kb += 64 * U) {     // (cuts are multiples of 64)
-            uint4 w[U][8], x[U][G][2];
-            float s[U];
+        const uint32_t Kp = (uint32_t)((K + kQ - 1) / kQ * kQ);
+        // (columns past the matrix are its last one again, whose sums nobody takes; k past the matrix meets its zero padding)
+        const uint8_t* w0 = (const uint8_t*)W + (size_t)min(c0 + g, N - 1) * Kp + 16 * t;
+        const int last = max(N - 1 - c0 - g, 0);
+        struct Unit { uint4 w[8], x[G == 4 ? 1 : G][2]; float s; };     // (32 tokens: their values only when it is their turn)
+        auto load_x = [&](uint4* v, int q, int kk) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int kk = kb + 64 * u;
-                const bool ok = kk < k1;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) w[u][j] = ok && c0 + 8 * j + g < N ? ld_stream16(w0 + (size_t)8 * j * Kp + kk) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-                for (int q = 0; q < G; ++q)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int kt = kk + 16 * t + 8 * h;
-                        x[u][q][h] = ok && 8 * q + g < Tn && kt < K ? *(const uint4*)(A + (size_t)(8 * q + g) * ld + kt) : make_uint4(0, 0, 0, 0);
-                    }
-                s[u] = ok ? __ldg(scale + kk / kQ) : 0.f;
+            for (int h = 0; h < 2; ++h) {
+                v[h] = *(const uint4*)(A + (size_t)min(8 * q + g, Tn - 1) * ld + min(kk + 16 * t + 8 * h, K - 8));
             }
+        };
+        auto load = [&](Unit& v, int kk) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                // A token's 64 values as half: times a power of two that brings the largest of them to [2^14, 2^15), exact but for what lies
-                // 2^-29 below it (an error of 2^-40 of the largest, where the float32 sums have 2^-24); the power goes back in with the block's scale
-                float back[G][2];                      // of tokens 2 t and 2 t + 1
+            for (int j = 0; j < 8; ++j) v.w[j] = ld_stream16(w0 + kk + (size_t)(uint32_t)min(8 * j, last) * Kp);
+            if constexpr (G < 4) {
 #pragma unroll
-                for (int q = 0; q < G; ++q) {
-                    uint32_t* v = (uint32_t*)&x[u][q][0];
+                for (int q = 0; q < G; ++q) load_x(v.x[q], q, kk);
+            }
+            v.s = __ldg(scale + kk / kQ);
+        };
+        auto multiply = [&](Unit& n, int kk) {
+            // A token's 64 values as half: times a power of two that brings the largest of them to [2^14, 2^15), exact but for what lies
+            // 2^-29 below it (an error of 2^-40 of the largest, where the float32 sums have 2^-24); the power goes back in with the block's scale
+            constexpr int GG = G == 4 ? 1 : G;         // token groups at a time
+#pragma unroll
+            for (int q0 = 0; q0 < G; q0 += GG) {
+                if constexpr (G == 4) load_x(n.x[0], q0, kk);
+                float back[GG][2];                     // of tokens 2 t and 2 t + 1
+#pragma unroll
+                for (int q = 0; q < GG; ++q) {
+                    uint32_t* v = (uint32_t*)&n.x[q][0];
                     uint32_t top = 0;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) top = __vmaxu2(top, v[i] & 0x7fff7fffu);
@@ -270,7 +277,7 @@ __device__ __forceinline__ void accumulate(float (*c)[4][4], const __nv_bfloat16
                     // (a token with an infinity or NaN keeps it: half has both.  Factors within the floats' normal range.)
                     const uint32_t e = min(max(top >> 23, 16u), 254u);
                     const float f = __uint_as_float((268u - e) << 23);  // 2^(14 - (e - 127))
-                    const float r = s[u] * __uint_as_float((e - 14u) << 23);
+                    const float r = n.s * __uint_as_float((e - 14u) << 23);
                     back[q][0] = __shfl_sync(0xffffffffu, r, 8 * t);
                     back[q][1] = __shfl_sync(0xffffffffu, r, 8 * t + 4);
 #pragma unroll
@@ -281,30 +288,37 @@ __device__ __forceinline__ void accumulate(float (*c)[4][4], const __nv_bfloat16
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const uint32_t* wa = (const uint32_t*)&w[u][2 * i];
-                    const uint32_t* wb = (const uint32_t*)&w[u][2 * i + 1];
-                    float p[G][4];
-#pragma unroll
-                    for (int q = 0; q < G; ++q)
-#pragma unroll
-                        for (int v = 0; v < 4; ++v) p[q][v] = 0.f;
+                    const uint32_t* wa = (const uint32_t*)&n.w[2 * i];
+                    const uint32_t* wb = (const uint32_t*)&n.w[2 * i + 1];
+                    float p[GG][4] = {};
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {      // k = 16 t + 4 k .. + 3
                         uint32_t f[4];
                         halves_of_e4m3(wa[k], f[0], f[2]);
                         halves_of_e4m3(wb[k], f[1], f[3]);
 #pragma unroll
-                        for (int q = 0; q < G; ++q) {
-                            const uint32_t* xv = (const uint32_t*)&x[u][q][0];
+                        for (int q = 0; q < GG; ++q) {
+                            const uint32_t* xv = (const uint32_t*)&n.x[q][0];
                             mma16_half(p[q], f, xv[2 * k], xv[2 * k + 1]);
                         }
                     }
 #pragma unroll
-                    for (int q = 0; q < G; ++q)
+                    for (int q = 0; q < GG; ++q)
 #pragma unroll
-                        for (int v = 0; v < 4; ++v) c[q][i][v] = fmaf(back[q][v & 1], p[q][v], c[q][i][v]);
+                        for (int v = 0; v < 4; ++v) c[q0 + q][i][v] = fmaf(back[q][v & 1], p[q][v], c[q0 + q][i][v]);
                 }
             }
+        };
+        // (cuts are multiples of 64) a unit's loads are on their way while the one before it is multiplied
+        if (k0 >= k1) return;
+        Unit u0, u1;
+        load(u0, k0);
+        for (int kk = k0; kk < k1; kk += 128) {
+            if (kk + 64 < k1) load(u1, kk + 64);
+            multiply(u0, kk);
+            if (kk + 64 >= k1) break;
+            if (kk + 128 < k1) load(u0, kk + 128);
+            multiply(u1, kk + 64);
         }
     }
 }
@@ -372,8 +386,8 @@ struct Smem {                       // dynamic shared memory, sizes in floats
     static size_t bytes(int Tn, int n) { return sizeof(float) * ((size_t)(kWarps + 1) * Tn * kCols + (size_t)Tn * n) + sizeof(Routed); }
 };
 
-// This CTA's sums of a tile (its warps' parts added in order) into its buffer `cta`, visible to the whole cluster.
-__device__ __forceinline__ void meet(const float* red, float* cta, int Tn) {
+// This CTA's sums of a tile (its warps' parts added in order) into its buffer `cta`, visible to the CTAs that share the tile.
+__device__ __forceinline__ void meet(const float* red, float* cta, int Tn, int S) {
     __syncthreads();
     for (int q = threadIdx.x; q < Tn * kCols; q += kThreads) {
         float s = 0.f;
@@ -381,8 +395,8 @@ __device__ __forceinline__ void meet(const float* red, float* cta, int Tn) {
         for (int w = 0; w < kWarps; ++w) s += red[w * Tn * kCols + q];
         cta[q] = s;
     }
-    cluster_wait();
-    cluster_sync_all();
+    if (S > 1) cluster_sync_all();
+    else __syncthreads();
 }
 
 template <int WT>
@@ -391,16 +405,15 @@ __device__ __forceinline__ size_t matrix_bytes(int K, int N) {
 }
 
 template <int WT, int G>
-__global__ void __launch_bounds__(kThreads, G < 4 ? 2 : 1)
+__global__ void __launch_bounds__(kThreads, G == 1 ? 2 : 1)
 first_layer_kernel(const TokArgs a, int S) {
     using T = typename Elem<WT>::T;
     extern __shared__ __align__(16) uint8_t smem_raw[];
     const int rank = (int)cluster_ctarank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int t0 = blockIdx.z * kTok, Tn = min(kTok, a.T - t0);
     Smem sm(smem_raw, Tn, a.n);
-    pdl_wait();
-    // Only now: when the second kernel starts, everything in front of this one is complete, and it may read the inputs at once.
     pdl_trigger();
+    pdl_wait();
     route_tokens<WT, (G + 1) / 2>(a, t0, Tn, rank, sm.red, sm.part, *sm.R);
     const Routed& R = *sm.R;
     const int tiles_n = (a.d_e + kCols - 1) / kCols, tiles = __popc(R.any) * tiles_n;
@@ -411,6 +424,8 @@ first_layer_kernel(const TokArgs a, int S) {
     cut((a.d + unit_len<WT>() - 1) / unit_len<WT>(), S * kWarps, kr * kWarps + warp, lo, hi);
     const int k0 = lo * unit_len<WT>(), k1 = min(a.d, hi * unit_len<WT>());
     const void* W = (const uint8_t*)a.W1 + (size_t)e * matrix_bytes<WT>(a.d, a.d_e);
+    if (blockIdx.x == 0)
+        for (int q = threadIdx.x; q < (int)(sizeof(Routed) / 4); q += kThreads) ((uint32_t*)(a.routed + blockIdx.z))[q] = ((const uint32_t*)sm.R)[q];
     if (blockIdx.x == 0 && a.r.expert_idx) {
         for (int tok = warp; tok < Tn; tok += kWarps) {
             const uint32_t m = R.mask[tok];
@@ -443,7 +458,8 @@ first_layer_kernel(const TokArgs a, int S) {
                         if (token_of_sum(q, v, t) < Tn) red[token_of_sum(q, v, t) * kCols + col_of<WT>(i, v, g)] = c[q][i][v];
         }
     }
-    meet(sm.red, sm.cta, Tn);
+    cluster_wait();
+    meet(sm.red, sm.cta, Tn, S);
     if (live) {
         for (int q = kr * kThreads + threadIdx.x; q < Tn * kCols; q += S * kThreads) {
             const int tok = q / kCols, col = c0 + q % kCols;
@@ -455,11 +471,11 @@ first_layer_kernel(const TokArgs a, int S) {
             out[((size_t)slot * kTok + tok) * a.d_e + col] = (T)act_precise(h, a.act);
         }
     }
-    cluster_sync_all();            // nobody's shared memory goes while another CTA may read it
+    if (S > 1) cluster_sync_all();      // nobody's shared memory goes while another CTA may read it
 }
 
 template <int WT, int G>
-__global__ void __launch_bounds__(kThreads, G < 4 ? 2 : 1)
+__global__ void __launch_bounds__(kThreads, G == 1 ? 2 : 1)
 second_layer_kernel(const TokArgs a, int S) {
     using T = typename Elem<WT>::T;
     extern __shared__ __align__(16) uint8_t smem_raw[];
@@ -467,7 +483,9 @@ second_layer_kernel(const TokArgs a, int S) {
     const int t0 = blockIdx.z * kTok, Tn = min(kTok, a.T - t0);
     Smem sm(smem_raw, Tn, a.n);
     pdl_trigger();
-    route_tokens<WT, (G + 1) / 2>(a, t0, Tn, rank, sm.red, sm.part, *sm.R);
+    pdl_wait();
+    for (int q = threadIdx.x; q < (int)(sizeof(Routed) / 4); q += kThreads) ((uint32_t*)sm.R)[q] = __ldcg((const uint32_t*)(a.routed + blockIdx.z) + q);
+    __syncthreads();
     const Routed& R = *sm.R;
     const int c0 = blockIdx.x / S * kCols, kr = rank % S, first = rank - kr;
     const bool live = c0 < a.d;                        // (the grid is whole clusters)
@@ -476,7 +494,6 @@ second_layer_kernel(const TokArgs a, int S) {
     int lo, hi;
     cut(live ? __popc(R.any) * per : 0, S * kWarps, kr * kWarps + warp, lo, hi);
     auto weights = [&](int e) { return (const void*)((const uint8_t*)a.W2 + (size_t)e * matrix_bytes<WT>(a.d_e, a.d)); };
-    pdl_wait();
     if (blockIdx.x == 0 && blockIdx.z == 0 && warp == 0 && a.r.expert_offsets) {      // Eq. 23, from every group's choices
         int cnt = 0;
         for (int q0 = 0; q0 < a.T * a.k; q0 += 32) {
@@ -543,7 +560,7 @@ second_layer_kernel(const TokArgs a, int S) {
                 for (int v = 0; v < 4; ++v)
                     if (token_of_sum(q, v, t) < Tn) red[token_of_sum(q, v, t) * kCols + col_of<WT>(i, v, g)] = tot[q][i][v];
     }
-    meet(sm.red, sm.cta, Tn);
+    meet(sm.red, sm.cta, Tn, S);
     for (int q = kr * kThreads + threadIdx.x; q < Tn * kCols; q += S * kThreads) {
         const int tok = q / kCols, col = c0 + q % kCols;
         if (col >= a.d) continue;
@@ -561,7 +578,7 @@ second_layer_kernel(const TokArgs a, int S) {
         if (a.residual) s += to_f32(((const T*)a.x)[at]);
         ((T*)a.y)[at] = (T)s;
     }
-    cluster_sync_all();
+    if (S > 1) cluster_sync_all();
 }
 
 template <typename... KArgs, typename... Args>
@@ -629,7 +646,8 @@ uoe_status launch_tokens(const TokArgs& a, cudaStream_t s) {
 
 size_t mlp_tokens_workspace_bytes(const Dims& D) {
     if (D.L != 1 || D.B > kMaxTokens) return 0;
-    return align_up(kStatusBytes + (size_t)((D.B + kTok - 1) / kTok) * D.n * kTok * D.d_e * D.esize, 1024);
+    const int groups = (D.B + kTok - 1) / kTok;
+    return align_up(kStatusBytes + align_up(groups * sizeof(Routed), 1024) + (size_t)groups * D.n * kTok * D.d_e * D.esize, 1024);
 }
 
 }  // namespace uoe
@@ -651,7 +669,9 @@ extern "C" uoe_status uoe_mlp_tokens(const uoe_problem* prob, const void* x, con
     if (ws_bytes < mlp_tokens_workspace_bytes(D)) return UOE_ERR_WORKSPACE;
     TokArgs a = {};
     a.x = x; a.Wr = W_r; a.W1 = W1; a.W2 = W2; a.b1 = b1; a.b2 = b2; a.s1 = w1_scale; a.s2 = w2_scale;
-    a.a = (char*)ws + kStatusBytes; a.y = y;
+    a.routed = (Routed*)((char*)ws + kStatusBytes);
+    a.a = (char*)ws + kStatusBytes + align_up((D.B + kTok - 1) / kTok * sizeof(Routed), 1024);
+    a.y = y;
     if (r) a.r = RoutingPtrs{r->expert_idx, r->patch_idx, r->gate, r->p_samp, r->p_patch, r->expert_offsets};
     a.T = D.B; a.d = D.d; a.d_e = D.d_e; a.n = D.n; a.k = D.k; a.act = prob->act;
     a.use_gate = (prob->flags & UOE_FLAG_GATE) != 0; a.residual = (prob->flags & UOE_FLAG_RESIDUAL) != 0;
