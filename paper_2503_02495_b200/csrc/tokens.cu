@@ -195,130 +195,296 @@ __device__ __forceinline__ int nth_bit(uint32_t m, int i) {
     return __ffs(m) - 1;
 }
 
-// One warp: c[q][i] += the products of A's rows (tokens) 8 q .. 8 q + 7 with W[k0 .. k1, columns of fragments 2 i and 2 i + 1].  A [Tn rows, ld];
-// W the expert's matrix, its first column c0 of N.  scale: 8-bit weights only, [K / 128] of this column block.
-template <int WT, int G>
+// How the CTA's eight warps divide a tile.  Up to eight tokens: 64 columns, every warp by itself on an eighth of the contraction, its
+// activations straight from L2.  More tokens: 256 columns, four warps side by side times two halves of every 128 of the contraction,
+// which the CTA first brings into shared memory (as half, or as they are): that work is shared by four warps.  float32: 64 columns, 16
+// of every 128 of the contraction per warp, activations in shared memory as well.
+template <int WT, int G> struct Shape {
+    static constexpr bool STAGED = WT == kF32 || G > 1;
+    static constexpr int COLS = STAGED && WT != kF32 ? 256 : 64;
+    static constexpr int PARTS = kWarps * kCols / COLS;        // of the contraction, whose sums are added at the end
+    static constexpr int UNIT = STAGED ? 128 : WT == kFp8 ? 64 : 16;                      // of the contraction, in which it is cut
+    static constexpr int PITCH = WT == kFp8 ? 272 : WT == kBf16 ? 288 : 32 * G;           // bytes of a staged token (float32: of one k of all)
+    static constexpr int STAGE = WT == kF32 ? 128 * PITCH : 8 * G * PITCH;
+    static constexpr int BACK = WT == kFp8 ? 2 * 8 * G * 4 : 0;                           // factors of the two halves behind it
+    static constexpr int CTAS = G == 1 && WT != kF32 ? 2 : 1;                             // per SM
+};
+
+// A token's values as half: times a power of two that brings the largest of a 64 to [2^14, 2^15), exact but for what lies 2^-29 below it (an
+// error of 2^-40 of the largest, where the float32 sums have 2^-24); the power goes back in with the block's scale.  v: 16 values of
+// bfloat16 in each of the four neighbouring lanes that hold the 64; returns the power.
+__device__ __forceinline__ float to_half64(uint32_t* v) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = __vmaxu2(top, v[i] & 0x7fff7fffu);
+    top = max(top >> 16, top & 0xffffu) << 16;                  // float bits of the largest magnitude
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    // (a token with an infinity or NaN keeps it: half has both.  Factors within the floats' normal range.)
+    const uint32_t e = min(max(top >> 23, 16u), 254u);
+    const float f = __uint_as_float((268u - e) << 23);          // 2^(14 - (e - 127))
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const __half2 p = __floats2half2_rn(__uint_as_float(v[i] << 16) * f, __uint_as_float(v[i] & 0xffff0000u) * f);
+        v[i] = *reinterpret_cast<const uint32_t*>(&p);
+    }
+    return __uint_as_float((e - 14u) << 23);
+}
+
+// 64 of the contraction of 64 columns of 8-bit weights: w[j] holds k = 16 t .. 16 t + 15 of column 8 j + g.  x(q, v): this lane's 16 values of
+// token 8 q + g as half; back[q]: factors of the sums of tokens 8 q + 2 t and the next.
+template <int G, typename X>
+__device__ __forceinline__ void multiply_fp8(float (*c)[4][4], const uint4* w, X x, const float (*back)[2]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t* wa = (const uint32_t*)&w[2 * i];
+        const uint32_t* wb = (const uint32_t*)&w[2 * i + 1];
+        float p[G][4] = {};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {                          // k = 16 t + 4 k .. + 3
+            uint32_t f[4];
+            halves_of_e4m3(wa[k], f[0], f[2]);
+            halves_of_e4m3(wb[k], f[1], f[3]);
+#pragma unroll
+            for (int q = 0; q < G; ++q) {
+                const uint2 v = x(q, k);
+                mma16_half(p[q], f, v.x, v.y);
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < G; ++q)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) c[q][i][v] = fmaf(back[q][v & 1], p[q][v], c[q][i][v]);
+    }
+}
+// A step of 16 of the contraction of 64 columns of bfloat16 weights: w[r] holds columns 8 g .. 8 g + 7 of k = 4 t + r.
+template <int G>
+__device__ __forceinline__ void multiply_bf16(float (*c)[4][4], const uint4* w, const uint2* x) {
+    const uint32_t* r0 = (const uint32_t*)&w[0];
+    const uint32_t* r1 = (const uint32_t*)&w[1];
+    const uint32_t* r2 = (const uint32_t*)&w[2];
+    const uint32_t* r3 = (const uint32_t*)&w[3];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t f[4] = {__byte_perm(r0[i], r1[i], 0x5410), __byte_perm(r0[i], r1[i], 0x7632),
+                               __byte_perm(r2[i], r3[i], 0x5410), __byte_perm(r2[i], r3[i], 0x7632)};
+#pragma unroll
+        for (int q = 0; q < G; ++q) mma16(c[q][i], f, x[q].x, x[q].y);
+    }
+}
+
+// 64 columns of 8-bit weights from column c0 on, 64 of the contraction from kk on.  (Columns past the matrix are its last one again, whose
+// sums nobody takes; k past the matrix meets its zero padding.)
+struct Fp8Columns {
+    const uint8_t* p;
+    uint32_t Kp;
+    int last;
+    __device__ Fp8Columns(const void* W, int c0, int N, int K) {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+        Kp = (uint32_t)((K + kQ - 1) / kQ * kQ);
+        p = (const uint8_t*)W + (size_t)min(c0 + g, N - 1) * Kp + 16 * t;
+        last = max(N - 1 - c0 - g, 0);
+    }
+    __device__ __forceinline__ void load(uint4* w, int kk) const {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = ld_stream16(p + kk + (size_t)(uint32_t)min(8 * j, last) * Kp);
+    }
+};
+
+// Up to eight tokens, one warp by itself: c[i] += the products of A's rows with W[k0 .. k1, columns of fragments 2 i and 2 i + 1].  A [Tn rows,
+// ld]; W the expert's matrix, its first column c0 of N.  scale: 8-bit weights only, [K / 128] of this column block.
+template <int WT>
 __device__ __forceinline__ void accumulate(float (*c)[4][4], const __nv_bfloat16* A, int ld, int Tn, const void* W, const float* scale, int c0, int N, int K,
                                            int k0, int k1) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const __nv_bfloat16* mine = A + (size_t)min(g, Tn - 1) * ld;           // (tokens past the last are the last again, whose sums nobody takes)
+    if (k0 >= k1) return;
     if constexpr (WT == kBf16) {
-        constexpr int U = G == 1 ? 4 : 2;              // steps of 16 in flight: 8 or 4 KB of weights per warp
-        // (columns past the matrix are other columns again, whose sums nobody takes; rows of k past the cut are other rows, times zero)
+        constexpr int U = 4;                           // steps of 16 in flight: 8 KB of weights per warp
+        // (columns past the matrix are other columns again; rows of k past the cut are other rows, times zero)
         const __nv_bfloat16* w0 = (const __nv_bfloat16*)W + min(c0 + 8 * g, N - 8);
         for (int kk = k0; kk < k1; kk += 16 * U) {
             uint4 w[U][4];
-            uint2 x[U][G];
+            uint2 x[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (kk + 16 * u >= k1) break;
                 const int kt = kk + 16 * u + 4 * t, kc = min(kt, k1 - 4);             // (K and the cuts are multiples of 4)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) w[u][r] = ld_stream16(w0 + (size_t)(kc + r) * N);
-#pragma unroll
-                for (int q = 0; q < G; ++q) {
-                    x[u][q] = *(const uint2*)(A + (size_t)min(8 * q + g, Tn - 1) * ld + kc);
-                    if (kt >= k1) x[u][q] = make_uint2(0, 0);
-                }
+                x[u] = *(const uint2*)(mine + kc);
+                if (kt >= k1) x[u] = make_uint2(0, 0);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (kk + 16 * u >= k1) break;
-                const uint32_t* r0 = (const uint32_t*)&w[u][0];
-                const uint32_t* r1 = (const uint32_t*)&w[u][1];
-                const uint32_t* r2 = (const uint32_t*)&w[u][2];
-                const uint32_t* r3 = (const uint32_t*)&w[u][3];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t f[4] = {__byte_perm(r0[i], r1[i], 0x5410), __byte_perm(r0[i], r1[i], 0x7632),
-                                           __byte_perm(r2[i], r3[i], 0x5410), __byte_perm(r2[i], r3[i], 0x7632)};
-#pragma unroll
-                    for (int q = 0; q < G; ++q) mma16(c[q][i], f, x[u][q].x, x[u][q].y);
-                }
+                multiply_bf16<1>(c, w[u], &x[u]);
             }
         }
     } else {
-        const uint32_t Kp = (uint32_t)((K + kQ - 1) / kQ * kQ);
-        // (columns past the matrix are its last one again, whose sums nobody takes; k past the matrix meets its zero padding)
-        const uint8_t* w0 = (const uint8_t*)W + (size_t)min(c0 + g, N - 1) * Kp + 16 * t;
-        const int last = max(N - 1 - c0 - g, 0);
-        struct Unit { uint4 w[8], x[G == 4 ? 1 : G][2]; float s; };     // (32 tokens: their values only when it is their turn)
-        auto load_x = [&](uint4* v, int q, int kk) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                v[h] = *(const uint4*)(A + (size_t)min(8 * q + g, Tn - 1) * ld + min(kk + 16 * t + 8 * h, K - 8));
-            }
-        };
+        const Fp8Columns cols(W, c0, N, K);
+        struct Unit { uint4 w[8], x[2]; float s; };
         auto load = [&](Unit& v, int kk) {
+            cols.load(v.w, kk);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v.w[j] = ld_stream16(w0 + kk + (size_t)(uint32_t)min(8 * j, last) * Kp);
-            if constexpr (G < 4) {
-#pragma unroll
-                for (int q = 0; q < G; ++q) load_x(v.x[q], q, kk);
-            }
+            for (int h = 0; h < 2; ++h) v.x[h] = *(const uint4*)(mine + min(kk + 16 * t + 8 * h, K - 8));
             v.s = __ldg(scale + kk / kQ);
         };
-        auto multiply = [&](Unit& n, int kk) {
-            // A token's 64 values as half: times a power of two that brings the largest of them to [2^14, 2^15), exact but for what lies
-            // 2^-29 below it (an error of 2^-40 of the largest, where the float32 sums have 2^-24); the power goes back in with the block's scale
-            constexpr int GG = G == 4 ? 1 : G;         // token groups at a time
-#pragma unroll
-            for (int q0 = 0; q0 < G; q0 += GG) {
-                if constexpr (G == 4) load_x(n.x[0], q0, kk);
-                float back[GG][2];                     // of tokens 2 t and 2 t + 1
-#pragma unroll
-                for (int q = 0; q < GG; ++q) {
-                    uint32_t* v = (uint32_t*)&n.x[q][0];
-                    uint32_t top = 0;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) top = __vmaxu2(top, v[i] & 0x7fff7fffu);
-                    top = max(top >> 16, top & 0xffffu) << 16;          // float bits of the largest magnitude
-                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                    // (a token with an infinity or NaN keeps it: half has both.  Factors within the floats' normal range.)
-                    const uint32_t e = min(max(top >> 23, 16u), 254u);
-                    const float f = __uint_as_float((268u - e) << 23);  // 2^(14 - (e - 127))
-                    const float r = n.s * __uint_as_float((e - 14u) << 23);
-                    back[q][0] = __shfl_sync(0xffffffffu, r, 8 * t);
-                    back[q][1] = __shfl_sync(0xffffffffu, r, 8 * t + 4);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const __half2 p = __floats2half2_rn(__uint_as_float(v[i] << 16) * f, __uint_as_float(v[i] & 0xffff0000u) * f);
-                        v[i] = *reinterpret_cast<const uint32_t*>(&p);
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t* wa = (const uint32_t*)&n.w[2 * i];
-                    const uint32_t* wb = (const uint32_t*)&n.w[2 * i + 1];
-                    float p[GG][4] = {};
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {      // k = 16 t + 4 k .. + 3
-                        uint32_t f[4];
-                        halves_of_e4m3(wa[k], f[0], f[2]);
-                        halves_of_e4m3(wb[k], f[1], f[3]);
-#pragma unroll
-                        for (int q = 0; q < GG; ++q) {
-                            const uint32_t* xv = (const uint32_t*)&n.x[q][0];
-                            mma16_half(p[q], f, xv[2 * k], xv[2 * k + 1]);
-                        }
-                    }
-#pragma unroll
-                    for (int q = 0; q < GG; ++q)
-#pragma unroll
-                        for (int v = 0; v < 4; ++v) c[q0 + q][i][v] = fmaf(back[q][v & 1], p[q][v], c[q0 + q][i][v]);
-                }
-            }
+        auto multiply = [&](Unit& n) {
+            uint32_t* v = (uint32_t*)&n.x[0];
+            const float r = n.s * to_half64(v);
+            const float back[1][2] = {{__shfl_sync(0xffffffffu, r, 8 * t), __shfl_sync(0xffffffffu, r, 8 * t + 4)}};
+            multiply_fp8<1>(c, n.w, [&](int, int k) { return make_uint2(v[2 * k], v[2 * k + 1]); }, back);
         };
         // (cuts are multiples of 64) a unit's loads are on their way while the one before it is multiplied
-        if (k0 >= k1) return;
         Unit u0, u1;
         load(u0, k0);
         for (int kk = k0; kk < k1; kk += 128) {
             if (kk + 64 < k1) load(u1, kk + 64);
-            multiply(u0, kk);
+            multiply(u0);
             if (kk + 64 >= k1) break;
             if (kk + 128 < k1) load(u0, kk + 128);
-            multiply(u1, kk + 64);
+            multiply(u1);
+        }
+    }
+}
+
+// The staged form, by the whole CTA: 128 of the contraction at a time.  `hold` / `put`: a thread's share of the activations, first to
+// registers (while the 128 before them are multiplied), then to shared memory.
+template <int WT, int G> struct Staged {
+    using T = typename Elem<WT>::T;
+    using Sh = Shape<WT, G>;
+    static constexpr int VECS = WT == kF32 ? 4 : 2;            // 16 values of one token
+    uint4 v[VECS];
+    __device__ __forceinline__ void hold(const T* A, int ld, int Tn, int K, int k0) {
+        const int tok = threadIdx.x >> 3, kx = k0 + 16 * (threadIdx.x & 7);
+#pragma unroll
+        for (int i = 0; i < VECS; ++i) {
+            const int k = kx + i * (16 / VECS);
+            v[i] = make_uint4(0, 0, 0, 0);
+            if (tok < Tn && k < K) v[i] = *(const uint4*)(A + (size_t)tok * ld + k);
+        }
+    }
+    __device__ __forceinline__ void put(uint8_t* buf) {
+        const int tok = threadIdx.x >> 3, part = threadIdx.x & 7;
+        if constexpr (WT == kF32) {
+            if (tok < 8 * G) {
+                const float* f = (const float*)v;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) *(float*)(buf + (16 * part + i) * Sh::PITCH + 4 * tok) = f[i];
+            }
+        } else {
+            float back = 0.f;
+            if constexpr (WT == kFp8) back = to_half64((uint32_t*)v);
+            if (tok < 8 * G) {
+                *(uint4*)(buf + tok * Sh::PITCH + 32 * part) = v[0];
+                *(uint4*)(buf + tok * Sh::PITCH + 32 * part + 16) = v[1];
+                if (WT == kFp8 && (part & 3) == 0) ((float*)(buf + Sh::STAGE))[(part >> 2) * 8 * G + tok] = back;
+            }
+        }
+    }
+};
+
+// c += A[rows, k0 .. k1) W[k0 .. k1, the warp's 64 columns from c0 on] (k0 a multiple of 128; every warp takes its part of every 128).  buf: two
+// stages.  All threads of the CTA call it with the same k0, k1.  float32: c is [8 G tokens][4 columns 4 (lane % 16) ..] of every other k.
+template <int WT, int G, typename C>
+__device__ __forceinline__ void accumulate_staged(C& c, const typename Elem<WT>::T* A, int ld, int Tn, const void* W, const float* scale, int c0, int N, int K,
+                                                  int k0, int k1, uint8_t* buf) {
+    using Sh = Shape<WT, G>;
+    constexpr int SZ = Sh::STAGE + Sh::BACK;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const int part = warp / (Sh::COLS / kCols);                // of every 128
+    Staged<WT, G> st;
+    if (k0 >= k1) return;
+    st.hold(A, ld, Tn, K, k0);
+    __syncthreads();                                           // whoever still reads the stages of an earlier call
+    st.put(buf);
+    __syncthreads();
+    int b = 0;
+    auto next = [&](int kk) {                                  // activations of the next 128, behind the work on this one
+        b ^= 1;
+        if (kk + 128 < k1) st.put(buf + b * SZ);
+        __syncthreads();
+    };
+    if constexpr (WT == kFp8) {
+        const Fp8Columns cols(W, c0, N, K);
+        uint4 w[2][8];
+        float s[2];
+        cols.load(w[0], k0 + 64 * part);
+        s[0] = __ldg(scale + k0 / kQ);
+#pragma unroll 2
+        for (int kk = k0, u = 0; kk < k1; kk += 128, u ^= 1) {
+            if (kk + 128 < k1) {
+                st.hold(A, ld, Tn, K, kk + 128);
+                cols.load(w[u ^ 1], kk + 128 + 64 * part);
+                s[u ^ 1] = __ldg(scale + (kk + 128) / kQ);
+            }
+            const uint8_t* x = buf + b * SZ + g * Sh::PITCH + 128 * part + 32 * t;
+            const float* bk = (const float*)(buf + b * SZ + Sh::STAGE) + part * 8 * G + 2 * t;
+            float back[G][2];
+#pragma unroll
+            for (int q = 0; q < G; ++q) { back[q][0] = s[u] * bk[8 * q]; back[q][1] = s[u] * bk[8 * q + 1]; }
+            multiply_fp8<G>(c, w[u], [&](int q, int k) { return *(const uint2*)(x + q * 8 * Sh::PITCH + 8 * k); }, back);
+            next(kk);
+        }
+    } else if constexpr (WT == kBf16) {
+        const __nv_bfloat16* w0 = (const __nv_bfloat16*)W + min(c0 + 8 * g, N - 8);
+        uint4 w[2][2][4];                                      // two steps of 16 at a time, the next two on their way
+        auto load = [&](uint4 (*v)[4], int k) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[h][r] = ld_stream16(w0 + (size_t)min(k + 16 * h + 4 * t + r, K - 1) * N);
+        };
+        load(w[0], k0 + 64 * part);
+        for (int kk = k0; kk < k1; kk += 128) {
+            const bool more = kk + 128 < k1;
+            if (more) st.hold(A, ld, Tn, K, kk + 128);
+            const uint8_t* x = buf + b * SZ + g * Sh::PITCH + 128 * part + 8 * t;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if (u == 0) load(w[1], kk + 64 * part + 32);
+                else if (more) load(w[0], kk + 128 + 64 * part);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint2 v[G];
+#pragma unroll
+                    for (int q = 0; q < G; ++q) v[q] = *(const uint2*)(x + q * 8 * Sh::PITCH + 64 * u + 32 * h);
+                    multiply_bf16<G>(c, w[u][h], v);
+                }
+            }
+            next(kk);
+        }
+    } else {
+        const int h = lane >> 4;
+        const float* w0 = (const float*)W + min(c0 + 4 * (lane & 15), N - 4);
+        uint4 w[2][8];                                         // rows h, h + 2, .. of the warp's 16
+        auto load = [&](uint4* v, int kk) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = ld_stream16(w0 + (size_t)min(kk + 16 * part + 2 * i + h, K - 1) * N);
+        };
+        load(w[0], k0);
+#pragma unroll 2
+        for (int kk = k0, u = 0; kk < k1; kk += 128, u ^= 1) {
+            if (kk + 128 < k1) {
+                st.hold(A, ld, Tn, K, kk + 128);
+                load(w[u ^ 1], kk + 128);
+            }
+            const uint8_t* x = buf + b * SZ + (16 * part + h) * Sh::PITCH;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float wf[4] = {__uint_as_float(w[u][i].x), __uint_as_float(w[u][i].y), __uint_as_float(w[u][i].z), __uint_as_float(w[u][i].w)};
+#pragma unroll
+                for (int q = 0; q < 2 * G; ++q) {
+                    const float4 xv = *(const float4*)(x + 2 * i * Sh::PITCH + 16 * q);
+                    const float xf[4] = {xv.x, xv.y, xv.z, xv.w};
+#pragma unroll
+                    for (int m = 0; m < 4; ++m)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) c[4 * q + m][v] = fmaf(xf[m], wf[v], c[4 * q + m][v]);
+                }
+            }
+            next(kk);
         }
     }
 }
@@ -330,74 +496,69 @@ __device__ __forceinline__ int col_of(int i, int v, int g) {
 }
 __device__ __forceinline__ int token_of_sum(int q, int v, int t) { return 8 * q + 2 * t + (v & 1); }
 
-// float32: a half warp takes every other row of W, a lane four columns; eight tokens per pass over the weights.  Adds weight(tok) times the
-// product to red[tok][col] of this warp (first: sets it).
-template <typename Weight>
-__device__ void accumulate_f32(float* red, const float* A, int ld, int Tn, const float* W, int c0, int N, int k0, int k1, bool first, Weight weight) {
-    const int lane = threadIdx.x & 31, h = lane >> 4, col = 4 * (lane & 15);
-    const bool col_ok = c0 + col < N;
-    for (int tb = 0; tb < Tn; tb += 8) {
-        float4 s[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s[i] = make_float4(0, 0, 0, 0);
-#pragma unroll 4
-        for (int kk = k0 + h; kk < k1; kk += 2) {
-            const uint4 v = col_ok ? ld_stream16(W + (size_t)kk * N + c0 + col) : make_uint4(0, 0, 0, 0);
-            const float4 w = make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float q = tb + i < Tn ? A[(size_t)(tb + i) * ld + kk] : 0.f;
-                s[i].x = fmaf(q, w.x, s[i].x); s[i].y = fmaf(q, w.y, s[i].y); s[i].z = fmaf(q, w.z, s[i].z); s[i].w = fmaf(q, w.w, s[i].w);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (tb + i >= Tn) break;
-            float f[4] = {s[i].x, s[i].y, s[i].z, s[i].w};
-#pragma unroll
-            for (int u = 0; u < 4; ++u) f[u] += __shfl_xor_sync(0xffffffffu, f[u], 16);
-            float wt;
-            const bool on = weight(tb + i, wt);
-            if (h == 0) {
-                float* o = red + (tb + i) * kCols + col;
-#pragma unroll
-                for (int u = 0; u < 4; ++u) o[u] = (first ? 0.f : o[u]) + (on ? wt * f[u] : 0.f);
-            }
-        }
-    }
-}
-
 // Cut of `units` pieces of work among `workers`: worker w's [lo, hi).
 __device__ __forceinline__ void cut(int units, int workers, int w, int& lo, int& hi) {
     lo = (int)((long long)units * w / workers);
     hi = (int)((long long)units * (w + 1) / workers);
 }
-template <int WT> __host__ __device__ constexpr int unit_len() { return WT == kFp8 ? 64 : 16; }
-
-struct Smem {                       // dynamic shared memory, sizes in floats
-    float *red, *cta, *part;
+template <int WT, int G> struct Smem {         // dynamic shared memory
+    using Sh = Shape<WT, G>;
+    float *red, *cta, *part;                   // [PARTS][Tn][COLS] (the router's partial sums fit as well: n <= 32), [Tn][COLS], [Tn][n]
     Routed* R;
+    uint8_t* stage;
     __device__ Smem(uint8_t* base, int Tn, int n) {
         red = (float*)base;
-        cta = red + kWarps * Tn * kCols;               // (n <= 32: the router's partial sums fit as well)
-        part = cta + Tn * kCols;
-        R = (Routed*)(part + Tn * n);
+        cta = red + kWarps * Tn * kCols;
+        stage = (uint8_t*)(cta + Tn * Sh::COLS);
+        R = (Routed*)(stage + (Sh::STAGED ? 2 * (Sh::STAGE + Sh::BACK) : 0));
+        part = (float*)(R + 1);
     }
-    static size_t bytes(int Tn, int n) { return sizeof(float) * ((size_t)(kWarps + 1) * Tn * kCols + (size_t)Tn * n) + sizeof(Routed); }
+    static size_t bytes(int Tn, int n) {
+        return sizeof(float) * ((size_t)kWarps * Tn * kCols + Tn * Sh::COLS + (size_t)Tn * n) + (Sh::STAGED ? 2 * (Sh::STAGE + Sh::BACK) : 0) + sizeof(Routed);
+    }
 };
 
-// This CTA's sums of a tile (its warps' parts added in order) into its buffer `cta`, visible to the CTAs that share the tile.
-__device__ __forceinline__ void meet(const float* red, float* cta, int Tn, int S) {
+// This CTA's sums of a tile (its parts' added in order) into its buffer `cta`, visible to the CTAs that share the tile.
+template <int PARTS>
+__device__ __forceinline__ void meet(const float* red, float* cta, int size, int S) {
     __syncthreads();
-    for (int q = threadIdx.x; q < Tn * kCols; q += kThreads) {
+    for (int q = threadIdx.x; q < size; q += kThreads) {
         float s = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) s += red[w * Tn * kCols + q];
+        for (int w = 0; w < PARTS; ++w) s += red[w * size + q];
         cta[q] = s;
     }
     if (S > 1) cluster_sync_all();
     else __syncthreads();
 }
+
+// A warp's sums to its part of `red` ([Tn][COLS], this warp's 64 columns).
+template <int WT, int G, typename C>
+__device__ __forceinline__ void put_sums(float* red, int Tn, C& c) {
+    constexpr int COLS = Shape<WT, G>::COLS;
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    if constexpr (WT == kF32) {
+#pragma unroll
+        for (int m = 0; m < 8 * G; ++m) {
+            float4 f;
+            f.x = c[m][0] + __shfl_xor_sync(0xffffffffu, c[m][0], 16);
+            f.y = c[m][1] + __shfl_xor_sync(0xffffffffu, c[m][1], 16);
+            f.z = c[m][2] + __shfl_xor_sync(0xffffffffu, c[m][2], 16);
+            f.w = c[m][3] + __shfl_xor_sync(0xffffffffu, c[m][3], 16);
+            if (m < Tn && lane < 16) *(float4*)(red + m * COLS + 4 * lane) = f;
+        }
+    } else {
+#pragma unroll
+        for (int q = 0; q < G; ++q)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+                    if (token_of_sum(q, v, t) < Tn) red[token_of_sum(q, v, t) * COLS + col_of<WT>(i, v, g)] = c[q][i][v];
+    }
+}
+template <int WT, int G> struct Sums { float c[G][4][4]; };
+template <int G> struct Sums<kF32, G> { float c[8 * G][4]; };
 
 template <int WT>
 __device__ __forceinline__ size_t matrix_bytes(int K, int N) {
@@ -405,25 +566,19 @@ __device__ __forceinline__ size_t matrix_bytes(int K, int N) {
 }
 
 template <int WT, int G>
-__global__ void __launch_bounds__(kThreads, G == 1 ? 2 : 1)
+__global__ void __launch_bounds__(kThreads, Shape<WT, G>::CTAS)
 first_layer_kernel(const TokArgs a, int S) {
     using T = typename Elem<WT>::T;
+    using Sh = Shape<WT, G>;
+    constexpr int COLS = Sh::COLS;
     extern __shared__ __align__(16) uint8_t smem_raw[];
-    const int rank = (int)cluster_ctarank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int rank = (int)cluster_ctarank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int t0 = blockIdx.z * kTok, Tn = min(kTok, a.T - t0);
-    Smem sm(smem_raw, Tn, a.n);
+    const Smem<WT, G> sm(smem_raw, Tn, a.n);
     pdl_trigger();
     pdl_wait();
     route_tokens<WT, (G + 1) / 2>(a, t0, Tn, rank, sm.red, sm.part, *sm.R);
     const Routed& R = *sm.R;
-    const int tiles_n = (a.d_e + kCols - 1) / kCols, tiles = __popc(R.any) * tiles_n;
-    const int tile = blockIdx.x / S, kr = rank % S, first = rank - kr;        // this CTA's tile, its place among the tile's CTAs, the first of them
-    const bool live = tile < tiles;
-    const int slot = live ? tile / tiles_n : 0, c0 = (tile - slot * tiles_n) * kCols, e = nth_bit(R.any, slot);
-    int lo, hi;
-    cut((a.d + unit_len<WT>() - 1) / unit_len<WT>(), S * kWarps, kr * kWarps + warp, lo, hi);
-    const int k0 = lo * unit_len<WT>(), k1 = min(a.d, hi * unit_len<WT>());
-    const void* W = (const uint8_t*)a.W1 + (size_t)e * matrix_bytes<WT>(a.d, a.d_e);
     if (blockIdx.x == 0)
         for (int q = threadIdx.x; q < (int)(sizeof(Routed) / 4); q += kThreads) ((uint32_t*)(a.routed + blockIdx.z))[q] = ((const uint32_t*)sm.R)[q];
     if (blockIdx.x == 0 && a.r.expert_idx) {
@@ -439,30 +594,33 @@ first_layer_kernel(const TokArgs a, int S) {
             }
         }
     }
+    const int tiles_n = (a.d_e + COLS - 1) / COLS;
+    const int tile = blockIdx.x / S, kr = rank % S, first = rank - kr;        // this CTA's tile, its place among the tile's CTAs, the first of them
+    const bool live = tile < __popc(R.any) * tiles_n;
+    const int slot = live ? tile / tiles_n : 0, c0 = (tile - slot * tiles_n) * COLS, e = nth_bit(R.any, slot);
     const T* x = (const T*)a.x + (size_t)t0 * a.d;
     T* out = (T*)a.a + (size_t)blockIdx.z * a.n * kTok * a.d_e;
-    float* red = sm.red + warp * Tn * kCols;
     if (live) {
-        if constexpr (WT == kF32) {
-            accumulate_f32(red, (const float*)x, a.d, Tn, (const float*)W, c0, a.d_e, k0, k1, true, [](int, float& w) { w = 1.f; return true; });
+        const void* W = (const uint8_t*)a.W1 + (size_t)e * matrix_bytes<WT>(a.d, a.d_e);
+        const int c1 = c0 + warp * kCols % COLS;              // this warp's columns
+        const float* sc = WT == kFp8 ? a.s1 + ((size_t)e * ((a.d_e + kQ - 1) / kQ) + min(c1, a.d_e - 1) / kQ) * ((a.d + kQ - 1) / kQ) : nullptr;
+        Sums<WT, G> s = {};
+        int lo, hi;
+        const int units = (a.d + Sh::UNIT - 1) / Sh::UNIT;
+        if constexpr (Sh::STAGED) {
+            cut(units, S, kr, lo, hi);
+            accumulate_staged<WT, G>(s.c, x, a.d, Tn, W, sc, c1, a.d_e, a.d, lo * Sh::UNIT, min(a.d, hi * Sh::UNIT), sm.stage);
         } else {
-            float c[G][4][4] = {};
-            const float* sc = WT == kFp8 ? a.s1 + ((size_t)e * ((a.d_e + kQ - 1) / kQ) + c0 / kQ) * ((a.d + kQ - 1) / kQ) : nullptr;
-            accumulate<WT, G>(c, (const __nv_bfloat16*)x, a.d, Tn, W, sc, c0, a.d_e, a.d, k0, k1);
-#pragma unroll
-            for (int q = 0; q < G; ++q)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int v = 0; v < 4; ++v)
-                        if (token_of_sum(q, v, t) < Tn) red[token_of_sum(q, v, t) * kCols + col_of<WT>(i, v, g)] = c[q][i][v];
+            cut(units, S * kWarps, kr * kWarps + warp, lo, hi);
+            accumulate<WT>(s.c, x, a.d, Tn, W, sc, c1, a.d_e, a.d, lo * Sh::UNIT, min(a.d, hi * Sh::UNIT));
         }
+        put_sums<WT, G>(sm.red + warp / (COLS / kCols) * Tn * COLS + warp * kCols % COLS, Tn, s.c);
     }
     cluster_wait();
-    meet(sm.red, sm.cta, Tn, S);
+    meet<Sh::PARTS>(sm.red, sm.cta, Tn * COLS, S);
     if (live) {
-        for (int q = kr * kThreads + threadIdx.x; q < Tn * kCols; q += S * kThreads) {
-            const int tok = q / kCols, col = c0 + q % kCols;
+        for (int q = kr * kThreads + threadIdx.x; q < Tn * COLS; q += S * kThreads) {
+            const int tok = q / COLS, col = c0 + q % COLS;
             if (col >= a.d_e || !((R.mask[tok] >> e) & 1)) continue;
             float h = 0.f;
             for (int s = 0; s < S; ++s) h += ld_cluster(sm.cta + q, first + s);
@@ -475,25 +633,20 @@ first_layer_kernel(const TokArgs a, int S) {
 }
 
 template <int WT, int G>
-__global__ void __launch_bounds__(kThreads, G == 1 ? 2 : 1)
+__global__ void __launch_bounds__(kThreads, Shape<WT, G>::CTAS)
 second_layer_kernel(const TokArgs a, int S) {
     using T = typename Elem<WT>::T;
+    using Sh = Shape<WT, G>;
+    constexpr int COLS = Sh::COLS;
     extern __shared__ __align__(16) uint8_t smem_raw[];
-    const int rank = (int)cluster_ctarank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int rank = (int)cluster_ctarank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = lane & 3;
     const int t0 = blockIdx.z * kTok, Tn = min(kTok, a.T - t0);
-    Smem sm(smem_raw, Tn, a.n);
+    const Smem<WT, G> sm(smem_raw, Tn, a.n);
     pdl_trigger();
     pdl_wait();
     for (int q = threadIdx.x; q < (int)(sizeof(Routed) / 4); q += kThreads) ((uint32_t*)sm.R)[q] = __ldcg((const uint32_t*)(a.routed + blockIdx.z) + q);
     __syncthreads();
     const Routed& R = *sm.R;
-    const int c0 = blockIdx.x / S * kCols, kr = rank % S, first = rank - kr;
-    const bool live = c0 < a.d;                        // (the grid is whole clusters)
-    constexpr int UL = unit_len<WT>();
-    const int per = (a.d_e + UL - 1) / UL;             // units of one expert
-    int lo, hi;
-    cut(live ? __popc(R.any) * per : 0, S * kWarps, kr * kWarps + warp, lo, hi);
-    auto weights = [&](int e) { return (const void*)((const uint8_t*)a.W2 + (size_t)e * matrix_bytes<WT>(a.d_e, a.d)); };
     if (blockIdx.x == 0 && blockIdx.z == 0 && warp == 0 && a.r.expert_offsets) {      // Eq. 23, from every group's choices
         int cnt = 0;
         for (int q0 = 0; q0 < a.T * a.k; q0 += 32) {
@@ -510,30 +663,39 @@ second_layer_kernel(const TokArgs a, int S) {
         if (lane < a.n) a.r.expert_offsets[lane + 1] = incl;
         if (lane == 0) a.r.expert_offsets[0] = 0;
     }
+    const int c0 = blockIdx.x / S * COLS, kr = rank % S, first = rank - kr, c1 = c0 + warp * kCols % COLS;
+    const bool live = c0 < a.d;                        // (the grid is whole clusters)
+    const int per = (a.d_e + Sh::UNIT - 1) / Sh::UNIT; // units of one expert
+    int lo, hi;
+    if constexpr (Sh::STAGED) cut(live ? __popc(R.any) * per : 0, S, kr, lo, hi);
+    else cut(live ? __popc(R.any) * per : 0, S * kWarps, kr * kWarps + warp, lo, hi);
     const T* hid = (const T*)a.a + (size_t)blockIdx.z * a.n * kTok * a.d_e;
-    float* red = sm.red + warp * Tn * kCols;
     auto weight = [&](int tok, int e, float& w) {      // combine weight of (token, expert); false: not chosen
         const float p = R.p[tok][e];
         w = a.use_gate ? p * p : 1.f;
         return ((R.mask[tok] >> e) & 1) != 0;
     };
-    if constexpr (WT == kF32) {
-        for (int q = lane; q < Tn * kCols; q += 32) red[q] = 0.f;
-        __syncwarp();
-    }
-    float tot[G][4][4] = {};
+    Sums<WT, G> tot = {};
     for (int u = lo; u < hi;) {
-        const int slot = u / per, k0 = (u - slot * per) * UL, n_u = min(hi - u, per - (u - slot * per)), k1 = min(a.d_e, k0 + n_u * UL);
+        const int slot = u / per, k0 = (u - slot * per) * Sh::UNIT, n_u = min(hi - u, per - (u - slot * per)), k1 = min(a.d_e, k0 + n_u * Sh::UNIT);
         const int e = nth_bit(R.any, slot);
         const T* A = hid + (size_t)slot * kTok * a.d_e;
+        const void* W = (const uint8_t*)a.W2 + (size_t)e * matrix_bytes<WT>(a.d_e, a.d);
+        const float* sc = WT == kFp8 ? a.s2 + ((size_t)e * ((a.d + kQ - 1) / kQ) + min(c1, a.d - 1) / kQ) * ((a.d_e + kQ - 1) / kQ) : nullptr;
+        Sums<WT, G> s = {};
+        if constexpr (Sh::STAGED) accumulate_staged<WT, G>(s.c, A, a.d_e, Tn, W, sc, c1, a.d, a.d_e, k0, k1, sm.stage);
+        else accumulate<WT>(s.c, A, a.d_e, Tn, W, sc, c1, a.d, a.d_e, k0, k1);
+        // the tokens that chose this expert take its sums (the hidden rows of the others were never written)
         if constexpr (WT == kF32) {
-            accumulate_f32(red, (const float*)A, a.d_e, Tn, (const float*)weights(e), c0, a.d, k0, k1, false,
-                           [&](int tok, float& w) { return weight(tok, e, w); });
+#pragma unroll
+            for (int m = 0; m < 8 * G; ++m) {
+                float w = 0.f;
+                if (m < Tn && weight(m, e, w)) {
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) tot.c[m][v] = fmaf(w, s.c[m][v], tot.c[m][v]);
+                }
+            }
         } else {
-            float c[G][4][4] = {};
-            const float* sc = WT == kFp8 ? a.s2 + ((size_t)e * ((a.d + kQ - 1) / kQ) + c0 / kQ) * ((a.d_e + kQ - 1) / kQ) : nullptr;
-            accumulate<WT, G>(c, (const __nv_bfloat16*)A, a.d_e, Tn, weights(e), sc, c0, a.d, a.d_e, k0, k1);
-            // the tokens that chose this expert take its sums (the hidden rows of the others were never written)
 #pragma unroll
             for (int q = 0; q < G; ++q)
 #pragma unroll
@@ -543,26 +705,18 @@ second_layer_kernel(const TokArgs a, int S) {
                     if (tok < Tn && weight(tok, e, w)) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            tot[q][i][h] = fmaf(w, c[q][i][h], tot[q][i][h]);
-                            tot[q][i][2 + h] = fmaf(w, c[q][i][2 + h], tot[q][i][2 + h]);
+                            tot.c[q][i][h] = fmaf(w, s.c[q][i][h], tot.c[q][i][h]);
+                            tot.c[q][i][2 + h] = fmaf(w, s.c[q][i][2 + h], tot.c[q][i][2 + h]);
                         }
                     }
                 }
         }
         u += n_u;
     }
-    if constexpr (WT != kF32) {
-#pragma unroll
-        for (int q = 0; q < G; ++q)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int v = 0; v < 4; ++v)
-                    if (token_of_sum(q, v, t) < Tn) red[token_of_sum(q, v, t) * kCols + col_of<WT>(i, v, g)] = tot[q][i][v];
-    }
-    meet(sm.red, sm.cta, Tn, S);
-    for (int q = kr * kThreads + threadIdx.x; q < Tn * kCols; q += S * kThreads) {
-        const int tok = q / kCols, col = c0 + q % kCols;
+    put_sums<WT, G>(sm.red + warp / (COLS / kCols) * Tn * COLS + warp * kCols % COLS, Tn, tot.c);
+    meet<Sh::PARTS>(sm.red, sm.cta, Tn * COLS, S);
+    for (int q = kr * kThreads + threadIdx.x; q < Tn * COLS; q += S * kThreads) {
+        const int tok = q / COLS, col = c0 + q % COLS;
         if (col >= a.d) continue;
         float s = 0.f;
         for (int r = 0; r < S; ++r) s += ld_cluster(sm.cta + q, first + r);
@@ -602,10 +756,11 @@ cudaError_t launch_clusters(void (*kern)(KArgs...), dim3 grid, size_t smem, cuda
 
 constexpr int kMaxSmem = 160 * 1024;
 
-// CTAs of a tile: the largest split that leaves every warp a unit of the contraction and no more than two CTAs per SM.
-int split_of(int units, long long tiles) {
+// CTAs of a tile: the largest split that leaves every worker (a warp, or the CTA where it works together) a unit of the contraction and no
+// more CTAs than the SMs hold.
+int split_of(int units, int workers, long long tiles, int ctas) {
     int S = kCluster;
-    while (S > 1 && (units < S * kWarps || tiles * S > 2ll * sm_count())) S >>= 1;
+    while (S > 1 && (units < S * workers || tiles * S > (long long)ctas * sm_count())) S >>= 1;
     return S;
 }
 
@@ -616,21 +771,23 @@ uoe_status launch_layers(const TokArgs& a, cudaStream_t s) {
     if (st == UOE_OK) st = smem_opt_in(once2, second_layer_kernel<WT, G>, kMaxSmem);
     if (st != UOE_OK) return st;
     const int groups = (a.T + kTok - 1) / kTok, Tn = a.T < kTok ? a.T : kTok;
-    constexpr int UL = unit_len<WT>();
+    using Sh = Shape<WT, G>;
+    constexpr int workers = Sh::STAGED ? 1 : kWarps;
     const long long chosen = a.n < (long long)Tn * a.k ? a.n : (long long)Tn * a.k;      // experts at most
     auto grid = [&](long long tiles, int S) { return dim3((unsigned)((tiles * S + kCluster - 1) / kCluster * kCluster), 1, groups); };
+    const size_t smem = Smem<WT, G>::bytes(Tn, a.n);
     {
-        const long long tiles = chosen * ((a.d_e + kCols - 1) / kCols);
-        const int S = split_of((a.d + UL - 1) / UL, tiles * groups);
+        const long long tiles = chosen * ((a.d_e + Sh::COLS - 1) / Sh::COLS);
+        const int S = split_of((a.d + Sh::UNIT - 1) / Sh::UNIT, workers, tiles * groups, Sh::CTAS);
         ProfScope ps("tokens_first", s);
-        launch_clusters(first_layer_kernel<WT, G>, grid(tiles, S), Smem::bytes(Tn, a.n), s, a, S);
+        launch_clusters(first_layer_kernel<WT, G>, grid(tiles, S), smem, s, a, S);
         UOE_LAUNCHED();
     }
     {
-        const long long tiles = (a.d + kCols - 1) / kCols;
-        const int S = split_of((int)(a.k * ((a.d_e + UL - 1) / UL)), tiles * groups);
+        const long long tiles = (a.d + Sh::COLS - 1) / Sh::COLS;
+        const int S = split_of((int)(a.k * ((a.d_e + Sh::UNIT - 1) / Sh::UNIT)), workers, tiles * groups, Sh::CTAS);
         ProfScope ps("tokens_second", s);
-        launch_clusters(second_layer_kernel<WT, G>, grid(tiles, S), Smem::bytes(Tn, a.n), s, a, S);
+        launch_clusters(second_layer_kernel<WT, G>, grid(tiles, S), smem, s, a, S);
         UOE_LAUNCHED();
     }
     return UOE_OK;
