@@ -45,7 +45,6 @@ static_assert(sizeof(Ctl) <= 1024, "control block");
 template <int BN, bool WGRAD, int EPI>
 __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
 fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ Fp8Args a) {
-    pdl_trigger();
     using Cf = Cfg<BN>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -62,8 +61,10 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         prefetch_tmap(&tmA);
         prefetch_tmap(&tmB);
     }
-    if (warp == 1) tmem_alloc(&ctl->tmem_base, Cf::TMEM_COLS);
     pdl_wait();
+    // (TMEM only when the grids before this one are complete, and the grid behind it only when it is taken: no CTA holds TMEM while it waits
+    // for one that still needs some)
+    if (warp == 1) tmem_alloc(&ctl->tmem_base, Cf::TMEM_COLS);
     // tiles of the rows: per expert its 128-row blocks; without offsets all rows are one expert's; wgrad: every expert has all of C
     const int m_tiles = (int)((a.M + BM - 1) / BM);
     if (warp == 2) {
@@ -72,6 +73,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    pdl_trigger();
     const uint32_t tmem_base = ctl->tmem_base;
     float* s_scales = (float*)((uint8_t*)ctl + Cf::CTL_BYTES);
     const int n_tiles = (a.N + BN - 1) / BN;

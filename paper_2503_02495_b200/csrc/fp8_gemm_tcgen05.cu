@@ -59,7 +59,6 @@ __device__ __forceinline__ uint32_t exponent_word(float s, bool there, bool& bad
 template <int BN, bool WGRAD, int EPI, bool PAIR>
 __global__ void __launch_bounds__(Cfg<BN, PAIR>::THREADS, 1)
 fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ Fp8Args a) {
-    pdl_trigger();
     using Cf = Cfg<BN, PAIR>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -79,17 +78,20 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         prefetch_tmap(&tmA);
         prefetch_tmap(&tmB);
     }
+    pdl_wait();
+    // (TMEM only when the grids before this one are complete, and the grid behind it only when it is taken: no CTA holds TMEM while it waits
+    // for one that still needs some)
     if (warp == 1) {
         if constexpr (PAIR) tmem_alloc_pair(&ctl->tmem_base, Cf::TMEM_COLS);
         else tmem_alloc(&ctl->tmem_base, Cf::TMEM_COLS);
     }
-    pdl_wait();
     const int m_tiles = (int)((a.M + Cf::TILE - 1) / Cf::TILE);
     if (warp == 2) load_regions<WGRAD, Cf::TILE>(ctl->reg, a, m_tiles, lane);
     tc_fence_before();
     __syncthreads();
     if constexpr (PAIR) cluster_sync_all();           // the other CTA's barriers exist before anything arrives on them
     tc_fence_after();
+    pdl_trigger();
     const uint32_t tmem_base = ctl->tmem_base;
     uint8_t* s_sf = (uint8_t*)ctl + 1024;
     const int n_tiles = (a.N + BN - 1) / BN;
