@@ -26,6 +26,7 @@ struct TokArgs {
     const float *s1, *s2;
     Routed* routed;                 // [groups]: what the first kernel's router says, for the second
     void *a, *y;                    // a [groups, n, group, d_e]: hidden rows by place in the group's list of chosen experts
+    float* af;                      // 8-bit: a is [n, 2 terms, group, d_e padded] bytes, af their scales [n, d_e / 128, group]
     RoutingPtrs r;                  // all null, or all to be written
     int T, d, d_e, n, k, act, use_gate, residual;
     int group;                      // tokens of a z slice of the grid

@@ -18,7 +18,7 @@
 // columns of one MMA.  A stage is one block of the weights' scales, so its product, times one number per token, is added to float32
 // registers by the write-out warps; the weights' scales may be any numbers.
 //   warp 0       TMA producer         warp 1       MMA issuer
-//   warps 4..7   sums: one column per thread, all tokens            warps 8..11  8-bit: the tokens' values of the stages to come
+//   warps 4..7   sums: one column per thread, all tokens            warps 8..     8-bit, first kernel: the tokens' values of the stages to come
 #include "tmap.cuh"
 #include "tokens.cuh"
 
@@ -38,7 +38,8 @@ template <int WT, int NT /* tokens, rounded up */> struct Cfg {
     static constexpr int CTAS = NT <= 32 ? 2 : 1;                         // per SM
     static constexpr int STAGES = CTAS == 1 ? 6 : NT <= 16 ? 5 : 4;
     static constexpr int TMEM_COLS = 2 * N < 32 ? 32 : 2 * N;
-    static constexpr int WARPS = WT == kFp8 ? 12 : 8, THREADS = 32 * WARPS;
+    static constexpr int TEAM = NT / 8, TEAMS = NT == 8 ? 4 : NT == 64 ? 1 : 2;       // 8-bit: a team of warps fills a stage, 8 tokens each
+    static constexpr int WARPS1 = WT == kFp8 ? 8 + TEAM * TEAMS : 8, WARPS2 = 8;      // of the two kernels
     static constexpr int PITCH = kCols + 4;                               // floats of a token's sums in shared memory
     static constexpr int RING = STAGES * STAGE;
 };
@@ -47,7 +48,7 @@ template <int NT> struct Ctl {
     uint64_t full[8], empty[8], tfull[2], tempty[2];
     uint32_t tmem_base;
     int abort_flag;
-    float f[kScaleSlots * NT];          // 8-bit: scales of the tokens' values, by stage
+    alignas(16) float f[kScaleSlots * NT];      // 8-bit: scales of the tokens' values, by stage
     Routed R;
 };
 
@@ -68,12 +69,25 @@ static_assert(Cfg<kBf16, 64>::RING >= 8 * 64 * 32 * 4 && Cfg<kBf16, 16>::RING >=
 // What one CTA multiplies: stages [lo, hi) of a line of `per` stages per expert.
 struct Line { int lo, hi, per, slot0; };
 
+// 128 values, four per lane, as s (hi + lo / 16): returns s.
+__device__ __forceinline__ float two_terms(float a, float b, float c, float d, uint32_t& hi, uint32_t& lo) {
+    const uint32_t m = __reduce_max_sync(0xffffffffu, max(max(abs_bits(a), abs_bits(b)), max(abs_bits(c), abs_bits(d))));
+    const BlockScale k = block_scale(m);
+    hi = e4m3x4(a, b, c, d, k.inv);
+    uint32_t h01, h23;                                 // hi as half pairs
+    halves_of_e4m3(hi, h01, h23);
+    const float2 g0 = __half22float2(*reinterpret_cast<const __half2*>(&h01)), g1 = __half22float2(*reinterpret_cast<const __half2*>(&h23));
+    lo = e4m3x4(fmaf(a, k.inv, -g0.x), fmaf(b, k.inv, -g0.y), fmaf(c, k.inv, -g1.x), fmaf(d, k.inv, -g1.y), k.inv == 0.f ? 0.f : 16.f);
+    return k.s;
+}
+
 // The tile's sums: on return every thread of warps 4..7 holds column 32 (warp % 4) + lane of NT tokens in sum[].
 //   tmW, tmX   the weights [n, ..] (tile column c0); bfloat16: the tokens' values, one matrix [rows, K] per slot (x: one for all)
-//   x, ld      8-bit: the tokens' values, slot_stride elements from slot to slot
+//              8-bit, SECOND: their two terms, [2 n, rows, Kp], and the terms' scales f [n, K / 128, rows]
+//   x, ld      8-bit, first kernel: the tokens' values
 //   weight(tok, e): factor of a token's product with expert e (SECOND: only for the tokens that chose it)
 template <int WT, int NT, bool SECOND, typename Weight>
-__device__ __forceinline__ void run_line(const Smem<WT, NT>& sm, const CUtensorMap* tmW, const CUtensorMap* tmX, const __nv_bfloat16* x, int ld, size_t slot_stride,
+__device__ __forceinline__ void run_line(const Smem<WT, NT>& sm, const CUtensorMap* tmW, const CUtensorMap* tmX, const __nv_bfloat16* x, int ld, const float* f,
                                          const float* scale /* 8-bit: [n][N / 128][K / 128] of this column block */, size_t scale_stride, int c0, int K, int Tn,
                                          const Line& line, int* status, float* sum, Weight weight) {
     using Cf = Cfg<WT, NT>;
@@ -95,9 +109,14 @@ __device__ __forceinline__ void run_line(const Smem<WT, NT>& sm, const CUtensorM
             if (!mbar_wait_warp_quick(&ctl->empty[stage], phase ^ 1, abort_flag, status)) break;
             if (lane == 0) {
                 uint8_t* st = sm.ring + stage * Cf::STAGE;
-                mbar_arrive_expect_tx(&ctl->full[stage], Cf::A_BYTES + (WT == kBf16 ? Cf::B_BYTES : 0));
+                mbar_arrive_expect_tx(&ctl->full[stage], Cf::A_BYTES + (WT == kBf16 || SECOND ? Cf::B_BYTES : 0) + (WT == kFp8 && SECOND ? NT * 4 : 0));
                 if constexpr (WT == kFp8) {
                     tma_load_3d(st, tmW, kb * 128, c0, e, &ctl->full[stage]);
+                    if constexpr (SECOND) {
+                        tma_load_3d(st + Cf::A_BYTES, tmX, kb * 128, 0, 2 * slot, &ctl->full[stage]);
+                        tma_load_3d(st + Cf::A_BYTES + NT * 128, tmX, kb * 128, 0, 2 * slot + 1, &ctl->full[stage]);
+                        bulk_load(ctl->f + (u - line.lo) % kScaleSlots * NT, f + ((size_t)slot * line.per + kb) * kMaxTokens, NT * 4, &ctl->full[stage]);
+                    }
                 } else {
                     tma_load_3d(st, tmW, c0, kb * 64, e, &ctl->full[stage]);
                     tma_load_3d(st + 8192, tmW, c0 + 64, kb * 64, e, &ctl->full[stage]);
@@ -139,52 +158,38 @@ __device__ __forceinline__ void run_line(const Smem<WT, NT>& sm, const CUtensorM
             if (++stage == Cf::STAGES) { stage = 0; phase ^= 1; }
         }
     } else if (warp >= 8) {
-        // warp w: tokens w - 8, w - 4, ..; a lane four of their 128 values
-        constexpr int PER = (NT + 3) / 4;
-        int stage = 0, at = 0;
-        uint32_t phase = 0;
-        uint2 v[PER];
+        // teams take the stages in turn; a warp has eight tokens, a lane four of their 128 values
+        const int team = (warp - 8) / Cf::TEAM, tok0 = (warp - 8) % Cf::TEAM * 8;
+        uint2 v[8];
         auto ask = [&](int u) {
-            int kb;
-            const int slot = slot_of(u, kb);
-            const __nv_bfloat16* p = x + (SECOND ? slot * slot_stride : 0) + kb * 128 + 4 * lane;
-            const bool in = kb * 128 + 4 * lane < K;
+            const int k = (u % line.per) * 128 + 4 * lane;
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int tok = warp - 8 + 4 * i;
+            for (int i = 0; i < 8; ++i) {
                 v[i] = make_uint2(0, 0);
-                if (in && tok < Tn) v[i] = *(const uint2*)(p + (size_t)tok * ld);
+                if (k < K && tok0 + i < Tn) v[i] = *(const uint2*)(x + (size_t)(tok0 + i) * ld + k);
             }
         };
-        if (line.lo < line.hi) ask(line.lo);
-        for (int u = line.lo; u < line.hi; ++u) {
+        if (line.lo + team < line.hi) ask(line.lo + team);
+        for (int u = line.lo + team; u < line.hi; u += Cf::TEAMS) {
+            const int i_u = u - line.lo, stage = i_u % Cf::STAGES, at = i_u % kScaleSlots;
+            const uint32_t phase = (i_u / Cf::STAGES) & 1;
             if (!mbar_wait_warp_quick(&ctl->empty[stage], phase ^ 1, abort_flag, status)) break;
             uint8_t* st = sm.ring + stage * Cf::STAGE + Cf::A_BYTES;
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int tok = warp - 8 + 4 * i;
-                if (tok >= NT) break;
-                const float f[4] = {__uint_as_float(v[i].x << 16), __uint_as_float(v[i].x & 0xffff0000u), __uint_as_float(v[i].y << 16),
-                                    __uint_as_float(v[i].y & 0xffff0000u)};
-                uint32_t m = max(max(abs_bits(f[0]), abs_bits(f[1])), max(abs_bits(f[2]), abs_bits(f[3])));
-                m = __reduce_max_sync(0xffffffffu, m);
-                const BlockScale b = block_scale(m);
-                const uint32_t hi = e4m3x4(f[0], f[1], f[2], f[3], b.inv);
-                uint32_t h01, h23;                     // hi as half pairs
-                halves_of_e4m3(hi, h01, h23);
-                const float2 g0 = __half22float2(*reinterpret_cast<const __half2*>(&h01)), g1 = __half22float2(*reinterpret_cast<const __half2*>(&h23));
-                const uint32_t lo = e4m3x4(f[0] * b.inv - g0.x, f[1] * b.inv - g0.y, f[2] * b.inv - g1.x, f[3] * b.inv - g1.y, b.inv == 0.f ? 0.f : 16.f);
-                const int at_row = 16 * (lane >> 2), off = 4 * (lane & 3);
-                *(uint32_t*)(st + tok * 128 + (at_row ^ ((tok & 7) << 4)) + off) = hi;
-                *(uint32_t*)(st + (NT + tok) * 128 + (at_row ^ ((tok & 7) << 4)) + off) = lo;       // (NT is a multiple of 8)
-                if (lane == 0) ctl->f[at * NT + tok] = b.s;
+            for (int i = 0; i < 8; ++i) {
+                const int tok = tok0 + i;
+                uint32_t hi, lo;
+                const float sc = two_terms(__uint_as_float(v[i].x << 16), __uint_as_float(v[i].x & 0xffff0000u), __uint_as_float(v[i].y << 16),
+                                           __uint_as_float(v[i].y & 0xffff0000u), hi, lo);
+                uint8_t* o = st + tok * 128 + ((16 * (lane >> 2)) ^ (i << 4)) + 4 * (lane & 3);      // (128-byte swizzle: tok % 8 = i)
+                *(uint32_t*)o = hi;
+                *(uint32_t*)(o + NT * 128) = lo;
+                if (lane == 0) ctl->f[at * NT + tok] = sc;
             }
-            if (u + 1 < line.hi) ask(u + 1);
+            if (u + Cf::TEAMS < line.hi) ask(u + Cf::TEAMS);
             fence_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(&ctl->full[stage]);
-            if (++stage == Cf::STAGES) { stage = 0; phase ^= 1; }
-            if (++at == kScaleSlots) at = 0;
         }
     } else if (warp >= 4) {
         int acc = 0, at = 0;
@@ -248,11 +253,11 @@ __device__ __forceinline__ void run_line(const Smem<WT, NT>& sm, const CUtensorM
 
 // Barriers and TMEM of a CTA.  TMEM is taken only when the grids before this one are complete, and the grid behind it is let in only when it
 // is taken: no CTA holds TMEM while it waits for one that still needs some.
-template <int WT, int NT>
+template <int WT, int NT, bool SECOND>
 __device__ __forceinline__ void set_up(const Smem<WT, NT>& sm) {
     using Cf = Cfg<WT, NT>;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < Cf::STAGES; ++s) { mbar_init(&sm.ctl->full[s], WT == kFp8 ? 5 : 1); mbar_init(&sm.ctl->empty[s], 1); }
+        for (int s = 0; s < Cf::STAGES; ++s) { mbar_init(&sm.ctl->full[s], WT == kFp8 && !SECOND ? 1 + Cf::TEAM : 1); mbar_init(&sm.ctl->empty[s], 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(&sm.ctl->tfull[i], 1); mbar_init(&sm.ctl->tempty[i], 4); }
         sm.ctl->abort_flag = 0;
         fence_barrier_init();
@@ -285,7 +290,7 @@ __device__ __forceinline__ float* meet(const Smem<WT, NT>& sm, const float* sum,
 }
 
 template <int WT, int NT>
-__global__ void __launch_bounds__(Cfg<WT, NT>::THREADS, Cfg<WT, NT>::CTAS)
+__global__ void __launch_bounds__(32 * Cfg<WT, NT>::WARPS1, Cfg<WT, NT>::CTAS)
 first_layer_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const __grid_constant__ TokArgs a, int S, int* status) {
     using Cf = Cfg<WT, NT>;
     using bf16 = __nv_bfloat16;
@@ -293,7 +298,7 @@ first_layer_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
     const int rank = (int)cluster_ctarank(), Tn = a.T;
     const Smem<WT, NT> sm(smem_raw);
     if (threadIdx.x == 0) { prefetch_tmap(&tmW); if (WT == kBf16) prefetch_tmap(&tmX); }
-    set_up(sm);
+    set_up<WT, NT, false>(sm);
     route_tokens<WT, (NT + 15) / 16>(a, 0, Tn, rank, (float*)sm.ring, sm.part, sm.ctl->R);
     fence_async_smem();                                // the ring is the copies' from here on
     __syncthreads();
@@ -307,28 +312,45 @@ first_layer_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
         Line line{0, 0, Kb, slot};
         cut(Kb, S, kr, line.lo, line.hi);
         const size_t blocks = (a.d + kQ - 1) / kQ;     // of the scales, along d
-        run_line<WT, NT, false>(sm, &tmW, &tmX, (const bf16*)a.x, a.d, 0, WT == kFp8 ? a.s1 + c0 / kQ * blocks : nullptr,
+        run_line<WT, NT, false>(sm, &tmW, &tmX, (const bf16*)a.x, a.d, nullptr, WT == kFp8 ? a.s1 + c0 / kQ * blocks : nullptr,
                                 (size_t)((a.d_e + kQ - 1) / kQ) * blocks, c0, a.d, Tn, line, status, sum, [](int, int) { return 1.f; });
     }
     cluster_wait();
     const float* cta = meet(sm, sum, Tn, S);
     if (live) {
-        bf16* out = (bf16*)a.a + (size_t)slot * a.group * a.d_e;
-        for (int q = kr * Cf::THREADS + threadIdx.x; q < Tn * kCols; q += S * Cf::THREADS) {
-            const int tok = q / kCols, col = c0 + q % kCols;
-            if (col >= a.d_e || !((R.of[slot] >> tok) & 1)) continue;
-            float h = 0.f;
-            for (int s = 0; s < S; ++s) h += ld_cluster(cta + tok * Cf::PITCH + q % kCols, first + s);
-            if (a.b1) h += to_f32(((const bf16*)a.b1)[(size_t)e * a.d_e + col]);
-            // (half a step, 2^-9 of the value, like the hidden rows of uoe_mlp_forward)
-            out[(size_t)tok * a.d_e + col] = __float2bfloat16_rn(act_precise(h, a.act));
+        // (token, 32 columns) per warp, or the token's 128 columns, a lane four of them, where they become two terms
+        constexpr int W = 4, WARPS = Cf::WARPS1;
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        for (int tok = kr * WARPS + warp; tok < Tn; tok += S * WARPS) {
+            if (!((R.of[slot] >> tok) & 1)) continue;
+            float h[W];
+#pragma unroll
+            for (int v = 0; v < W; ++v) {
+                const int col = c0 + W * lane + v;
+                h[v] = 0.f;
+                for (int s = 0; s < S; ++s) h[v] += ld_cluster(cta + tok * Cf::PITCH + W * lane + v, first + s);
+                if (a.b1 && col < a.d_e) h[v] += to_f32(((const bf16*)a.b1)[(size_t)e * a.d_e + col]);
+                // (half a step, 2^-9 of the value, like the hidden rows of uoe_mlp_forward)
+                h[v] = col < a.d_e ? to_f32(__float2bfloat16_rn(act_precise(h[v], a.act))) : 0.f;
+            }
+            if constexpr (WT == kFp8) {
+                uint32_t hi, lo;
+                const float sc = two_terms(h[0], h[1], h[2], h[3], hi, lo);
+                const size_t dp = (size_t)tiles_n * kCols;
+                uint8_t* o = (uint8_t*)a.a + ((size_t)2 * slot * a.group + tok) * dp + c0 + W * lane;
+                *(uint32_t*)o = hi;
+                *(uint32_t*)(o + a.group * dp) = lo;
+                if (lane == 0) a.af[((size_t)slot * tiles_n + c0 / kCols) * kMaxTokens + tok] = sc;
+            } else if (c0 + W * lane < a.d_e) {        // (d_e is a multiple of 8)
+                *(uint2*)((bf16*)a.a + ((size_t)slot * a.group + tok) * a.d_e + c0 + W * lane) = make_uint2(pack_bf16x2(h[0], h[1]), pack_bf16x2(h[2], h[3]));
+            }
         }
     }
     if (S > 1) cluster_sync_all();      // nobody's shared memory goes while another CTA may read it
 }
 
 template <int WT, int NT>
-__global__ void __launch_bounds__(Cfg<WT, NT>::THREADS, Cfg<WT, NT>::CTAS)
+__global__ void __launch_bounds__(32 * Cfg<WT, NT>::WARPS2, Cfg<WT, NT>::CTAS)
 second_layer_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const __grid_constant__ TokArgs a, int S, int* status) {
     using Cf = Cfg<WT, NT>;
     using bf16 = __nv_bfloat16;
@@ -336,7 +358,7 @@ second_layer_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
     const int rank = (int)cluster_ctarank(), Tn = a.T;
     const Smem<WT, NT> sm(smem_raw);
     if (threadIdx.x == 0) { prefetch_tmap(&tmW); if (WT == kBf16) prefetch_tmap(&tmX); }
-    set_up(sm);
+    set_up<WT, NT, true>(sm);
     read_routing(a, sm.ctl->R);
     const Routed& R = sm.ctl->R;
     if (blockIdx.x == 0 && threadIdx.x < 32 && a.r.expert_offsets) write_offsets(a);
@@ -346,10 +368,10 @@ second_layer_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
     cut(c0 < a.d ? R.experts * line.per : 0, S, kr, line.lo, line.hi);      // (the grid is whole clusters)
     float sum[NT] = {};
     const size_t blocks = (a.d_e + kQ - 1) / kQ;
-    run_line<WT, NT, true>(sm, &tmW, &tmX, (const bf16*)a.a, a.d_e, (size_t)a.group * a.d_e, WT == kFp8 ? a.s2 + c0 / kQ * blocks : nullptr,
+    run_line<WT, NT, true>(sm, &tmW, &tmX, nullptr, 0, a.af, WT == kFp8 ? a.s2 + c0 / kQ * blocks : nullptr,
                            (size_t)((a.d + kQ - 1) / kQ) * blocks, c0, a.d_e, Tn, line, status, sum, weight);
     const float* cta = meet(sm, sum, Tn, S);
-    for (int q = kr * Cf::THREADS + threadIdx.x; q < Tn * kCols; q += S * Cf::THREADS) {
+    for (int q = kr * blockDim.x + threadIdx.x; q < Tn * kCols; q += S * blockDim.x) {
         const int tok = q / kCols, col = c0 + q % kCols;
         if (col >= a.d) continue;
         float s = 0.f;
@@ -386,6 +408,13 @@ bool value_map(CUtensorMap* tm, const void* x, int rows, int K, int slots, size_
     return make_tmap(tm, x, 3, dims, str, box);
 }
 
+// the hidden rows' two terms, [2 n, group, d_e padded]
+bool term_map(CUtensorMap* tm, const void* a, int group, int d_e, int n, int NT) {
+    const uint64_t dp = q_pad(d_e), dims[3] = {dp, (uint64_t)group, 2 * (uint64_t)n}, str[2] = {dp, dp * group};
+    const uint32_t box[3] = {128, (uint32_t)NT, 1};
+    return make_tmap(tm, a, 3, dims, str, box, CU_TENSOR_MAP_DATA_TYPE_UINT8);
+}
+
 template <int WT, int NT>
 uoe_status launch_layers(const TokArgs& a, int* status, cudaStream_t s) {
     using Cf = Cfg<WT, NT>;
@@ -404,7 +433,7 @@ uoe_status launch_layers(const TokArgs& a, int* status, cudaStream_t s) {
         if (WT != kBf16) tmX = tmW;
         else if (!value_map(&tmX, a.x, a.T, a.d, 1, (size_t)a.T * a.d, NT)) return UOE_ERR_CUDA;
         ProfScope ps("tokens_first", s);
-        launch_clusters(first_layer_kernel<WT, NT>, grid(tiles, S), Cf::THREADS, smem, s, tmW, tmX, a, S, status);
+        launch_clusters(first_layer_kernel<WT, NT>, grid(tiles, S), 32 * Cf::WARPS1, smem, s, tmW, tmX, a, S, status);
         UOE_LAUNCHED();
     }
     {
@@ -413,8 +442,9 @@ uoe_status launch_layers(const TokArgs& a, int* status, cudaStream_t s) {
         if (!weight_map<WT>(&tmW, a.W2, a.n, a.d_e, a.d)) return UOE_ERR_CUDA;
         if (WT != kBf16) tmX = tmW;
         else if (!value_map(&tmX, a.a, a.group, a.d_e, a.n, (size_t)a.group * a.d_e, NT)) return UOE_ERR_CUDA;
+        if (WT == kFp8 && !term_map(&tmX, a.a, a.group, a.d_e, a.n, NT)) return UOE_ERR_CUDA;
         ProfScope ps("tokens_second", s);
-        launch_clusters(second_layer_kernel<WT, NT>, grid(tiles, S), Cf::THREADS, smem, s, tmW, tmX, a, S, status);
+        launch_clusters(second_layer_kernel<WT, NT>, grid(tiles, S), 32 * Cf::WARPS2, smem, s, tmW, tmX, a, S, status);
         UOE_LAUNCHED();
     }
     return UOE_OK;
@@ -432,11 +462,22 @@ int group_of(bool bf16) { return bf16 ? kMaxTokens : group_f32(); }
 }  // namespace
 }  // namespace tokens
 
+// Workspace: status, the router's word, the hidden rows (bfloat16, or two e4m3 terms and a scale per 128), float32 groups behind one another.
+static size_t tokens_ws(const Dims& D, size_t* routed, size_t* a, size_t* af) {
+    using namespace tokens;
+    const int group = group_of(D.bf16), groups = (D.B + group - 1) / group;
+    const size_t width = D.bf16 ? (size_t)q_pad(D.d_e) * 2 : (size_t)D.d_e * 4;
+    WsCarver w;
+    w.take(kStatusBytes);
+    const size_t r = w.take(groups * sizeof(Routed)), h = w.take((size_t)groups * D.n * group * width), f = w.take((size_t)D.n * q_blocks(D.d_e) * kMaxTokens * 4);
+    if (routed) { *routed = r; *a = h; *af = f; }
+    return w.off;
+}
+
 size_t mlp_tokens_workspace_bytes(const Dims& D) {
     using namespace tokens;
     if (D.L != 1 || D.B > kMaxTokens) return 0;
-    const int group = group_of(D.bf16), groups = (D.B + group - 1) / group;
-    return align_up(kStatusBytes + align_up(groups * sizeof(Routed), 1024) + (size_t)groups * D.n * group * D.d_e * D.esize, 1024);
+    return tokens_ws(D, nullptr, nullptr, nullptr);
 }
 
 }  // namespace uoe
@@ -460,8 +501,11 @@ extern "C" uoe_status uoe_mlp_tokens(const uoe_problem* prob, const void* x, con
     TokArgs a = {};
     a.x = x; a.Wr = W_r; a.W1 = W1; a.W2 = W2; a.b1 = b1; a.b2 = b2; a.s1 = w1_scale; a.s2 = w2_scale;
     a.group = group_of(D.bf16);
-    a.routed = (Routed*)((char*)ws + kStatusBytes);
-    a.a = (char*)ws + kStatusBytes + align_up((D.B + a.group - 1) / a.group * sizeof(Routed), 1024);
+    size_t o_r, o_a, o_f;
+    tokens_ws(D, &o_r, &o_a, &o_f);
+    a.routed = (Routed*)((char*)ws + o_r);
+    a.a = (char*)ws + o_a;
+    a.af = (float*)((char*)ws + o_f);
     a.y = y;
     if (r) a.r = RoutingPtrs{r->expert_idx, r->patch_idx, r->gate, r->p_samp, r->p_patch, r->expert_offsets};
     a.T = D.B; a.d = D.d; a.d_e = D.d_e; a.n = D.n; a.k = D.k; a.act = prob->act;
