@@ -9,17 +9,18 @@ namespace tokens {
 using namespace tc;
 
 constexpr int kMaxTokens = 64;
-constexpr int kCluster = 4;         // CTAs, which share the router's work and the contraction of a tile
 constexpr int kRouteWarps = 8;
 enum { kBf16 = 0, kFp8 = 1, kF32 = 2 };
 
 struct Routed {                     // what the router says about a group's tokens
-    uint32_t mask[kMaxTokens];      // experts that token chose
-    float p[kMaxTokens][32];        // sample gate (Eq. 21)
+    unsigned long long of[32];      // tokens that chose expert list[i]
     int experts;                    // that some token chose
     int list[32];                   // these, ascending
-    unsigned long long of[32];      // tokens that chose expert list[i]
+    uint32_t mask[kMaxTokens];      // experts that token chose
+    float p[kMaxTokens][32];        // sample gate (Eq. 21)
 };
+// words of it that say something about Tn tokens
+__device__ __forceinline__ int routed_words(int Tn) { return (int)(offsetof(Routed, p) / 4) + 32 * Tn; }
 
 struct TokArgs {
     const void *x, *Wr, *W1, *W2, *b1, *b2;
@@ -55,11 +56,11 @@ __device__ __forceinline__ void halves_of_e4m3(uint32_t v, uint32_t& lo, uint32_
 }
 
 // Sums over this CTA's piece of d: part[token * n + expert].
-template <int WT, int MT>
+template <int WT, int MT, int CL>
 __device__ void router_piece(const TokArgs& a, int t0, int Tn, int rank, float* red /* [8][Tn * n] */, float* part) {
     using T = typename Elem<WT>::T;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int d = a.d, n = a.n, len = ((d + kCluster - 1) / kCluster + 15) / 16 * 16;
+    const int d = a.d, n = a.n, len = ((d + CL - 1) / CL + 15) / 16 * 16;
     const T* x = (const T*)a.x + (size_t)t0 * d;
     const T* Wr = (const T*)a.Wr;
     const int k0 = rank * len, k1 = min(d, k0 + len);
@@ -85,35 +86,56 @@ __device__ void router_piece(const TokArgs& a, int t0, int Tn, int rank, float* 
             }
         } else {
             const int J = (n + 7) / 8;                 // fragment j: experts g * J + j
-            float c[MT][4][4];
+            const bool whole = n == 8 * J && J != 3;   // a lane's experts of a row of W_r in one load
+            constexpr int U = MT == 1 ? 4 : 2;         // steps of 16 whose loads are in flight together
+            float c[MT][4][4] = {};
+            for (int kb = k0 + warp * 16; kb < k1; kb += kRouteWarps * 16 * U) {
+                uint2 xv[U][MT][2], wv[U][4];          // a row's (up to) four experts, two per word
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+                for (int u = 0; u < U; ++u) {
+                    const int kt = kb + u * kRouteWarps * 16 + 4 * t;
+                    const bool in = kt < k1;
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
+                    for (int m = 0; m < MT; ++m)
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) c[m][j][u] = 0.f;
-#pragma unroll 4
-            for (int kk = k0 + warp * 16; kk < k1; kk += kRouteWarps * 16) {
-                const int kt = kk + 4 * t;
-                uint32_t af[MT][4];
+                        for (int h = 0; h < 2; ++h) {
+                            const int row = m * 16 + h * 8 + g;
+                            xv[u][m][h] = make_uint2(0, 0);
+                            if (row < Tn && in) xv[u][m][h] = *(const uint2*)(x + (size_t)row * d + kt);
+                        }
 #pragma unroll
-                for (int m = 0; m < MT; ++m)
+                    for (int r = 0; r < 4; ++r) {
+                        const T* p = Wr + (size_t)(kt + r) * n + g * J;
+                        wv[u][r] = make_uint2(0, 0);
+                        if (!in) continue;
+                        if (whole) {
+                            if (J == 1) wv[u][r].x = *(const uint16_t*)p;
+                            else if (J == 2) wv[u][r].x = *(const uint32_t*)p;
+                            else wv[u][r] = *(const uint2*)p;
+                        } else {
+                            uint32_t q[4] = {0, 0, 0, 0};
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        uint2 v = make_uint2(0, 0);
-                        const int row = m * 16 + h * 8 + g;
-                        if (row < Tn && kt < k1) v = *(const uint2*)(x + (size_t)row * d + kt);
-                        af[m][h] = v.x; af[m][2 + h] = v.y;
+                            for (int j = 0; j < 4; ++j)
+                                if (j < J && g * J + j < n) q[j] = *(const uint16_t*)(p + j);
+                            wv[u][r] = make_uint2(q[0] | (q[1] << 16), q[2] | (q[3] << 16));
+                        }
                     }
+                }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (j >= J) break;
-                    const int i = g * J + j;
-                    uint32_t w[4];
+                for (int u = 0; u < U; ++u) {
+                    if (kb + u * kRouteWarps * 16 >= k1) break;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) w[r] = i < n && kt < k1 ? *(const uint16_t*)(Wr + (size_t)(kt + r) * n + i) : 0u;
+                    for (int j = 0; j < 4; ++j) {
+                        if (j >= J) break;
+                        const uint32_t sel = j & 1 ? 0x7632 : 0x5410;
+                        const uint32_t b0 = j < 2 ? __byte_perm(wv[u][0].x, wv[u][1].x, sel) : __byte_perm(wv[u][0].y, wv[u][1].y, sel);
+                        const uint32_t b1 = j < 2 ? __byte_perm(wv[u][2].x, wv[u][3].x, sel) : __byte_perm(wv[u][2].y, wv[u][3].y, sel);
 #pragma unroll
-                    for (int m = 0; m < MT; ++m) mma16(c[m][j], af[m], w[0] | (w[1] << 16), w[2] | (w[3] << 16));
+                        for (int m = 0; m < MT; ++m) {
+                            const uint32_t af[4] = {xv[u][m][0].x, xv[u][m][1].x, xv[u][m][0].y, xv[u][m][1].y};
+                            mma16(c[m][j], af, b0, b1);
+                        }
+                    }
                 }
             }
 #pragma unroll
@@ -137,9 +159,9 @@ __device__ void router_piece(const TokArgs& a, int t0, int Tn, int rank, float* 
 }
 
 // Eq. 21-22 for the group's tokens, the same in every CTA.
-template <int WT, int MT>
+template <int WT, int MT, int CL /* CTAs of the cluster */>
 __device__ void route_tokens(const TokArgs& a, int t0, int Tn, int rank, float* red, float* part, Routed& R) {
-    router_piece<WT, MT>(a, t0, Tn, rank, red, part);
+    router_piece<WT, MT, CL>(a, t0, Tn, rank, red, part);
     if (threadIdx.x < 32) R.of[threadIdx.x] = 0;       // (by expert for now)
     cluster_sync_all();                                // every CTA's piece is there
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = a.n;
@@ -148,7 +170,7 @@ __device__ void route_tokens(const TokArgs& a, int t0, int Tn, int rank, float* 
         if (lane < n) {
             v = 0.f;
 #pragma unroll
-            for (int p = 0; p < kCluster; ++p) v += ld_cluster(part + tok * n + lane, p);
+            for (int p = 0; p < CL; ++p) v += ld_cluster(part + tok * n + lane, p);
         }
         float mx = v;
 #pragma unroll
@@ -194,7 +216,7 @@ __device__ __forceinline__ void cut(int units, int workers, int w, int& lo, int&
 // The router's outputs for the caller, by one CTA of the group's first cluster.
 __device__ __forceinline__ void write_routing(const TokArgs& a, const Routed& R, int t0, int Tn) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-    for (int q = threadIdx.x; q < (int)(sizeof(Routed) / 4); q += blockDim.x) ((uint32_t*)(a.routed + blockIdx.z))[q] = ((const uint32_t*)&R)[q];
+    for (int q = threadIdx.x; q < routed_words(Tn); q += blockDim.x) ((uint32_t*)(a.routed + blockIdx.z))[q] = ((const uint32_t*)&R)[q];
     if (!a.r.expert_idx) return;
     for (int tok = warp; tok < Tn; tok += warps) {
         const uint32_t m = R.mask[tok];
@@ -227,12 +249,12 @@ __device__ __forceinline__ void write_offsets(const TokArgs& a) {
     if (lane == 0) a.r.expert_offsets[0] = 0;
 }
 // The router's word from the first kernel, into shared memory.
-__device__ __forceinline__ void read_routing(const TokArgs& a, Routed& R) {
-    for (int q = threadIdx.x; q < (int)(sizeof(Routed) / 4); q += blockDim.x) ((uint32_t*)&R)[q] = __ldcg((const uint32_t*)(a.routed + blockIdx.z) + q);
+__device__ __forceinline__ void read_routing(const TokArgs& a, Routed& R, int Tn) {
+    for (int q = threadIdx.x; q < routed_words(Tn); q += blockDim.x) ((uint32_t*)&R)[q] = __ldcg((const uint32_t*)(a.routed + blockIdx.z) + q);
     __syncthreads();
 }
 
-template <typename... KArgs, typename... Args>
+template <int CL, typename... KArgs, typename... Args>
 cudaError_t launch_clusters(void (*kern)(KArgs...), dim3 grid, int threads, size_t smem, cudaStream_t s, Args&&... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
@@ -243,7 +265,7 @@ cudaError_t launch_clusters(void (*kern)(KArgs...), dim3 grid, int threads, size
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = kCluster;
+    at[1].val.clusterDim.x = CL;
     at[1].val.clusterDim.y = 1;
     at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
@@ -253,8 +275,8 @@ cudaError_t launch_clusters(void (*kern)(KArgs...), dim3 grid, int threads, size
 
 
 // CTAs of a tile: the largest split that leaves every CTA a unit of the contraction and no more CTAs than the SMs hold.
-inline int split_of(int units, long long tiles, int ctas_per_sm) {
-    int S = kCluster;
+inline int split_of(int units, long long tiles, int cluster, int ctas_per_sm) {
+    int S = cluster;
     while (S > 1 && (units < S || tiles * S > (long long)ctas_per_sm * sm_count())) S >>= 1;
     return S;
 }

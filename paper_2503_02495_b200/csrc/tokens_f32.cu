@@ -10,6 +10,7 @@ namespace tokens {
 namespace {
 
 constexpr int kCols = 64, kWarps = 8, kThreads = 32 * kWarps, kGroup = 16, kStep = 128;
+constexpr int kCluster = 4;
 
 // Tokens in steps of 8: TG = 1 or 2.
 template <int TG> struct Smem {
@@ -121,7 +122,7 @@ first_layer_f32_kernel(const TokArgs a, int S) {
     const Smem<TG> sm(smem_raw, Tn, a.n);
     pdl_trigger();
     pdl_wait();
-    route_tokens<kF32, 1>(a, t0, Tn, rank, sm.red, sm.part, *sm.R);
+    route_tokens<kF32, 1, kCluster>(a, t0, Tn, rank, sm.red, sm.part, *sm.R);
     const Routed& R = *sm.R;
     if (blockIdx.x == 0) write_routing(a, R, t0, Tn);
     const int tiles_n = (a.d_e + kCols - 1) / kCols, tile = blockIdx.x / S, kr = rank % S, first = rank - kr;
@@ -157,7 +158,7 @@ second_layer_f32_kernel(const TokArgs a, int S) {
     const Smem<TG> sm(smem_raw, Tn, a.n);
     pdl_trigger();
     pdl_wait();
-    read_routing(a, *sm.R);
+    read_routing(a, *sm.R, Tn);
     const Routed& R = *sm.R;
     if (blockIdx.x == 0 && blockIdx.z == 0 && threadIdx.x < 32 && a.r.expert_offsets) write_offsets(a);
     const int c0 = blockIdx.x / S * kCols, kr = rank % S, first = rank - kr, per = (a.d_e + kStep - 1) / kStep;
@@ -210,16 +211,16 @@ uoe_status launch_layers(const TokArgs& a, cudaStream_t s) {
     const long long chosen = a.n < (long long)Tn * a.k ? a.n : (long long)Tn * a.k;      // experts at most
     {
         const long long tiles = chosen * ((a.d_e + kCols - 1) / kCols);
-        const int S = split_of((a.d + kStep - 1) / kStep, tiles * groups, 1);
+        const int S = split_of((a.d + kStep - 1) / kStep, tiles * groups, kCluster, 1);
         ProfScope ps("tokens_first", s);
-        launch_clusters(first_layer_f32_kernel<TG>, grid(tiles, S), kThreads, smem, s, a, S);
+        launch_clusters<kCluster>(first_layer_f32_kernel<TG>, grid(tiles, S), kThreads, smem, s, a, S);
         UOE_LAUNCHED();
     }
     {
         const long long tiles = (a.d + kCols - 1) / kCols;
-        const int S = split_of(a.k * ((a.d_e + kStep - 1) / kStep), tiles * groups, 1);
+        const int S = split_of(a.k * ((a.d_e + kStep - 1) / kStep), tiles * groups, kCluster, 1);
         ProfScope ps("tokens_second", s);
-        launch_clusters(second_layer_f32_kernel<TG>, grid(tiles, S), kThreads, smem, s, a, S);
+        launch_clusters<kCluster>(second_layer_f32_kernel<TG>, grid(tiles, S), kThreads, smem, s, a, S);
         UOE_LAUNCHED();
     }
     return UOE_OK;

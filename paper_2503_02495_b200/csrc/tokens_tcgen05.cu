@@ -8,7 +8,7 @@
 //   first_layer_kernel   routes, then a = phi(x W1 + b1) for every (chosen expert, 128 hidden columns)
 //   second_layer_kernel  y = x + sum over experts gate (a W2 + b2) for every 128 columns of y, the contraction running over all chosen
 //                        experts' hidden columns in one line
-// Clusters of four CTAs share the router's work, a quarter of d each; every cluster routes for itself (a few KB from L2, instead of a third
+// The CTAs of a cluster share the router's work, a part of d each; every cluster routes for itself (a few KB from L2, instead of a third
 // kernel).  S of them share a tile's contraction; their sums meet in distributed shared memory in a fixed order.
 //
 // Stages: 128 columns x 64 of the contraction of bfloat16 weights (as they lie, columns contiguous), or x 128 of 8-bit weights (the
@@ -36,9 +36,10 @@ template <int WT, int NT /* tokens, rounded up */> struct Cfg {
     static constexpr int K = WT == kFp8 ? 128 : 64;                       // of the contraction per stage
     static constexpr int A_BYTES = 16384, B_BYTES = N * 128, STAGE = A_BYTES + B_BYTES;
     static constexpr int CTAS = NT <= 32 ? 2 : 1;                         // per SM
+    static constexpr int CLUSTER = CTAS == 2 ? 8 : 4;                     // (eight CTAs of an SM each: some clusters wait for a second turn)
     static constexpr int STAGES = CTAS == 1 ? 6 : NT <= 16 ? 5 : 4;
     static constexpr int TMEM_COLS = 2 * N < 32 ? 32 : 2 * N;
-    static constexpr int TEAM = NT / 8, TEAMS = NT == 8 ? 4 : NT == 64 ? 1 : 2;       // 8-bit: a team of warps fills a stage, 8 tokens each
+    static constexpr int TEAM = NT / 8, TEAMS = NT == 8 ? 4 : NT == 16 ? 2 : 1;       // 8-bit: a team of warps fills a stage, 8 tokens each
     static constexpr int WARPS1 = WT == kFp8 ? 8 + TEAM * TEAMS : 8, WARPS2 = 8;      // of the two kernels
     static constexpr int PITCH = kCols + 4;                               // floats of a token's sums in shared memory
     static constexpr int RING = STAGES * STAGE;
@@ -200,10 +201,17 @@ __device__ __forceinline__ void run_line(const Smem<WT, NT>& sm, const CUtensorM
             if (!ends(u, kb)) continue;
             const int e = R.list[slot];
             const unsigned long long of = SECOND ? R.of[slot] : ~0ull;
+            float w[(NT + 31) / 32];                   // factors of tokens lane, lane + 32
+#pragma unroll
+            for (int i = 0; i < (NT + 31) / 32; ++i) w[i] = lane + 32 * i < Tn ? weight(lane + 32 * i, e) : 0.f;
             float s = 1.f;
             if constexpr (WT == kFp8) s = __ldg(scale + (size_t)e * scale_stride + kb);
             if (!mbar_wait_warp_quick(&ctl->tfull[acc], acc_phase, abort_flag, status)) break;
             tc_fence_after();
+            if constexpr (WT == kFp8) {
+#pragma unroll
+                for (int i = 0; i < (NT + 31) / 32; ++i) w[i] *= s * ctl->f[at * NT + (lane + 32 * i) % NT];
+            }
             const uint32_t taddr = tmem_base + acc * Cf::N + ((uint32_t)((warp & 3) * 32) << 16);
             constexpr int STEP = Cf::N < 32 ? 16 : 32;                    // columns at a time: 8-bit: 16 hi columns, then their 16 lo columns
             if constexpr (WT == kFp8) {
@@ -222,10 +230,8 @@ __device__ __forceinline__ void run_line(const Smem<WT, NT>& sm, const CUtensorM
 #pragma unroll
                     for (int i = 0; i < H; ++i) {
                         const int tok = t + i;
-                        if ((of >> tok) & 1) {
-                            const float w = s * ctl->f[at * NT + tok] * weight(tok, e);
-                            sum[tok] = fmaf(w, fmaf(0.0625f, __uint_as_float(vl[i]), __uint_as_float(vh[i])), sum[tok]);
-                        }
+                        const float f = __shfl_sync(0xffffffffu, w[tok / 32], tok % 32);
+                        if ((of >> tok) & 1) sum[tok] = fmaf(f, fmaf(0.0625f, __uint_as_float(vl[i]), __uint_as_float(vh[i])), sum[tok]);
                     }
                 }
             } else {
@@ -241,8 +247,10 @@ __device__ __forceinline__ void run_line(const Smem<WT, NT>& sm, const CUtensorM
                         if (lane == 0) mbar_arrive(&ctl->tempty[acc]);
                     }
 #pragma unroll
-                    for (int i = 0; i < STEP; ++i)
-                        if ((of >> (t + i)) & 1) sum[t + i] = fmaf(weight(t + i, e), __uint_as_float(v[i]), sum[t + i]);
+                    for (int i = 0; i < STEP; ++i) {
+                        const float f = __shfl_sync(0xffffffffu, w[(t + i) / 32], (t + i) % 32);
+                        if ((of >> (t + i)) & 1) sum[t + i] = fmaf(f, __uint_as_float(v[i]), sum[t + i]);
+                    }
                 }
             }
             if (++acc == 2) { acc = 0; acc_phase ^= 1; }
@@ -299,7 +307,7 @@ first_layer_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
     const Smem<WT, NT> sm(smem_raw);
     if (threadIdx.x == 0) { prefetch_tmap(&tmW); if (WT == kBf16) prefetch_tmap(&tmX); }
     set_up<WT, NT, false>(sm);
-    route_tokens<WT, (NT + 15) / 16>(a, 0, Tn, rank, (float*)sm.ring, sm.part, sm.ctl->R);
+    route_tokens<WT, (NT + 15) / 16, Cf::CLUSTER>(a, 0, Tn, rank, (float*)sm.ring, sm.part, sm.ctl->R);
     fence_async_smem();                                // the ring is the copies' from here on
     __syncthreads();
     const Routed& R = sm.ctl->R;
@@ -359,7 +367,7 @@ second_layer_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
     const Smem<WT, NT> sm(smem_raw);
     if (threadIdx.x == 0) { prefetch_tmap(&tmW); if (WT == kBf16) prefetch_tmap(&tmX); }
     set_up<WT, NT, true>(sm);
-    read_routing(a, sm.ctl->R);
+    read_routing(a, sm.ctl->R, Tn);
     const Routed& R = sm.ctl->R;
     if (blockIdx.x == 0 && threadIdx.x < 32 && a.r.expert_offsets) write_offsets(a);
     const int c0 = blockIdx.x / S * kCols, kr = rank % S, first = rank - kr;
@@ -424,27 +432,27 @@ uoe_status launch_layers(const TokArgs& a, int* status, cudaStream_t s) {
     if (st != UOE_OK) return st;
     CUtensorMap tmW, tmX;
     const size_t smem = Smem<WT, NT>::bytes(a.T, a.n);
-    auto grid = [&](long long tiles, int S) { return dim3((unsigned)((tiles * S + kCluster - 1) / kCluster * kCluster)); };
+    auto grid = [&](long long tiles, int S) { return dim3((unsigned)((tiles * S + Cf::CLUSTER - 1) / Cf::CLUSTER * Cf::CLUSTER)); };
     const long long chosen = a.n < (long long)a.T * a.k ? a.n : (long long)a.T * a.k;      // experts at most
     {
         const long long tiles = chosen * ((a.d_e + kCols - 1) / kCols);
-        const int S = split_of((a.d + Cf::K - 1) / Cf::K, tiles, Cf::CTAS);
+        const int S = split_of((a.d + Cf::K - 1) / Cf::K, tiles, Cf::CLUSTER, Cf::CTAS);
         if (!weight_map<WT>(&tmW, a.W1, a.n, a.d, a.d_e)) return UOE_ERR_CUDA;
         if (WT != kBf16) tmX = tmW;
         else if (!value_map(&tmX, a.x, a.T, a.d, 1, (size_t)a.T * a.d, NT)) return UOE_ERR_CUDA;
         ProfScope ps("tokens_first", s);
-        launch_clusters(first_layer_kernel<WT, NT>, grid(tiles, S), 32 * Cf::WARPS1, smem, s, tmW, tmX, a, S, status);
+        launch_clusters<Cf::CLUSTER>(first_layer_kernel<WT, NT>, grid(tiles, S), 32 * Cf::WARPS1, smem, s, tmW, tmX, a, S, status);
         UOE_LAUNCHED();
     }
     {
         const long long tiles = (a.d + kCols - 1) / kCols;
-        const int S = split_of(a.k * ((a.d_e + Cf::K - 1) / Cf::K), tiles, Cf::CTAS);
+        const int S = split_of(a.k * ((a.d_e + Cf::K - 1) / Cf::K), tiles, Cf::CLUSTER, Cf::CTAS);
         if (!weight_map<WT>(&tmW, a.W2, a.n, a.d_e, a.d)) return UOE_ERR_CUDA;
         if (WT != kBf16) tmX = tmW;
         else if (!value_map(&tmX, a.a, a.group, a.d_e, a.n, (size_t)a.group * a.d_e, NT)) return UOE_ERR_CUDA;
         if (WT == kFp8 && !term_map(&tmX, a.a, a.group, a.d_e, a.n, NT)) return UOE_ERR_CUDA;
         ProfScope ps("tokens_second", s);
-        launch_clusters(second_layer_kernel<WT, NT>, grid(tiles, S), 32 * Cf::WARPS2, smem, s, tmW, tmX, a, S, status);
+        launch_clusters<Cf::CLUSTER>(second_layer_kernel<WT, NT>, grid(tiles, S), 32 * Cf::WARPS2, smem, s, tmW, tmX, a, S, status);
         UOE_LAUNCHED();
     }
     return UOE_OK;
