@@ -35,67 +35,75 @@ __device__ __forceinline__ uint4 load_piece(const T* row, int c, int C, bool who
 template <typename T>
 __global__ void __launch_bounds__(256)
 quantize_rows_kernel(const T* __restrict__ x, uint8_t* __restrict__ q, float* __restrict__ scale, long long rows, int C, int Cb, int groups /* of kBlocksPerCta blocks */,
-                     int whole, const SrcMap map, const int* __restrict__ offsets, int n) {
+                     int splits, int whole, const SrcMap map, const int* __restrict__ offsets, int n) {
     pdl_trigger();
     constexpr int V = Vec16<T>::N;                    // elements per 16 bytes
     constexpr int LPB = kQ / V;                       // lanes per block: 16 or 32
     constexpr int BPW = 32 / LPB;                     // blocks a warp loads at a time
     constexpr int ROUNDS = kBlocksPerCta / BPW;
     constexpr int RPW = kRowsPerCta / 8;              // rows per warp
-    __shared__ float s_scale[kBlocksPerCta][kRowsPerCta];
+    __shared__ float s_scale[2][kBlocksPerCta][kRowsPerCta];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const long long per_mat = ((rows + kRowsPerCta - 1) / kRowsPerCta) * groups;
+    const long long per_mat = ((rows + kRowsPerCta - 1) / kRowsPerCta) * splits;
     const long long mat = blockIdx.x / per_mat;
     const long long rest = blockIdx.x - mat * per_mat;
-    const long long row0 = rest / groups * kRowsPerCta;
-    const int cb0 = (int)(rest % groups) * kBlocksPerCta;
+    const long long row0 = rest / splits * kRowsPerCta;
     pdl_wait();
-    int e = 0, off_e = 0;
+    // where the warp's rows come from: looked up once for all columns, a lane per row
+    long long mine = row0 + warp * RPW + (lane % RPW) < rows ? mat * rows + row0 + warp * RPW + (lane % RPW) : -1;
     if (map.on()) {
         if (row0 >= offsets[n]) return;               // (regions are multiples of 128 rows: the CTA's rows are one expert's)
+        int e = 0;
         while (e + 1 < n && row0 >= offsets[e + 1]) ++e;
-        off_e = offsets[e];
+        mine = source_row(map, (int)row0 + warp * RPW + (lane % RPW), e, offsets[e]);
     }
-    uint4 v[RPW][ROUNDS];
+    long long src[RPW];
 #pragma unroll
-    for (int i = 0; i < RPW; ++i) {
-        const long long r = row0 + warp * RPW + i;
-        long long src = r < rows ? mat * rows + r : -1;
-        if (map.on()) src = source_row(map, (int)r, e, off_e);
-#pragma unroll
-        for (int u = 0; u < ROUNDS; ++u) {
-            const int c = (cb0 + u * BPW + lane / LPB) * kQ + (lane % LPB) * V;
-            v[i][u] = src >= 0 ? load_piece(x + src * C, c, C, whole) : make_uint4(0, 0, 0, 0);
-        }
-    }
+    for (int i = 0; i < RPW; ++i) src[i] = __shfl_sync(0xffffffffu, mine, i);
     const long long Cp = (long long)Cb * kQ;
+    uint4 v[RPW][ROUNDS];
+    auto load = [&](int group) {
 #pragma unroll
-    for (int i = 0; i < RPW; ++i) {
-        const long long r = row0 + warp * RPW + i;
+        for (int i = 0; i < RPW; ++i)
 #pragma unroll
-        for (int u = 0; u < ROUNDS; ++u) {
-            float f[V];
-            unpack16<T>(v[i][u], f);
-            uint32_t m = 0;
+            for (int u = 0; u < ROUNDS; ++u) {
+                const int c = (group * kBlocksPerCta + u * BPW + lane / LPB) * kQ + (lane % LPB) * V;
+                v[i][u] = src[i] >= 0 ? load_piece(x + src[i] * C, c, C, whole) : make_uint4(0, 0, 0, 0);
+            }
+    };
+    int group = (int)(rest % splits), b = 0;
+    load(group);
+    for (; group < groups; group += splits, b ^= 1) {
+        const int cb0 = group * kBlocksPerCta;
 #pragma unroll
-            for (int j = 0; j < V; ++j) m = max(m, abs_bits(f[j]));
+        for (int i = 0; i < RPW; ++i) {
+            const long long r = row0 + warp * RPW + i;
 #pragma unroll
-            for (int o = LPB / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-            const BlockScale b = block_scale(m);
-            const int cb = cb0 + u * BPW + lane / LPB;
-            if (lane % LPB == 0) s_scale[u * BPW + lane / LPB][warp * RPW + i] = b.s;
-            if (r < rows && cb < Cb) {
-                uint8_t* o = q + (mat * rows + r) * Cp + cb * kQ + (lane % LPB) * V;
-                if constexpr (V == 8) *(uint2*)o = make_uint2(e4m3x4(f[0], f[1], f[2], f[3], b.inv), e4m3x4(f[4], f[5], f[6], f[7], b.inv));
-                else *(uint32_t*)o = e4m3x4(f[0], f[1], f[2], f[3], b.inv);
+            for (int u = 0; u < ROUNDS; ++u) {
+                float f[V];
+                unpack16<T>(v[i][u], f);
+                uint32_t m = 0;
+#pragma unroll
+                for (int j = 0; j < V; ++j) m = max(m, abs_bits(f[j]));
+#pragma unroll
+                for (int o = LPB / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+                const BlockScale k = block_scale(m);
+                const int cb = cb0 + u * BPW + lane / LPB;
+                if (lane % LPB == 0) s_scale[b][u * BPW + lane / LPB][warp * RPW + i] = k.s;
+                if (r < rows && cb < Cb) {
+                    uint8_t* o = q + (mat * rows + r) * Cp + cb * kQ + (lane % LPB) * V;
+                    if constexpr (V == 8) *(uint2*)o = make_uint2(e4m3x4(f[0], f[1], f[2], f[3], k.inv), e4m3x4(f[4], f[5], f[6], f[7], k.inv));
+                    else *(uint32_t*)o = e4m3x4(f[0], f[1], f[2], f[3], k.inv);
+                }
             }
         }
-    }
-    __syncthreads();
-    if (threadIdx.x < kBlocksPerCta * kRowsPerCta) {
-        const int cb = cb0 + threadIdx.x / kRowsPerCta;
-        const long long r = row0 + threadIdx.x % kRowsPerCta;
-        if (cb < Cb && r < rows) scale[(mat * Cb + cb) * rows + r] = s_scale[threadIdx.x / kRowsPerCta][threadIdx.x % kRowsPerCta];
+        if (group + splits < groups) load(group + splits);
+        __syncthreads();                              // (two buffers: the next group's scales wait for nobody)
+        if (threadIdx.x < kBlocksPerCta * kRowsPerCta) {
+            const int cb = cb0 + threadIdx.x / kRowsPerCta;
+            const long long r = row0 + threadIdx.x % kRowsPerCta;
+            if (cb < Cb && r < rows) scale[(mat * Cb + cb) * rows + r] = s_scale[b][threadIdx.x / kRowsPerCta][threadIdx.x % kRowsPerCta];
+        }
     }
 }
 
@@ -204,11 +212,15 @@ uoe_status launch_tile(int layout, int G, int R, int C, const void* x, void* q, 
 uoe_status launch_quantize_rows(const void* x, bool bf16, int G, long long rows, int C, void* q, float* scale, const SrcMap& map,
                                 const int* offsets, int n, const char* label, cudaStream_t s) {
     const int Cb = q_blocks(C), groups = (Cb + kBlocksPerCta - 1) / kBlocksPerCta, whole = ((size_t)C * (bf16 ? 2 : 4)) % 16 == 0;
-    const long long ctas = (long long)G * ((rows + kRowsPerCta - 1) / kRowsPerCta) * groups;
+    // CTAs of a row block: as many as keep some eight per SM; a row's columns are a loop otherwise
+    const long long row_ctas = (long long)G * ((rows + kRowsPerCta - 1) / kRowsPerCta);
+    int splits = groups;
+    while (splits > 1 && row_ctas * (splits / 2) >= 8ll * sm_count()) splits = (splits + 1) / 2;
+    const long long ctas = row_ctas * splits;
     if (ctas > 0x7fffffffll) return UOE_ERR_UNSUPPORTED;
     ProfScope ps(label, s);
-    if (bf16) launch_k(quantize_rows_kernel<__nv_bfloat16>, dim3((unsigned)ctas), dim3(256), 0, s, (const __nv_bfloat16*)x, (uint8_t*)q, scale, rows, C, Cb, groups, whole, map, offsets, n);
-    else launch_k(quantize_rows_kernel<float>, dim3((unsigned)ctas), dim3(256), 0, s, (const float*)x, (uint8_t*)q, scale, rows, C, Cb, groups, whole, map, offsets, n);
+    if (bf16) launch_k(quantize_rows_kernel<__nv_bfloat16>, dim3((unsigned)ctas), dim3(256), 0, s, (const __nv_bfloat16*)x, (uint8_t*)q, scale, rows, C, Cb, groups, splits, whole, map, offsets, n);
+    else launch_k(quantize_rows_kernel<float>, dim3((unsigned)ctas), dim3(256), 0, s, (const float*)x, (uint8_t*)q, scale, rows, C, Cb, groups, splits, whole, map, offsets, n);
     UOE_LAUNCHED();
     return UOE_OK;
 }
