@@ -335,6 +335,7 @@ uoe_status dispatch(const Fp8Gemm& g, int* status, cudaStream_t s) {
 
 uoe_status launch_fp8_gemm(const Fp8Gemm& g, int* status, cudaStream_t s) {
     if (g.n > kMaxExperts) return UOE_ERR_UNSUPPORTED;
+    if (fp8_is_skinny(g)) return launch_fp8_skinny(g, status, s);
     if (g.any_scale) return launch_fp8_gemm_any(g, status, s);
     if (g.wgrad) return dispatch<true, kFp8Store>(g, status, s);
     return g.epi == kFp8ActQuant ? dispatch<false, kFp8ActQuant>(g, status, s) : dispatch<false, kFp8Store>(g, status, s);

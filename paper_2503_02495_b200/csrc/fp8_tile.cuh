@@ -132,4 +132,8 @@ inline Fp8Args fp8_args(const Fp8Gemm& g, int* status) {
 // Factors of any size: blocks' products added outside the tensor cores (fp8_gemm_any_tcgen05.cu).
 uoe_status launch_fp8_gemm_any(const Fp8Gemm& g, int* status, cudaStream_t s);
 
+// Up to 64 rows of one matrix, scales of any size: split along the contraction (fp8_skinny_tcgen05.cu).
+bool fp8_is_skinny(const Fp8Gemm& g);
+uoe_status launch_fp8_skinny(const Fp8Gemm& g, int* status, cudaStream_t s);
+
 }  // namespace uoe
