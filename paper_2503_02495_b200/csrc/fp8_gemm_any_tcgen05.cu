@@ -31,7 +31,7 @@ template <int BN> struct Cfg {
     static constexpr int TMEM_COLS = 2 * BN;
     static constexpr int SCALES = BM + BN;            // floats of a block's scales: the rows', then the columns' (or column blocks')
     static constexpr int CTL_BYTES = 1024;
-    static constexpr int SMEM = STAGES * STAGE + 1024 /* alignment */ + CTL_BYTES + kScaleSlots * SCALES * 4;
+    static constexpr int SMEM = STAGES * STAGE + 1024 /* alignment */ + CTL_BYTES + kScaleSlots * SCALES * 4 + EPI_WARPS * kTurnBytes;
 };
 
 struct Ctl {
@@ -95,15 +95,14 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
         constexpr int CW = Cf::CW;
         const int quarter = warp & 3, half = (warp - 4) >> 2;
+        float* turn = s_scales + kScaleSlots * Cf::SCALES + (warp - 4) * (kTurnBytes / 4);
         int acc = 0, e = 0, slot = 0;
         uint32_t acc_phase = 0, slot_phase = 0;
         bool stop = false;
         for (int tile = blockIdx.x; tile < total && !stop; tile += gridDim.x) {
             int row0, col0, kb0, kbs;
             locate(tile, e, row0, col0, kb0, kbs);
-            const long long row = row0 + quarter * 32 + lane;
             const int col = col0 + half * CW;
-            const bool row_ok = row < a.M;
             float sum[CW];
 #pragma unroll
             for (int q = 0; q < CW; ++q) sum[q] = 0.f;
@@ -161,8 +160,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 if (++slot == kScaleSlots) { slot = 0; slot_phase ^= 1; }
             }
             if (stop) break;
-            if (!row_ok || col >= a.N) continue;
-            store_tile<CW, WGRAD, EPI>(a, sum, e, row, col);
+            store_tile<CW, WGRAD, EPI>(a, sum, e, row0 + quarter * 32, a.M, col, turn);
+            __syncwarp();
         }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");

@@ -36,7 +36,7 @@ template <int BN, bool PAIR> struct Cfg {
     static constexpr int EPI_WARPS = 8, THREADS = 128 + 128 + 32 * EPI_WARPS;
     static constexpr int TMEM_COLS = 512, SF_COL = 256, SF_STRIDE = 16, SFB = 8;      // scales of stage s: A at SF_COL + 16 s, B 8 behind
     static constexpr int SF_BYTES = 512 + 4 * BN;                     // a stage's scale words: A's 128 rows, then B's BN
-    static constexpr int SMEM = STAGES * (STAGE + SF_BYTES) + 1024 /* alignment */ + 1024 /* control */;
+    static constexpr int SMEM = STAGES * (STAGE + SF_BYTES) + 1024 /* alignment */ + 1024 /* control */ + EPI_WARPS * kTurnBytes;
 };
 
 struct Ctl {
@@ -116,6 +116,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         constexpr int CW = Cf::CW;
         const int quarter = warp & 3, half = (warp - 8) >> 2;
+        float* turn = (float*)(s_sf + Cf::STAGES * Cf::SF_BYTES + (warp - 8) * kTurnBytes);
         int acc = 0, e = 0;
         uint32_t acc_phase = 0;
         for (int tile = worker; tile < total; tile += workers) {
@@ -139,8 +140,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
 #pragma unroll
                 for (int q = 0; q < CW; ++q) sum[q] = 0.f;
             }
-            const int row = t.row0 + quarter * 32 + lane, col = t.col0 + half * CW;
-            if (row < t.row_end && col < a.N) store_tile<CW, WGRAD, EPI>(a, sum, e, row, col);
+            store_tile<CW, WGRAD, EPI>(a, sum, e, t.row0 + quarter * 32, t.row_end, t.col0 + half * CW, turn);
             __syncwarp();
         }
     } else if (warp >= 4) {

@@ -58,17 +58,24 @@ __device__ __forceinline__ void load_regions(Regions& g, const Fp8Args& a, int m
     if (lane == 0 && bad) set_status(a.status, UOE_ERR_DEVICE_INDEX);
 }
 
-// One thread's CW sums of row `row`, columns col .. col + CW (within the rows and columns there are: row < M, col < N).
+// Shared memory through which a write-out warp turns its rows where they cannot leave in 32-byte pieces: 32 rows of 16 columns.
+constexpr int kTurnPitch = 17, kTurnBytes = 32 * kTurnPitch * 4;
+
+// A warp's sums: CW of row `row0` + lane in every lane, columns col .. col + CW.  Rows from row_end and columns from N on are not stored.
 template <int CW, bool WGRAD, int EPI>
-__device__ __forceinline__ void store_tile(const Fp8Args& a, float* sum, int e, long long row, int col) {
+__device__ __forceinline__ void store_tile(const Fp8Args& a, float* sum, int e, long long row0, long long row_end, int col, float* turn) {
+    const int lane = threadIdx.x & 31;
+    const long long row = row0 + lane;
+    if (col >= a.N) return;
+    if (!WGRAD && a.bias) {
+#pragma unroll
+        for (int q = 0; q < CW; ++q)
+            if (col + q < a.N) sum[q] += to_f32(a.bias[(size_t)e * a.N + col + q]);
+    }
     if constexpr (EPI == kFp8ActQuant) {
         static_assert(EPI != kFp8ActQuant || (!WGRAD && CW == kQ), "a thread holds one block of the result");
+        if (row >= row_end) return;
         uint32_t m = 0;
-        if (a.bias) {
-#pragma unroll
-            for (int q = 0; q < CW; ++q)
-                if (col + q < a.N) sum[q] += to_f32(a.bias[(size_t)e * a.N + col + q]);
-        }
         act_precise_n<CW>(sum, a.act);
 #pragma unroll
         for (int q = 0; q < CW; ++q) m = max(m, abs_bits(sum[q]));
@@ -85,33 +92,41 @@ __device__ __forceinline__ void store_tile(const Fp8Args& a, float* sum, int e, 
         }
     } else {
         const size_t at = ((WGRAD ? (size_t)e * a.M : 0) + row) * a.N + col;
-        if (a.bias) {
-#pragma unroll
-            for (int q = 0; q < CW; ++q)
-                if (col + q < a.N) sum[q] += to_f32(a.bias[(size_t)e * a.N + col + q]);
-        }
-        if (a.out_bf16) {
-            __nv_bfloat16* o = (__nv_bfloat16*)a.C + at;
-            if (a.vec && col + CW <= a.N) {
+        if (a.vec && col + CW <= a.N) {
+            if (row >= row_end) return;
+            if (!WGRAD && a.out_bf16) {
+                __nv_bfloat16* o = (__nv_bfloat16*)a.C + at;
                 const bool whole = sector_aligned(o);
 #pragma unroll
                 for (int q = 0; q < CW; q += 16) st_sector(o + q, pack16<__nv_bfloat16>(sum + q), pack16<__nv_bfloat16>(sum + q + 8), whole);
             } else {
-#pragma unroll
-                for (int q = 0; q < CW; ++q)
-                    if (col + q < a.N) o[q] = __float2bfloat16_rn(sum[q]);
-            }
-        } else {
-            float* o = (float*)a.C + at;
-            if (a.vec && col + CW <= a.N) {
+                float* o = (float*)a.C + at;
                 const bool whole = sector_aligned(o);
 #pragma unroll
                 for (int q = 0; q < CW; q += 8) st_sector(o + q, pack16<float>(sum + q), pack16<float>(sum + q + 4), whole);
-            } else {
-#pragma unroll
-                for (int q = 0; q < CW; ++q)
-                    if (col + q < a.N) o[q] = sum[q];
             }
+        } else {
+            // rows that start anywhere: 16 columns of two rows per store (a row per lane, 4 bytes of 32 rows each: 1334 x 333 x 1000,
+            // float32, 15 us)
+#pragma unroll
+            for (int c = 0; c < CW; c += 16) {
+                __syncwarp();
+#pragma unroll
+                for (int q = 0; q < 16; ++q) turn[lane * kTurnPitch + q] = sum[c + q];
+                __syncwarp();
+                const int cc = col + c + (lane & 15);
+                if (cc >= a.N) continue;
+#pragma unroll 4
+                for (int i = 0; i < 16; ++i) {
+                    const int r = 2 * i + (lane >> 4);
+                    if (row0 + r >= row_end) break;
+                    const float v = turn[r * kTurnPitch + (lane & 15)];
+                    const size_t to = ((WGRAD ? (size_t)e * a.M : 0) + row0 + r) * a.N + cc;
+                    if (!WGRAD && a.out_bf16) ((__nv_bfloat16*)a.C)[to] = __float2bfloat16_rn(v);
+                    else ((float*)a.C)[to] = v;
+                }
+            }
+            __syncwarp();
         }
     }
 }
