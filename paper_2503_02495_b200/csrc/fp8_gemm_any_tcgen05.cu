@@ -44,7 +44,8 @@ static_assert(sizeof(Ctl) <= 1024, "control block");
 
 template <int BN, bool WGRAD, int EPI>
 __global__ void __launch_bounds__(Cfg<BN>::THREADS, 1)
-fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ Fp8Args a) {
+fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmC,
+                const __grid_constant__ Fp8Args a) {
     using Cf = Cfg<BN>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -160,7 +161,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 if (++slot == kScaleSlots) { slot = 0; slot_phase ^= 1; }
             }
             if (stop) break;
-            store_tile<CW, WGRAD, EPI>(a, sum, e, row0 + quarter * 32, a.M, col, turn);
+            store_tile<CW, WGRAD, EPI>(a, &tmC, sum, e, row0 + quarter * 32, a.M, col, turn);
             __syncwarp();
         }
     } else {
@@ -244,6 +245,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             asm volatile("cp.async.wait_all;" ::: "memory");      // none in flight when the CTA exits
         }
     }
+    if (warp >= 4 && lane == 0) bulk_wait_all();        // this warp's tensor stores are complete
     tc_fence_before();
     __syncthreads();
     if (warp == 1) {
@@ -274,12 +276,14 @@ uoe_status launch_one(const Fp8Gemm& g, int* status, cudaStream_t s) {
         if (!make_tmap(&tmB, g.B, 3, dims, str, box, CU_TENSOR_MAP_DATA_TYPE_UINT8)) return UOE_ERR_CUDA;
     }
     const Fp8Args a = fp8_args(g, status);
+    CUtensorMap tmC = tmA;
+    if (g.epi == kFp8Store && a.vec && !result_map(&tmC, g)) return UOE_ERR_CUDA;
     const long long m_tiles = (g.M + BM - 1) / BM, n_tiles = (g.N + BN - 1) / BN;
     const long long tiles = m_tiles * n_tiles * (g.wgrad ? g.n : 1);
     if (tiles > 0x3fffffffll) return UOE_ERR_UNSUPPORTED;
     const int grid = (int)(tiles < sm_count() ? tiles : sm_count());
     ProfScope ps(g.label, s);
-    launch_k(kern, dim3(grid), dim3(Cf::THREADS), (size_t)Cf::SMEM, s, tmA, tmB, a);
+    launch_k(kern, dim3(grid), dim3(Cf::THREADS), (size_t)Cf::SMEM, s, tmA, tmB, tmC, a);
     UOE_LAUNCHED();
     return UOE_OK;
 }

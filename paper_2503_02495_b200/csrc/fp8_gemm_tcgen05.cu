@@ -58,7 +58,8 @@ __device__ __forceinline__ uint32_t exponent_word(float s, bool there, bool& bad
 
 template <int BN, bool WGRAD, int EPI, bool PAIR>
 __global__ void __launch_bounds__(Cfg<BN, PAIR>::THREADS, 1)
-fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ Fp8Args a) {
+fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmC,
+                const __grid_constant__ Fp8Args a) {
     using Cf = Cfg<BN, PAIR>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -140,7 +141,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
 #pragma unroll
                 for (int q = 0; q < CW; ++q) sum[q] = 0.f;
             }
-            store_tile<CW, WGRAD, EPI>(a, sum, e, t.row0 + quarter * 32, t.row_end, t.col0 + half * CW, turn);
+            store_tile<CW, WGRAD, EPI>(a, &tmC, sum, e, t.row0 + quarter * 32, t.row_end, t.col0 + half * CW, turn);
             __syncwarp();
         }
     } else if (warp >= 4) {
@@ -268,6 +269,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             }
         }
     }
+    if (warp >= 8 && lane == 0) bulk_wait_all();        // this warp's tensor stores are complete
     tc_fence_before();
     __syncthreads();
     if constexpr (PAIR) cluster_sync_all();           // neither CTA leaves while the other may still arrive on its barriers or read its tiles
@@ -301,6 +303,8 @@ uoe_status launch_one(const Fp8Gemm& g, int* status, cudaStream_t s) {
         if (!make_tmap(&tmB, g.B, 3, dims, str, box, CU_TENSOR_MAP_DATA_TYPE_UINT8)) return UOE_ERR_CUDA;
     }
     const Fp8Args a = fp8_args(g, status);
+    CUtensorMap tmC = tmA;
+    if (g.epi == kFp8Store && a.vec && !result_map(&tmC, g)) return UOE_ERR_CUDA;
     const long long tiles = ((g.M + Cf::TILE - 1) / Cf::TILE + (PAIR && !g.wgrad ? g.n : 0)) * ((g.N + BN - 1) / BN) * (g.wgrad ? g.n : 1);
     if (tiles > 0x3fffffffll) return UOE_ERR_UNSUPPORTED;
     ProfScope ps(g.label, s);
@@ -314,9 +318,9 @@ uoe_status launch_one(const Fp8Gemm& g, int* status, cudaStream_t s) {
             pairs_cache.set(dev, v);
         }
         const long long pairs = pairs_cache.get(dev);
-        launch_k_pairs(kern, dim3(2 * (unsigned)(tiles < pairs ? tiles : pairs)), dim3(Cf::THREADS), (size_t)Cf::SMEM, s, tmA, tmB, a);
+        launch_k_pairs(kern, dim3(2 * (unsigned)(tiles < pairs ? tiles : pairs)), dim3(Cf::THREADS), (size_t)Cf::SMEM, s, tmA, tmB, tmC, a);
     } else {
-        launch_k(kern, dim3((unsigned)(tiles < sm_count() ? tiles : sm_count())), dim3(Cf::THREADS), (size_t)Cf::SMEM, s, tmA, tmB, a);
+        launch_k(kern, dim3((unsigned)(tiles < sm_count() ? tiles : sm_count())), dim3(Cf::THREADS), (size_t)Cf::SMEM, s, tmA, tmB, tmC, a);
     }
     UOE_LAUNCHED();
     return UOE_OK;

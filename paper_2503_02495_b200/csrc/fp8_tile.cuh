@@ -1,6 +1,8 @@
 // What the kernels for products of 8-bit operands share: arguments, the experts' regions, what becomes of a tile's sums.
 #pragma once
 #include "fp8.cuh"
+#include "tc.cuh"
+#include "tmap.cuh"
 
 namespace uoe {
 
@@ -58,12 +60,20 @@ __device__ __forceinline__ void load_regions(Regions& g, const Fp8Args& a, int m
     if (lane == 0 && bad) set_status(a.status, UOE_ERR_DEVICE_INDEX);
 }
 
-// Shared memory through which a write-out warp turns its rows where they cannot leave in 32-byte pieces: 32 rows of 16 columns.
-constexpr int kTurnPitch = 17, kTurnBytes = 32 * kTurnPitch * 4;
+// Shared memory of a write-out warp: 32 rows of 64 bytes (swizzled, for a tensor store), or of 16 columns and a gap.
+constexpr int kTurnPitch = 17, kTurnBytes = 2560;
+static_assert(kTurnBytes >= 32 * kTurnPitch * 4 && kTurnBytes % 512 == 0, "");
+// C as [n][rows][N] in pieces of 32 rows x 64 bytes (rows of C are multiples of 16 bytes: Fp8Args::vec)
+inline bool result_map(CUtensorMap* tm, const Fp8Gemm& g) {
+    const uint64_t size = g.out_bf16 ? 2 : 4;
+    const uint64_t dims[3] = {(uint64_t)g.N, (uint64_t)g.M, (uint64_t)(g.wgrad ? g.n : 1)}, str[2] = {(uint64_t)g.N * size, (uint64_t)g.N * g.M * size};
+    const uint32_t box[3] = {(uint32_t)(64 / size), 32, 1};
+    return make_tmap(tm, g.C, 3, dims, str, box, g.out_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, CU_TENSOR_MAP_SWIZZLE_64B);
+}
 
 // A warp's sums: CW of row `row0` + lane in every lane, columns col .. col + CW.  Rows from row_end and columns from N on are not stored.
 template <int CW, bool WGRAD, int EPI>
-__device__ __forceinline__ void store_tile(const Fp8Args& a, float* sum, int e, long long row0, long long row_end, int col, float* turn) {
+__device__ __forceinline__ void store_tile(const Fp8Args& a, const CUtensorMap* tmC, float* sum, int e, long long row0, long long row_end, int col, float* turn) {
     const int lane = threadIdx.x & 31;
     const long long row = row0 + lane;
     if (col >= a.N) return;
@@ -91,19 +101,37 @@ __device__ __forceinline__ void store_tile(const Fp8Args& a, float* sum, int e, 
             st_sector(o + q, make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]), whole);
         }
     } else {
-        const size_t at = ((WGRAD ? (size_t)e * a.M : 0) + row) * a.N + col;
-        if (a.vec && col + CW <= a.N) {
-            if (row >= row_end) return;
+        if (a.vec) {
+            // tensor stores of 32 rows x 64 bytes, which leave behind the arithmetic on the next piece (rows and columns past C are clipped;
+            // a region is whole blocks of 32 rows).  A row per lane and 32 bytes of it per store: 32768 x 4096 x 1024 127 us
+            if (row0 >= row_end) return;
+            auto put = [&](const uint4* v, int c) {
+                if (lane == 0) tc::bulk_wait_read();
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) *(uint4*)((uint8_t*)turn + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)) = v[i];
+                tc::fence_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    tc::tma_store_3d(tmC, turn, col + c, (int)row0, WGRAD ? e : 0);
+                    tc::bulk_commit();
+                }
+            };
             if (!WGRAD && a.out_bf16) {
-                __nv_bfloat16* o = (__nv_bfloat16*)a.C + at;
-                const bool whole = sector_aligned(o);
 #pragma unroll
-                for (int q = 0; q < CW; q += 16) st_sector(o + q, pack16<__nv_bfloat16>(sum + q), pack16<__nv_bfloat16>(sum + q + 8), whole);
+                for (int c = 0; c < CW; c += 32) {
+                    if (col + c >= a.N) break;
+                    const uint4 v[4] = {pack16<__nv_bfloat16>(sum + c), pack16<__nv_bfloat16>(sum + c + 8), pack16<__nv_bfloat16>(sum + c + 16),
+                                        pack16<__nv_bfloat16>(sum + c + 24)};
+                    put(v, c);
+                }
             } else {
-                float* o = (float*)a.C + at;
-                const bool whole = sector_aligned(o);
 #pragma unroll
-                for (int q = 0; q < CW; q += 8) st_sector(o + q, pack16<float>(sum + q), pack16<float>(sum + q + 4), whole);
+                for (int c = 0; c < CW; c += 16) {
+                    if (col + c >= a.N) break;
+                    const uint4 v[4] = {pack16<float>(sum + c), pack16<float>(sum + c + 4), pack16<float>(sum + c + 8), pack16<float>(sum + c + 12)};
+                    put(v, c);
+                }
             }
         } else {
             // rows that start anywhere: 16 columns of two rows per store (a row per lane, 4 bytes of 32 rows each: 1334 x 333 x 1000,
