@@ -8,6 +8,7 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <utility>
 
 #include "device_once.h"
 #include "uoe.h"
@@ -101,9 +102,9 @@ inline cudaError_t launch_k(void (*kern)(KArgs...), dim3 grid, dim3 block, size_
     return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
 }
 
-// The same for a kernel of CTA pairs: clusters of two CTAs along x (the grid's x extent is even).
+// The same for a kernel of clusters along x (the grid's x extent is a multiple of `cluster`).
 template <typename... KArgs, typename... Args>
-inline cudaError_t launch_k_pairs(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, Args&&... args) {
+inline cudaError_t launch_k_cluster(void (*kern)(KArgs...), dim3 grid, dim3 block, int cluster, size_t smem, cudaStream_t s, Args&&... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = block;
@@ -113,12 +114,18 @@ inline cudaError_t launch_k_pairs(void (*kern)(KArgs...), dim3 grid, dim3 block,
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = 2;
+    at[1].val.clusterDim.x = cluster;
     at[1].val.clusterDim.y = 1;
     at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
+}
+
+// The same for CTA pairs (the grid's x extent is even).
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_k_pairs(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, Args&&... args) {
+    return launch_k_cluster(kern, grid, block, 2, smem, s, std::forward<Args>(args)...);
 }
 
 // How many CTA pairs of a kernel can be resident on the device at once.

@@ -24,6 +24,7 @@ namespace {
 using namespace tc;
 
 constexpr int BM = 128;
+constexpr int kSplitPitch = 132;          // floats of a row of a split tile's sums (where the stages were)
 
 template <int BN, bool PAIR> struct Cfg {
     static_assert(!PAIR || BN == 256, "a pair works 256 x 256");
@@ -56,7 +57,7 @@ __device__ __forceinline__ uint32_t exponent_word(float s, bool there, bool& bad
     return __byte_perm(pow2 ? e : 255u, 0, 0);
 }
 
-template <int BN, bool WGRAD, int EPI, bool PAIR>
+template <int BN, bool WGRAD, int EPI, bool PAIR, bool SPLIT>
 __global__ void __launch_bounds__(Cfg<BN, PAIR>::THREADS, 1)
 fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmC,
                 const __grid_constant__ Fp8Args a) {
@@ -66,8 +67,11 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     Ctl* ctl = (Ctl*)(smem + Cf::STAGES * Cf::STAGE);
     volatile int* abort_flag = &ctl->abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    static_assert(!SPLIT || (BN == 128 && !PAIR && EPI == kFp8Store), "a split tile is 128 x 128");
     const int rank = PAIR ? (int)cluster_ctarank() : 0;
-    const int worker = PAIR ? blockIdx.x >> 1 : blockIdx.x, workers = PAIR ? gridDim.x >> 1 : gridDim.x;
+    const int share = SPLIT ? (int)cluster_ctarank() : 0, shares = SPLIT ? a.split : 1;      // of a tile's contraction
+    const int worker = PAIR ? blockIdx.x >> 1 : SPLIT ? blockIdx.x / shares : blockIdx.x;
+    const int workers = PAIR ? gridDim.x >> 1 : SPLIT ? gridDim.x / shares : gridDim.x;
     const int n = a.n;
     constexpr int CTAS = PAIR ? 2 : 1;
     if (threadIdx.x == 0) {
@@ -109,6 +113,11 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         t.col0 = (tile - rt * n_tiles) * BN;
         t.kb0 = WGRAD ? ctl->reg.offs[e] / kQ : 0;
         t.kbs = WGRAD ? (ctl->reg.offs[e + 1] - ctl->reg.offs[e]) / kQ : a.Kb;
+        if constexpr (SPLIT) {
+            const int lo = (int)((long long)t.kbs * share / shares), hi = (int)((long long)t.kbs * (share + 1) / shares);
+            t.kb0 += lo;
+            t.kbs = hi - lo;
+        }
         return t;
     };
 
@@ -117,7 +126,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         constexpr int CW = Cf::CW;
         const int quarter = warp & 3, half = (warp - 8) >> 2;
-        float* turn = (float*)(s_sf + Cf::STAGES * Cf::SF_BYTES + (warp - 8) * kTurnBytes);
+        [[maybe_unused]] float* turn = (float*)(s_sf + Cf::STAGES * Cf::SF_BYTES + (warp - 8) * kTurnBytes);
         int acc = 0, e = 0;
         uint32_t acc_phase = 0;
         for (int tile = worker; tile < total; tile += workers) {
@@ -141,7 +150,13 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
 #pragma unroll
                 for (int q = 0; q < CW; ++q) sum[q] = 0.f;
             }
-            store_tile<CW, WGRAD, EPI>(a, &tmC, sum, e, t.row0 + quarter * 32, t.row_end, t.col0 + half * CW, turn);
+            if constexpr (SPLIT) {                    // (its only tile: the stages have all been read)
+                float* o = (float*)smem + (quarter * 32 + lane) * kSplitPitch + half * CW;
+#pragma unroll
+                for (int q = 0; q < CW; q += 4) *(float4*)(o + q) = make_float4(sum[q], sum[q + 1], sum[q + 2], sum[q + 3]);
+            } else {
+                store_tile<CW, WGRAD, EPI>(a, &tmC, sum, e, t.row0 + quarter * 32, t.row_end, t.col0 + half * CW, turn);
+            }
             __syncwarp();
         }
     } else if (warp >= 4) {
@@ -156,7 +171,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             const Tile t = locate(tile, e);
             const int rows = t.row_end - t.row0, cols = a.N - t.col0;
             const float* sa = a.sa + (size_t)t.kb0 * a.M + t.row0;
-            const float* sb = WGRAD ? a.sb + (size_t)t.kb0 * a.N + t.col0 : a.sb + ((size_t)e * a.Nb + t.col0 / kQ) * a.Kb;
+            const float* sb = WGRAD ? a.sb + (size_t)t.kb0 * a.N + t.col0 : a.sb + ((size_t)e * a.Nb + t.col0 / kQ) * a.Kb + t.kb0;
             float ra[4], rb[NB];                                      // (whatever is there where there are no rows of this expert, or no columns)
             auto ask = [&](int kb) {
 #pragma unroll
@@ -272,6 +287,27 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     if (warp >= 8 && lane == 0) bulk_wait_all();        // this warp's tensor stores are complete
     tc_fence_before();
     __syncthreads();
+    if constexpr (SPLIT) {                            // the shares' sums, in order; a CTA stores its part of the rows
+        cluster_sync_all();
+        if (worker < total) {
+            int e = 0;
+            const Tile t = locate(worker, e);
+            for (int r = BM * share / shares + warp; r < BM * (share + 1) / shares; r += Cf::THREADS / 32) {
+                const long long row = t.row0 + r;
+                if (row >= t.row_end) break;
+#pragma unroll
+                for (int c = lane; c < BN; c += 32) {
+                    if (t.col0 + c >= a.N) break;
+                    float v = a.bias ? to_f32(a.bias[(size_t)e * a.N + t.col0 + c]) : 0.f;
+                    for (int q = 0; q < shares; ++q) v += ld_cluster_f32((const float*)smem + r * kSplitPitch + c, q);
+                    const size_t at = ((WGRAD ? (size_t)e * a.M : 0) + row) * a.N + t.col0 + c;
+                    if (!WGRAD && a.out_bf16) ((__nv_bfloat16*)a.C)[at] = __float2bfloat16_rn(v);
+                    else ((float*)a.C)[at] = v;
+                }
+            }
+        }
+        cluster_sync_all();                           // nobody's shared memory goes while another CTA may read it
+    }
     if constexpr (PAIR) cluster_sync_all();           // neither CTA leaves while the other may still arrive on its barriers or read its tiles
     if (warp == 1) {
         __syncwarp();
@@ -280,12 +316,12 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     }
 }
 
-template <int BN, bool WGRAD, int EPI, bool PAIR>
-uoe_status launch_one(const Fp8Gemm& g, int* status, cudaStream_t s) {
+template <int BN, bool WGRAD, int EPI, bool PAIR, bool SPLIT = false>
+uoe_status launch_one(const Fp8Gemm& g, int* status, cudaStream_t s, int split = 1) {
     using Cf = Cfg<BN, PAIR>;
     static DeviceOnce once;
     static DeviceValue pairs_cache;
-    auto kern = fp8_gemm_kernel<BN, WGRAD, EPI, PAIR>;
+    auto kern = fp8_gemm_kernel<BN, WGRAD, EPI, PAIR, SPLIT>;
     const uoe_status st = smem_opt_in(once, kern, Cf::SMEM);
     if (st != UOE_OK) return st;
     const uint64_t Kp = (uint64_t)((g.K + kQ - 1) / kQ * kQ);
@@ -302,7 +338,8 @@ uoe_status launch_one(const Fp8Gemm& g, int* status, cudaStream_t s) {
         const uint32_t box[3] = {kQ, Cf::BN_CTA, 1};
         if (!make_tmap(&tmB, g.B, 3, dims, str, box, CU_TENSOR_MAP_DATA_TYPE_UINT8)) return UOE_ERR_CUDA;
     }
-    const Fp8Args a = fp8_args(g, status);
+    Fp8Args a = fp8_args(g, status);
+    a.split = split;
     CUtensorMap tmC = tmA;
     if (g.epi == kFp8Store && a.vec && !result_map(&tmC, g)) return UOE_ERR_CUDA;
     const long long tiles = ((g.M + Cf::TILE - 1) / Cf::TILE + (PAIR && !g.wgrad ? g.n : 0)) * ((g.N + BN - 1) / BN) * (g.wgrad ? g.n : 1);
@@ -319,6 +356,8 @@ uoe_status launch_one(const Fp8Gemm& g, int* status, cudaStream_t s) {
         }
         const long long pairs = pairs_cache.get(dev);
         launch_k_pairs(kern, dim3(2 * (unsigned)(tiles < pairs ? tiles : pairs)), dim3(Cf::THREADS), (size_t)Cf::SMEM, s, tmA, tmB, tmC, a);
+    } else if constexpr (SPLIT) {
+        launch_k_cluster(kern, dim3((unsigned)tiles * split), dim3(Cf::THREADS), split, (size_t)Cf::SMEM, s, tmA, tmB, tmC, a);
     } else {
         launch_k(kern, dim3((unsigned)(tiles < sm_count() ? tiles : sm_count())), dim3(Cf::THREADS), (size_t)Cf::SMEM, s, tmA, tmB, tmC, a);
     }
@@ -331,7 +370,18 @@ uoe_status dispatch(const Fp8Gemm& g, int* status, cudaStream_t s) {
     const long long cols256 = (g.N + 255) / 256, mats = g.wgrad ? g.n : 1;
     if (g.N > 128 && (g.M + 255) / 256 * cols256 * mats >= sm_count()) return launch_one<256, WGRAD, EPI, true>(g, status, s);
     if (EPI == kFp8ActQuant || (g.N > 128 && (g.M + 127) / 128 * cols256 * mats >= sm_count())) return launch_one<256, WGRAD, EPI, false>(g, status, s);
-    if constexpr (EPI != kFp8ActQuant) return launch_one<128, WGRAD, EPI, false>(g, status, s);
+    if constexpr (EPI != kFp8ActQuant) {
+        // Tiles that leave SMs idle and have far to go: the contraction of a tile in up to eight parts, a CTA of a cluster each, from 24 blocks on
+        // (a block is 0.3 us, the sums' meeting some 4; wgrad: an expert's rows are an even share, as far as the host knows).  wgrad 128 x 128 x
+        // 30000 55.7 -> 13.5 us, 128 x 100 x 4096 15.1 -> 8.1, 300 x 1000 x 4096 12.8 -> 10.3; of 16 blocks, in two, 1000 x 500 x 2000 9.1 -> 11.4.
+        const long long tiles = (g.M + 127) / 128 * ((g.N + 127) / 128) * mats, blocks = (g.K + kQ - 1) / kQ / mats;
+        // (clusters of eight CTAs, one per SM, find room for two thirds of the SMs at once, of four for seven eighths)
+        const int sms = sm_count();
+        int split = 8;
+        while (split > 1 && (tiles * split > (split == 8 ? sms * 2 / 3 : split == 4 ? sms * 7 / 8 : sms) || blocks < 24 || blocks < 4 * split)) split >>= 1;
+        if (split > 1) return launch_one<128, WGRAD, EPI, false, true>(g, status, s, split);
+        return launch_one<128, WGRAD, EPI, false>(g, status, s);
+    }
     return UOE_ERR_UNSUPPORTED;
 }
 

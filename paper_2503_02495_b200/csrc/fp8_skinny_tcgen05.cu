@@ -149,11 +149,7 @@ fp8_skinny_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
         const int r = q / kCols, c = q % kCols;
         if (c0 + c >= a.N) continue;
         float s = 0.f;
-        for (int i = 0; i < S; ++i) {
-            float v;
-            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(map_to_cta(cta + r * Cf::PITCH + c, first + i)) : "memory");
-            s += v;
-        }
+        for (int i = 0; i < S; ++i) s += ld_cluster_f32(cta + r * Cf::PITCH + c, first + i);
         const size_t at = (size_t)r * a.N + c0 + c;
         if (a.out_bf16) ((__nv_bfloat16*)a.C)[at] = __float2bfloat16_rn(s);
         else ((float*)a.C)[at] = s;
@@ -187,22 +183,8 @@ uoe_status launch_one(const Fp8Gemm& g, int* status, cudaStream_t s) {
     while (S > 1 && (a.Kb < S || tiles * S > 2ll * sm_count())) S >>= 1;
     const long long ctas = (tiles * S + kCluster - 1) / kCluster * kCluster;
     if (ctas > 0x7fffffffll) return UOE_ERR_UNSUPPORTED;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)ctas);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = kCluster;
-    at[1].val.clusterDim.y = 1;
-    at[1].val.clusterDim.z = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 2;
     ProfScope ps(g.label, s);
-    cudaLaunchKernelEx(&cfg, kern, tmW, tmA, a, S);
+    launch_k_cluster(kern, dim3((unsigned)ctas), dim3(kThreads), kCluster, smem, s, tmW, tmA, a, S);
     UOE_LAUNCHED();
     return UOE_OK;
 }

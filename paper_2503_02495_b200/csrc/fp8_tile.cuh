@@ -21,6 +21,7 @@ struct Fp8Args {
     uint8_t* q;
     float* qs;
     long long ldq;
+    int split;                        // CTAs that share a tile's contraction
     int* status;
 };
 

@@ -36,12 +36,6 @@ struct TokArgs {
 template <int WT> struct Elem { using T = __nv_bfloat16; };
 template <> struct Elem<kF32> { using T = float; };
 
-__device__ __forceinline__ float ld_cluster(const float* p, uint32_t rank) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(map_to_cta(p, rank)) : "memory");
-    return v;
-}
-
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
@@ -170,7 +164,7 @@ __device__ void route_tokens(const TokArgs& a, int t0, int Tn, int rank, float* 
         if (lane < n) {
             v = 0.f;
 #pragma unroll
-            for (int p = 0; p < CL; ++p) v += ld_cluster(part + tok * n + lane, p);
+            for (int p = 0; p < CL; ++p) v += ld_cluster_f32(part + tok * n + lane, p);
         }
         float mx = v;
 #pragma unroll
@@ -253,26 +247,6 @@ __device__ __forceinline__ void read_routing(const TokArgs& a, Routed& R, int Tn
     for (int q = threadIdx.x; q < routed_words(Tn); q += blockDim.x) ((uint32_t*)&R)[q] = __ldcg((const uint32_t*)(a.routed + blockIdx.z) + q);
     __syncthreads();
 }
-
-template <int CL, typename... KArgs, typename... Args>
-cudaError_t launch_clusters(void (*kern)(KArgs...), dim3 grid, int threads, size_t smem, cudaStream_t s, Args&&... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = CL;
-    at[1].val.clusterDim.y = 1;
-    at[1].val.clusterDim.z = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
-}
-
 
 // CTAs of a tile: the largest split that leaves every CTA a unit of the contraction and no more CTAs than the SMs hold.
 inline int split_of(int units, long long tiles, int cluster, int ctas_per_sm) {

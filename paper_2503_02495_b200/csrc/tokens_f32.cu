@@ -143,7 +143,7 @@ first_layer_f32_kernel(const TokArgs a, int S) {
             const int tok = q / kCols, col = c0 + q % kCols;
             if (col >= a.d_e || !((R.of[slot] >> tok) & 1)) continue;
             float h = a.b1 ? ((const float*)a.b1)[(size_t)e * a.d_e + col] : 0.f;
-            for (int s = 0; s < S; ++s) h += ld_cluster(sm.cta + q, first + s);
+            for (int s = 0; s < S; ++s) h += ld_cluster_f32(sm.cta + q, first + s);
             out[(size_t)tok * a.d_e + col] = act_precise(h, a.act);
         }
     }
@@ -186,7 +186,7 @@ second_layer_f32_kernel(const TokArgs a, int S) {
         const int tok = q / kCols, col = c0 + q % kCols;
         if (col >= a.d) continue;
         float s = 0.f;
-        for (int r = 0; r < S; ++r) s += ld_cluster(sm.cta + q, first + r);
+        for (int r = 0; r < S; ++r) s += ld_cluster_f32(sm.cta + q, first + r);
         if (a.b2)
             for (uint32_t m = R.mask[tok]; m; m &= m - 1) {
                 const int e = __ffs(m) - 1;
@@ -213,14 +213,14 @@ uoe_status launch_layers(const TokArgs& a, cudaStream_t s) {
         const long long tiles = chosen * ((a.d_e + kCols - 1) / kCols);
         const int S = split_of((a.d + kStep - 1) / kStep, tiles * groups, kCluster, 1);
         ProfScope ps("tokens_first", s);
-        launch_clusters<kCluster>(first_layer_f32_kernel<TG>, grid(tiles, S), kThreads, smem, s, a, S);
+        launch_k_cluster(first_layer_f32_kernel<TG>, grid(tiles, S), dim3(kThreads), kCluster, smem, s, a, S);
         UOE_LAUNCHED();
     }
     {
         const long long tiles = (a.d + kCols - 1) / kCols;
         const int S = split_of(a.k * ((a.d_e + kStep - 1) / kStep), tiles * groups, kCluster, 1);
         ProfScope ps("tokens_second", s);
-        launch_clusters<kCluster>(second_layer_f32_kernel<TG>, grid(tiles, S), kThreads, smem, s, a, S);
+        launch_k_cluster(second_layer_f32_kernel<TG>, grid(tiles, S), dim3(kThreads), kCluster, smem, s, a, S);
         UOE_LAUNCHED();
     }
     return UOE_OK;

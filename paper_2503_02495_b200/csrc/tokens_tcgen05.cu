@@ -336,7 +336,7 @@ first_layer_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
             for (int v = 0; v < W; ++v) {
                 const int col = c0 + W * lane + v;
                 h[v] = 0.f;
-                for (int s = 0; s < S; ++s) h[v] += ld_cluster(cta + tok * Cf::PITCH + W * lane + v, first + s);
+                for (int s = 0; s < S; ++s) h[v] += ld_cluster_f32(cta + tok * Cf::PITCH + W * lane + v, first + s);
                 if (a.b1 && col < a.d_e) h[v] += to_f32(((const bf16*)a.b1)[(size_t)e * a.d_e + col]);
                 // (half a step, 2^-9 of the value, like the hidden rows of uoe_mlp_forward)
                 h[v] = col < a.d_e ? to_f32(__float2bfloat16_rn(act_precise(h[v], a.act))) : 0.f;
@@ -383,7 +383,7 @@ second_layer_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
         const int tok = q / kCols, col = c0 + q % kCols;
         if (col >= a.d) continue;
         float s = 0.f;
-        for (int r = 0; r < S; ++r) s += ld_cluster(cta + tok * Cf::PITCH + q % kCols, first + r);
+        for (int r = 0; r < S; ++r) s += ld_cluster_f32(cta + tok * Cf::PITCH + q % kCols, first + r);
         if (a.b2)
             for (uint32_t m = R.mask[tok]; m; m &= m - 1) {
                 const int e = __ffs(m) - 1;
@@ -441,7 +441,7 @@ uoe_status launch_layers(const TokArgs& a, int* status, cudaStream_t s) {
         if (WT != kBf16) tmX = tmW;
         else if (!value_map(&tmX, a.x, a.T, a.d, 1, (size_t)a.T * a.d, NT)) return UOE_ERR_CUDA;
         ProfScope ps("tokens_first", s);
-        launch_clusters<Cf::CLUSTER>(first_layer_kernel<WT, NT>, grid(tiles, S), 32 * Cf::WARPS1, smem, s, tmW, tmX, a, S, status);
+        launch_k_cluster(first_layer_kernel<WT, NT>, grid(tiles, S), dim3(32 * Cf::WARPS1), Cf::CLUSTER, smem, s, tmW, tmX, a, S, status);
         UOE_LAUNCHED();
     }
     {
@@ -452,7 +452,7 @@ uoe_status launch_layers(const TokArgs& a, int* status, cudaStream_t s) {
         else if (!value_map(&tmX, a.a, a.group, a.d_e, a.n, (size_t)a.group * a.d_e, NT)) return UOE_ERR_CUDA;
         if (WT == kFp8 && !term_map(&tmX, a.a, a.group, a.d_e, a.n, NT)) return UOE_ERR_CUDA;
         ProfScope ps("tokens_second", s);
-        launch_clusters<Cf::CLUSTER>(second_layer_kernel<WT, NT>, grid(tiles, S), 32 * Cf::WARPS2, smem, s, tmW, tmX, a, S, status);
+        launch_k_cluster(second_layer_kernel<WT, NT>, grid(tiles, S), dim3(32 * Cf::WARPS2), Cf::CLUSTER, smem, s, tmW, tmX, a, S, status);
         UOE_LAUNCHED();
     }
     return UOE_OK;

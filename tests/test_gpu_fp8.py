@@ -164,6 +164,8 @@ GEMMS = {
     "odd": dict(counts=[333], N=77, K=129),
     "wide": dict(counts=[1000], N=1000, K=384),
     "long": dict(counts=[130], N=130, K=5000),
+    "split": dict(counts=[250], N=300, K=9000),
+    "split_experts": dict(counts=[200, 0, 70], slack=40, N=140, K=3300),
     "experts": dict(counts=[100, 0, 300, 1], slack=130, N=200, K=260),
     "pairs": dict(counts=[5000, 128, 4100, 0, 3000, 129], slack=300, N=1030, K=640),
     "experts_wide_tiles": dict(counts=[2000, 3500, 129, 0, 4000], slack=1, N=1030, K=512),
@@ -212,6 +214,7 @@ WGRADS = {
     "wide": dict(counts=[3000, 1000, 2500], M=1100, N=600),
     "pairs": dict(counts=[300, 0, 128, 500, 1000, 129, 1, 700], M=1300, N=1000),
     "many_tiles": dict(counts=[300, 0, 128, 500], M=1024, N=2304),
+    "split": dict(counts=[6500, 1], M=130, N=77),
     "empty": dict(counts=[0, 0], M=40, N=24),
 }
 
