@@ -414,15 +414,23 @@ def uoe_route_balance_backward(prob: Problem, x, W_r, p_patch, alpha: float, dlo
     return dx, dW_r
 
 
+def _here(t):
+    """The library works on the current device: a tensor of another one is refused."""
+    assert t.is_cuda, "tensors must be contiguous CUDA tensors"
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
+
+
 def uoe_fp8_quantize(x, layout: str, q=None, scale=None):
     """(q float8_e4m3fn, scale float32) of x [R,C] or [G,R,C] in layout "rows", "cols", "blocks" or "blocks_t" (see uoe.h)."""
     assert x.dim() in (2, 3) and x.dtype in (torch.float32, torch.bfloat16), "x must be [R,C] or [G,R,C], float32 or bfloat16"
     if layout not in FP8_LAYOUTS:
         raise ValueError(f"layout must be one of {sorted(FP8_LAYOUTS)}")
     _contig(x)
+    _here(x)
     R, C = x.shape[-2:]
     blk = lambda v: -(-v // UOE_FP8_BLOCK)
-    lead = x.shape[:-2]
+    lead = tuple(x.shape[:-2])
     rows, inner = (R, C) if layout in ("rows", "blocks") else (C, R)      # of the stored matrix
     shape = (*lead, rows, blk(inner) * UOE_FP8_BLOCK)
     s_shape = (*lead, blk(inner), rows) if layout in ("rows", "cols") else (*lead, blk(rows), blk(inner))
@@ -461,6 +469,7 @@ def _fp8_operand(t, scale, shape, s_shape):
 def uoe_fp8_gemm(prob: Fp8Problem, A, a_scale, W, w_scale, expert_offsets=None, C=None, ws=None, check: bool = True):
     """C [M,N] = rows A times the weights of each row's expert (8-bit operands, see uoe.h).  Without C a new tensor is returned, zero
     behind the last region."""
+    _here(A)
     blk = lambda v: -(-v // UOE_FP8_BLOCK)
     Kb, Nb = blk(prob.K), blk(prob.N)
     _fp8_operand(A, a_scale, (1, prob.M, Kb * UOE_FP8_BLOCK), (1, Kb, prob.M))
@@ -481,6 +490,7 @@ def uoe_fp8_gemm(prob: Fp8Problem, A, a_scale, W, w_scale, expert_offsets=None, 
 
 def uoe_fp8_wgrad(prob: Fp8Problem, A, a_scale, B, b_scale, expert_offsets=None, dW=None, ws=None, check: bool = True):
     """dW [n,M,N] float32 = A B^T over the rows of each expert's region (8-bit operands, see uoe.h)."""
+    _here(A)
     Kb = -(-prob.K // UOE_FP8_BLOCK)
     _fp8_operand(A, a_scale, (1, prob.M, Kb * UOE_FP8_BLOCK), (1, Kb, prob.M))
     _fp8_operand(B, b_scale, (1, prob.N, Kb * UOE_FP8_BLOCK), (1, Kb, prob.N))
@@ -508,6 +518,7 @@ def uoe_mlp_forward_fp8(prob: Problem, x, W1, s1, W2, s2, r: Routing, b1=None, b
     """uoe_mlp_forward on 8-bit weights: (W1, s1), (W2, s2) = uoe_fp8_quantize(W1 [n,d,d_e], "blocks_t"), (W2 [n,d_e,d], "blocks_t")."""
     for t in (x, b1, b2):
         _contig(t, prob.torch_dtype)
+    _here(x)
     _fp8_weights(prob, W1, s1, W2, s2)
     y = y if y is not None else torch.empty_like(x)
     ws = ws if ws is not None else alloc_workspace(prob, UOE_OP_MLP_FWD_FP8, x.device)
@@ -526,6 +537,7 @@ def uoe_mlp_tokens(prob: Problem, x, W_r, W1, W2, s1=None, s2=None, b1=None, b2=
     Weights in the problem's type, or 8-bit with their scales s1, s2 as for uoe_mlp_forward_fp8.  Fills r when given."""
     for t in (x, W_r, b1, b2):
         _contig(t, prob.torch_dtype)
+    _here(x)
     if s1 is None:
         _contig(W1, prob.torch_dtype)
         _contig(W2, prob.torch_dtype)

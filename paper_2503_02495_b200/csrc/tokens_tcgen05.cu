@@ -259,11 +259,15 @@ __device__ __forceinline__ void run_line(const Smem<WT, NT>& sm, const CUtensorM
     }
 }
 
-// Barriers and TMEM of a CTA.  TMEM is taken only when the grids before this one are complete, and the grid behind it is let in only when it
-// is taken: no CTA holds TMEM while it waits for one that still needs some.
+// Barriers and TMEM of a CTA.  TMEM is taken when the grids before this one are complete, and the grid behind it let in when it is taken: no CTA
+// holds TMEM while it waits for an earlier grid that still needs some.  It is taken before the router, whose cluster barriers wait for CTAs that
+// may still be at theirs: the SMs start a second CTA only when the first has its TMEM (behind the router: 27 -> 34 us for a token, d = 4096), and
+// nothing else that waits for its cluster with TMEM in hand (tiles by pairs of CTAs, projections and attention by clusters) fits beside
+// one of these CTAs (more than 190 KB of shared memory each), so that what holds it back there always comes to an end.
 template <int WT, int NT, bool SECOND>
 __device__ __forceinline__ void set_up(const Smem<WT, NT>& sm) {
     using Cf = Cfg<WT, NT>;
+    static_assert(Cf::RING >= 64 * 1024, "room that such a kernel would need");
     if (threadIdx.x == 0) {
         for (int s = 0; s < Cf::STAGES; ++s) { mbar_init(&sm.ctl->full[s], WT == kFp8 && !SECOND ? 1 + Cf::TEAM : 1); mbar_init(&sm.ctl->empty[s], 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(&sm.ctl->tfull[i], 1); mbar_init(&sm.ctl->tempty[i], 4); }
