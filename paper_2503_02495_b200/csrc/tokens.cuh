@@ -207,10 +207,10 @@ __device__ __forceinline__ void cut(int units, int workers, int w, int& lo, int&
     lo = (int)((long long)units * w / workers);
     hi = (int)((long long)units * (w + 1) / workers);
 }
-// The router's outputs for the caller, by one CTA of the group's first cluster.
-__device__ __forceinline__ void write_routing(const TokArgs& a, const Routed& R, int t0, int Tn) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-    for (int q = threadIdx.x; q < routed_words(Tn); q += blockDim.x) ((uint32_t*)(a.routed + blockIdx.z))[q] = ((const uint32_t*)&R)[q];
+// The router's outputs for the second kernel and for the caller, by `warps` warps (this one: `warp`) of one CTA of the group.
+__device__ __forceinline__ void write_routing(const TokArgs& a, const Routed& R, int t0, int Tn, int warp, int warps) {
+    const int lane = threadIdx.x & 31;
+    for (int q = 32 * warp + lane; q < routed_words(Tn); q += 32 * warps) ((uint32_t*)(a.routed + blockIdx.z))[q] = ((const uint32_t*)&R)[q];
     if (!a.r.expert_idx) return;
     for (int tok = warp; tok < Tn; tok += warps) {
         const uint32_t m = R.mask[tok];

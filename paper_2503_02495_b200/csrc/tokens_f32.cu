@@ -124,7 +124,7 @@ first_layer_f32_kernel(const TokArgs a, int S) {
     pdl_wait();
     route_tokens<kF32, 1, kCluster>(a, t0, Tn, rank, sm.red, sm.part, *sm.R);
     const Routed& R = *sm.R;
-    if (blockIdx.x == 0) write_routing(a, R, t0, Tn);
+    if (blockIdx.x == 0) write_routing(a, R, t0, Tn, threadIdx.x >> 5, kWarps);
     const int tiles_n = (a.d_e + kCols - 1) / kCols, tile = blockIdx.x / S, kr = rank % S, first = rank - kr;
     const bool live = tile < R.experts * tiles_n;
     const int slot = live ? tile / tiles_n : 0, c0 = (tile - slot * tiles_n) * kCols, e = R.list[slot];

@@ -17,7 +17,7 @@
 // eight significant bits as bfloat16 has them, down to 2^-14 of the largest, and 2^-22 of the largest below that.  hi and lo are neighbouring
 // columns of one MMA.  A stage is one block of the weights' scales, so its product, times one number per token, is added to float32
 // registers by the write-out warps; the weights' scales may be any numbers.
-//   warp 0       TMA producer         warp 1       MMA issuer
+//   warp 0       TMA producer         warp 1       MMA issuer         warps 2, 3  the router's outputs
 //   warps 4..7   sums: one column per thread, all tokens            warps 8..     8-bit, first kernel: the tokens' values of the stages to come
 #include "tmap.cuh"
 #include "tokens.cuh"
@@ -315,7 +315,8 @@ first_layer_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
     fence_async_smem();                                // the ring is the copies' from here on
     __syncthreads();
     const Routed& R = sm.ctl->R;
-    if (blockIdx.x == 0) write_routing(a, R, 0, Tn);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (blockIdx.x == 0 && (warp & ~1) == 2) write_routing(a, R, 0, Tn, warp - 2, 2);      // (warps without a part in what follows)
     const int tiles_n = (a.d_e + kCols - 1) / kCols, tile = blockIdx.x / S, kr = rank % S, first = rank - kr;
     const bool live = tile < R.experts * tiles_n;
     const int slot = live ? tile / tiles_n : 0, c0 = (tile - slot * tiles_n) * kCols, e = R.list[slot], Kb = (a.d + Cf::K - 1) / Cf::K;
@@ -332,7 +333,6 @@ first_layer_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
     if (live) {
         // (token, 32 columns) per warp, or the token's 128 columns, a lane four of them, where they become two terms
         constexpr int W = 4, WARPS = Cf::WARPS1;
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
         for (int tok = kr * WARPS + warp; tok < Tn; tok += S * WARPS) {
             if (!((R.of[slot] >> tok) & 1)) continue;
             float h[W];
@@ -373,7 +373,7 @@ second_layer_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_consta
     set_up<WT, NT, true>(sm);
     read_routing(a, sm.ctl->R, Tn);
     const Routed& R = sm.ctl->R;
-    if (blockIdx.x == 0 && threadIdx.x < 32 && a.r.expert_offsets) write_offsets(a);
+    if (blockIdx.x == 0 && threadIdx.x >> 5 == 2 && a.r.expert_offsets) write_offsets(a);
     const int c0 = blockIdx.x / S * kCols, kr = rank % S, first = rank - kr;
     auto weight = [&](int tok, int e) { const float p = R.p[tok][e]; return a.use_gate ? p * p : 1.f; };
     Line line{0, 0, (a.d_e + Cf::K - 1) / Cf::K, 0};
