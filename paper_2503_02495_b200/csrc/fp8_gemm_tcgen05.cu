@@ -32,6 +32,7 @@ template <int BN, bool PAIR> struct Cfg {
     static constexpr int TILE = PAIR ? 2 * BM : BM;
     static constexpr int A_BYTES = BM * kQ, B_BYTES = BN_CTA * kQ, STAGE = A_BYTES + B_BYTES;
     static constexpr int STAGES = BN_CTA == 256 ? 4 : 6;
+    static_assert(STAGES >= 4, "four warps in turn: none looks for a stage's last use by parity two uses ahead");
     static constexpr int NACC = BN == 256 ? 1 : 2;
     static constexpr int CW = BN / 2;
     static constexpr int EPI_WARPS = 8, THREADS = 128 + 128 + 32 * EPI_WARPS;

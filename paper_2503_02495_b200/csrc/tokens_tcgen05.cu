@@ -37,9 +37,13 @@ template <int WT, int NT /* tokens, rounded up */> struct Cfg {
     static constexpr int A_BYTES = 16384, B_BYTES = N * 128, STAGE = A_BYTES + B_BYTES;
     static constexpr int CTAS = NT <= 32 ? 2 : 1;                         // per SM
     static constexpr int CLUSTER = CTAS == 2 ? 8 : 4;                     // (eight CTAs of an SM each: some clusters wait for a second turn)
-    static constexpr int STAGES = CTAS == 1 ? 6 : NT <= 16 ? 5 : 4;
+    static constexpr int STAGES = CTAS == 1 ? 6 : NT <= 16 ? 4 : 3;
     static constexpr int TMEM_COLS = 2 * N < 32 ? 32 : 2 * N;
     static constexpr int TEAM = NT / 8, TEAMS = NT == 8 ? 4 : NT == 16 ? 2 : 1;       // 8-bit: a team of warps fills a stage, 8 tokens each
+    // (A team looks for its next stage's last use by parity: it must not be two uses behind, and the team's own last stage vouches for no more
+    // than the uses before that.)
+    static_assert(WT != kFp8 || TEAMS <= STAGES, "teams");
+    static_assert(kScaleSlots >= STAGES + 3, "factors");
     static constexpr int WARPS1 = WT == kFp8 ? 8 + TEAM * TEAMS : 8, WARPS2 = 8;      // of the two kernels
     static constexpr int PITCH = kCols + 4;                               // floats of a token's sums in shared memory
     static constexpr int RING = STAGES * STAGE;
@@ -267,7 +271,7 @@ __device__ __forceinline__ void run_line(const Smem<WT, NT>& sm, const CUtensorM
 template <int WT, int NT, bool SECOND>
 __device__ __forceinline__ void set_up(const Smem<WT, NT>& sm) {
     using Cf = Cfg<WT, NT>;
-    static_assert(Cf::RING >= 64 * 1024, "room that such a kernel would need");
+    static_assert(Cf::RING >= 40 * 1024, "room that such a kernel would need");
     if (threadIdx.x == 0) {
         for (int s = 0; s < Cf::STAGES; ++s) { mbar_init(&sm.ctl->full[s], WT == kFp8 && !SECOND ? 1 + Cf::TEAM : 1); mbar_init(&sm.ctl->empty[s], 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(&sm.ctl->tfull[i], 1); mbar_init(&sm.ctl->tempty[i], 4); }
