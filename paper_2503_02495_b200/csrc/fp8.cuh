@@ -89,8 +89,11 @@ struct Fp8Gemm {
     Fp8Epilogue epi = kFp8Store;
     void* q = nullptr; float* qs = nullptr;      // kFp8ActQuant: [M, Np], [Np / 128, M]
     bool any_scale = false;                // scales need not be powers of two
+    SrcMap map;                            // kFp8ActQuant: if on, A and sa are those of the source rows [B m l_p]; row r of a region is gathered
     const char* label = "fp8_gemm";
 };
+// Patches that a tile's rows can be copied by: whole ones in 128 rows, whole 8-row groups of the swizzle.
+inline bool fp8_can_gather(int l_p) { return l_p % 8 == 0 && 128 % l_p == 0; }
 uoe_status launch_fp8_gemm(const Fp8Gemm& g, int* status, cudaStream_t s);
 
 }  // namespace uoe

@@ -13,10 +13,14 @@
 //   warps 8..15  write-out: a warp has 32 rows (its TMEM lane quarter) and half of the columns, all of them in registers before it
 //                gives the accumulator back (256 columns and the scales leave room for one accumulator: the next tile's products
 //                wait for these loads, not for the arithmetic and the stores)
+// The routed rows of A may be gathered (Eq. 18 inside the loads): A holds every token once, quantised, and a tile's rows come in one copy per
+// source patch, their scales by their source rows.
 // Regions of experts are whole 128-row blocks; the second half of a pair's last tile may be rows of nobody, which are not stored.
 #include "fp8_tile.cuh"
 #include "tc.cuh"
 #include "tmap.cuh"
+
+#include <type_traits>
 
 namespace uoe {
 namespace {
@@ -58,10 +62,12 @@ __device__ __forceinline__ uint32_t exponent_word(float s, bool there, bool& bad
     return __byte_perm(pow2 ? e : 255u, 0, 0);
 }
 
-template <int BN, bool WGRAD, int EPI, bool PAIR, bool SPLIT>
+struct NoMap {};                          // what a kernel without gathered rows takes in the map's place
+
+template <int BN, bool WGRAD, int EPI, bool PAIR, bool SPLIT, bool GATHER>
 __global__ void __launch_bounds__(Cfg<BN, PAIR>::THREADS, 1)
 fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmC,
-                const __grid_constant__ Fp8Args a) {
+                const __grid_constant__ Fp8Args a, const typename std::conditional<GATHER, SrcMap, NoMap>::type map) {
     using Cf = Cfg<BN, PAIR>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -171,13 +177,22 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         for (int tile = worker; tile < total && !stop; tile += workers) {
             const Tile t = locate(tile, e);
             const int rows = t.row_end - t.row0, cols = a.N - t.col0;
-            const float* sa = a.sa + (size_t)t.kb0 * a.M + t.row0;
+            const float* sa = GATHER ? a.sa : a.sa + (size_t)t.kb0 * a.M + t.row0;
+            [[maybe_unused]] int from[4] = {0, 0, 0, 0};              // source row of this lane's rows, -1: none
+            if constexpr (GATHER) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int r = t.row0 + q * 32 + lane, p = r < t.row_end ? src_of(map, r, e, ctl->reg.offs[e], -1) : -1;
+                    from[q] = p >= 0 && p < map.B * map.m ? p * map.l_p + r % map.l_p : -1;       // (a table that a bad index left unwritten: no row)
+                }
+            }
+            auto has = [&](int q) { return GATHER ? from[q] >= 0 : lane < rows - q * 32; };
             const float* sb = WGRAD ? a.sb + (size_t)t.kb0 * a.N + t.col0 : a.sb + ((size_t)e * a.Nb + t.col0 / kQ) * a.Kb + t.kb0;
             float ra[4], rb[NB];                                      // (whatever is there where there are no rows of this expert, or no columns)
             auto ask = [&](int kb) {
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
-                    if (lane < rows - q * 32) ra[q] = __ldg(sa + (size_t)kb * a.M + q * 32 + lane);
+                    if (has(q)) ra[q] = __ldg(GATHER ? sa + (size_t)kb * a.x_rows + from[q] : sa + (size_t)kb * a.M + q * 32 + lane);
 #pragma unroll
                 for (int q = 0; q < NB; ++q) {
                     if constexpr (WGRAD) { if (lane < cols - q * 32) rb[q] = __ldg(sb + (size_t)kb * a.N + q * 32 + lane); }
@@ -190,7 +205,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 if (((kb - first) & 3) == 0) {
                     uint32_t wa[4], wn[NB], wb[8];
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) wa[q] = exponent_word(ra[q], lane < rows - q * 32, bad);
+                    for (int q = 0; q < 4; ++q) wa[q] = exponent_word(ra[q], has(q), bad);
 #pragma unroll
                     for (int q = 0; q < NB; ++q) wn[q] = exponent_word(rb[q], WGRAD ? lane < cols - q * 32 : cols > q * kQ, bad);
 #pragma unroll
@@ -222,9 +237,28 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             bool stop = false;
             for (int tile = worker; tile < total && !stop; tile += workers) {
                 const Tile t = locate(tile, e);
+                [[maybe_unused]] int boxes = 0, src = 0;      // source patches of the CTA's 128 rows; this lane's one
+                if constexpr (GATHER) {
+                    boxes = BM / map.l_p;
+                    const int r = t.row0 + lane * map.l_p;
+                    src = lane < boxes && r < t.row_end ? src_of(map, r, e, ctl->reg.offs[e], map.B * map.m) : map.B * map.m;    // (past the last patch: zeros)
+                }
                 for (int kb = 0; kb < t.kbs; ++kb) {
                     if (!mbar_wait_warp_quick(&ctl->empty[stage], phase ^ 1, abort_flag, a.status)) { stop = true; break; }
-                    if (lane == 0) {
+                    if constexpr (GATHER) {                   // a copy per source patch, each by a lane of its own
+                        uint8_t* st = smem + stage * Cf::STAGE;
+                        const int k = (t.kb0 + kb) * kQ;
+                        if (lane == 0 && rank == 0) mbar_arrive_expect_tx(&ctl->full[stage], CTAS * Cf::STAGE);
+                        __syncwarp();
+                        if constexpr (PAIR) {
+                            const uint32_t full0 = map_to_cta(&ctl->full[stage], 0);
+                            if (lane < boxes) tma_load_3d_pair(st + lane * map.l_p * kQ, &tmA, k, 0, src, full0);
+                            if (lane == 0) tma_load_3d_pair(st + Cf::A_BYTES, &tmB, k, t.col0 + rank * Cf::BN_CTA, e, full0);
+                        } else {
+                            if (lane < boxes) tma_load_3d(st + lane * map.l_p * kQ, &tmA, k, 0, src, &ctl->full[stage]);
+                            if (lane == 0) tma_load_3d(st + Cf::A_BYTES, &tmB, k, t.col0, e, &ctl->full[stage]);
+                        }
+                    } else if (lane == 0) {
                         uint8_t* st = smem + stage * Cf::STAGE;
                         const int k = (t.kb0 + kb) * kQ, row = min(t.row0, (int)a.M);        // (a block behind the rows: all zeros)
                         if (rank == 0) mbar_arrive_expect_tx(&ctl->full[stage], CTAS * Cf::STAGE);
@@ -317,17 +351,21 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     }
 }
 
-template <int BN, bool WGRAD, int EPI, bool PAIR, bool SPLIT = false>
+template <int BN, bool WGRAD, int EPI, bool PAIR, bool SPLIT = false, bool GATHER = false>
 uoe_status launch_one(const Fp8Gemm& g, int* status, cudaStream_t s, int split = 1) {
     using Cf = Cfg<BN, PAIR>;
     static DeviceOnce once;
     static DeviceValue pairs_cache;
-    auto kern = fp8_gemm_kernel<BN, WGRAD, EPI, PAIR, SPLIT>;
+    auto kern = fp8_gemm_kernel<BN, WGRAD, EPI, PAIR, SPLIT, GATHER>;
     const uoe_status st = smem_opt_in(once, kern, Cf::SMEM);
     if (st != UOE_OK) return st;
     const uint64_t Kp = (uint64_t)((g.K + kQ - 1) / kQ * kQ);
     CUtensorMap tmA, tmB;
-    {
+    if constexpr (GATHER) {       // the source rows as [patches][l_p][Kp]
+        const uint64_t dims[3] = {Kp, (uint64_t)g.map.l_p, (uint64_t)g.map.B * g.map.m}, str[2] = {Kp, Kp * g.map.l_p};
+        const uint32_t box[3] = {kQ, (uint32_t)g.map.l_p, 1};
+        if (!make_tmap(&tmA, g.A, 3, dims, str, box, CU_TENSOR_MAP_DATA_TYPE_UINT8)) return UOE_ERR_CUDA;
+    } else {
         const uint64_t dims[2] = {Kp, (uint64_t)g.M};
         const uint64_t str[1] = {Kp};
         const uint32_t box[2] = {kQ, BM};
@@ -341,6 +379,9 @@ uoe_status launch_one(const Fp8Gemm& g, int* status, cudaStream_t s, int split =
     }
     Fp8Args a = fp8_args(g, status);
     a.split = split;
+    a.x_rows = (long long)g.map.B * g.map.m * g.map.l_p;
+    typename std::conditional<GATHER, SrcMap, NoMap>::type map;
+    if constexpr (GATHER) map = g.map;
     CUtensorMap tmC = tmA;
     if (g.epi == kFp8Store && a.vec && !result_map(&tmC, g)) return UOE_ERR_CUDA;
     const long long tiles = ((g.M + Cf::TILE - 1) / Cf::TILE + (PAIR && !g.wgrad ? g.n : 0)) * ((g.N + BN - 1) / BN) * (g.wgrad ? g.n : 1);
@@ -356,11 +397,11 @@ uoe_status launch_one(const Fp8Gemm& g, int* status, cudaStream_t s, int split =
             pairs_cache.set(dev, v);
         }
         const long long pairs = pairs_cache.get(dev);
-        launch_k_pairs(kern, dim3(2 * (unsigned)(tiles < pairs ? tiles : pairs)), dim3(Cf::THREADS), (size_t)Cf::SMEM, s, tmA, tmB, tmC, a);
+        launch_k_pairs(kern, dim3(2 * (unsigned)(tiles < pairs ? tiles : pairs)), dim3(Cf::THREADS), (size_t)Cf::SMEM, s, tmA, tmB, tmC, a, map);
     } else if constexpr (SPLIT) {
-        launch_k_cluster(kern, dim3((unsigned)tiles * split), dim3(Cf::THREADS), split, (size_t)Cf::SMEM, s, tmA, tmB, tmC, a);
+        launch_k_cluster(kern, dim3((unsigned)tiles * split), dim3(Cf::THREADS), split, (size_t)Cf::SMEM, s, tmA, tmB, tmC, a, map);
     } else {
-        launch_k(kern, dim3((unsigned)(tiles < sm_count() ? tiles : sm_count())), dim3(Cf::THREADS), (size_t)Cf::SMEM, s, tmA, tmB, tmC, a);
+        launch_k(kern, dim3((unsigned)(tiles < sm_count() ? tiles : sm_count())), dim3(Cf::THREADS), (size_t)Cf::SMEM, s, tmA, tmB, tmC, a, map);
     }
     UOE_LAUNCHED();
     return UOE_OK;
@@ -369,7 +410,11 @@ uoe_status launch_one(const Fp8Gemm& g, int* status, cudaStream_t s, int split =
 template <bool WGRAD, int EPI>
 uoe_status dispatch(const Fp8Gemm& g, int* status, cudaStream_t s) {
     const long long cols256 = (g.N + 255) / 256, mats = g.wgrad ? g.n : 1;
-    if (g.N > 128 && (g.M + 255) / 256 * cols256 * mats >= sm_count()) return launch_one<256, WGRAD, EPI, true>(g, status, s);
+    const bool pairs = g.N > 128 && (g.M + 255) / 256 * cols256 * mats >= sm_count();
+    if constexpr (EPI == kFp8ActQuant) {
+        if (g.map.on()) return pairs ? launch_one<256, WGRAD, EPI, true, false, true>(g, status, s) : launch_one<256, WGRAD, EPI, false, false, true>(g, status, s);
+    }
+    if (pairs) return launch_one<256, WGRAD, EPI, true>(g, status, s);
     if (EPI == kFp8ActQuant || (g.N > 128 && (g.M + 127) / 128 * cols256 * mats >= sm_count())) return launch_one<256, WGRAD, EPI, false>(g, status, s);
     if constexpr (EPI != kFp8ActQuant) {
         // Tiles that leave SMs idle and have far to go: the contraction of a tile in up to eight parts, a CTA of a cluster each, from 24 blocks on
@@ -391,6 +436,7 @@ uoe_status dispatch(const Fp8Gemm& g, int* status, cudaStream_t s) {
 uoe_status launch_fp8_gemm(const Fp8Gemm& g, int* status, cudaStream_t s) {
     if (g.n > kMaxExperts) return UOE_ERR_UNSUPPORTED;
     if (fp8_is_skinny(g)) return launch_fp8_skinny(g, status, s);
+    if (g.map.on() && (g.any_scale || g.epi != kFp8ActQuant || !fp8_can_gather(g.map.l_p))) return UOE_ERR_UNSUPPORTED;
     if (g.any_scale) return launch_fp8_gemm_any(g, status, s);
     if (g.wgrad) return dispatch<true, kFp8Store>(g, status, s);
     return g.epi == kFp8ActQuant ? dispatch<false, kFp8ActQuant>(g, status, s) : dispatch<false, kFp8Store>(g, status, s);

@@ -140,7 +140,7 @@ quantize_tile_kernel(const T* __restrict__ x, uint8_t* __restrict__ q, float* __
             uint32_t m = 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i) m = max(m, abs_bits(f[i][j]));
-            s_max[rg * kQ + ((cg + 16 * j) ^ 0)] = m;       // column cg * 8 + j kept at 16 j + cg: lanes side by side
+            s_max[rg * kQ + cg + 16 * j] = m;       // column cg * 8 + j kept at 16 j + cg: lanes side by side
         }
         __syncthreads();
 #pragma unroll

@@ -22,6 +22,7 @@ struct Fp8Args {
     float* qs;
     long long ldq;
     int split;                        // CTAs that share a tile's contraction
+    long long x_rows;                 // gathered: rows of A
     int* status;
 };
 

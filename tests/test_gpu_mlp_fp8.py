@@ -33,6 +33,9 @@ CASES = {
     "several_tiles": (_w(B=6, L=512, L_valid=500, m=16, c=8, d=384, n=6, k=3, d_ff=6 * 256, w_std=0.05), {}),
     "any_scale": (_w(B=3, L=96, L_valid=96, m=6, c=3, d=192, n=4, k=2, d_ff=4 * 136), dict(any_scale=True)),
     "pairs_of_ctas": (_w(B=40, L=1152, L_valid=1152, m=9, c=3, d=256, n=4, k=2, d_ff=4 * 320, w_std=0.05), {}),
+    "gathered_patches_of_8": (_w(B=14, L=1152, L_valid=1130, m=144, c=48, d=200, n=8, k=4, d_ff=8 * 320, w_std=0.05), dict(bias=True)),
+    "gathered_patches_of_64": (_w(B=9, L=2048, L_valid=2048, m=32, c=9, d=264, n=12, k=4, d_ff=12 * 392, act="gelu_erf", w_std=0.05), {}),
+    "gathered_whole_samples": (_w(B=7, L=256, L_valid=256, m=2, c=2, d=136, n=8, k=2, d_ff=8 * 136), {}),
 }
 
 
@@ -118,6 +121,41 @@ def test_mlp_fp8(name):
     assert (diff[~pad] <= bound[~pad]).all(), float((diff / bound)[~pad].max())
     assert torch.equal(got.view(-1, w.d)[pad.cuda()], to_dev(x).view(-1, w.d)[pad.cuda()] * (1 if prob.residual else 0))
     assert torch.equal(got, uoe.uoe_mlp_forward_fp8(prob, to_dev(x), W1, s1, W2, s2, r, b1=bd[0], b2=bd[1]))
+
+
+@pytest.mark.parametrize("name", ["several_tiles", "gathered_patches_of_8", "small"])
+def test_captured_and_on_two_streams(name):
+    """Replays follow the tensors' contents; two streams with a workspace each do not meet."""
+    import paper_2503_02495_b200 as uoe
+    w, prob, x, r, (W1, s1, v1), (W2, s2, v2), b = _setup(name)
+    xd = to_dev(x)
+    x2 = xd.flip(0).contiguous()
+    r2 = type(r)(**{k: v.clone() if torch.is_tensor(v) else v for k, v in vars(uoe.uoe_route(prob, x2, to_dev(gen.store(gen.make_router(w).f64 * 20, w.dtype)))).items()})
+    run = lambda xx, rr, ws: uoe.uoe_mlp_forward_fp8(prob, xx, W1, s1, W2, s2, rr, ws=ws, check=False)      # (the check waits for the device)
+    ws = [uoe.alloc_workspace(prob, uoe.UOE_OP_MLP_FWD_FP8) for _ in range(2)]
+    want, want2 = run(xd, r, ws[0]).clone(), run(x2, r2, ws[0]).clone()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [None, None]
+    for _ in range(3):
+        for i, (xx, rr) in enumerate(((xd, r), (x2, r2))):
+            with torch.cuda.stream(streams[i]):
+                got[i] = run(xx, rr, ws[i])
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want) and torch.equal(got[1], want2)
+    held = xd.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = run(held, r, ws[0])
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+    held.copy_(x2)
+    for a, c in ((r.expert_idx, r2.expert_idx), (r.patch_idx, r2.patch_idx), (r.gate, r2.gate), (r.expert_offsets, r2.expert_offsets)):
+        a.copy_(c)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want2)
 
 
 def test_prompt_then_tokens():
