@@ -280,7 +280,7 @@ typedef struct {
 
 /* The scales may be any float32 numbers, as weights quantised elsewhere have them.  Without it they are powers of two, as
  * uoe_fp8_quantize writes them, or NaN, and the tensor cores apply them; a scale that is neither counts as NaN and is reported in the
- * workspace's status word (UOE_ERR_FP8_SCALE). */
+ * workspace's status word (UOE_ERR_FP8_SCALE).  uoe_fp8_gemm of up to 64 rows without offsets takes any scales in either case. */
 enum { UOE_FP8_ANY_SCALE = 1 };
 
 /* Bytes of device workspace of the two products (0 on an invalid problem).  Prepared with uoe_workspace_init like any other. */
@@ -368,7 +368,8 @@ uoe_status uoe_block_forward(const uoe_problem* att, const uoe_problem* mlp, con
  * with gate = p_samp^2 (UOE_FLAG_GATE: P_samp times the gate of the token's one patch) or 1, and the residual by UOE_FLAG_RESIDUAL.  Every
  * chosen expert's weights are read once.
  *   Weights in prob->dtype as for uoe_mlp_forward (w1_scale = w2_scale = NULL), or, for bfloat16 problems, 8-bit as for
- *   uoe_mlp_forward_fp8 with any float32 scales; x and the hidden rows stay bfloat16 there (the products are exact in float32).
+ *   uoe_mlp_forward_fp8 with any float32 scales.  x and the hidden rows (rounded to bfloat16) enter those products as two e4m3 terms
+ *   each: exactly, but for values below 2^-13 of the largest in their block of 128, which are off by 2^-21 of that largest at most.
  *   r: host pointer to device arrays that receive the router's outputs, or NULL.    y: distinct from x.
  *   A token that holds a NaN gets the first k experts.
  * Workspace: UOE_OP_MLP_TOKENS.

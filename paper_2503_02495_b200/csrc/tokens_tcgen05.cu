@@ -14,7 +14,7 @@
 // Stages: 128 columns x 64 of the contraction of bfloat16 weights (as they lie, columns contiguous), or x 128 of 8-bit weights (the
 // contraction contiguous).  bfloat16: the tokens' values come by TMA as well, and one TMEM accumulator takes all of an expert.  8-bit: the
 // tensor cores want both operands in 8 bits, so a token's 128 values of a stage become two e4m3 terms, x = s (hi + lo / 16), s a power of two:
-// eight significant bits as bfloat16 has them, down to 2^-14 of the largest, and 2^-22 of the largest below that.  hi and lo are neighbouring
+// eight significant bits as bfloat16 has them, from 2^-6 s on; smaller values are off by 2^-14 s at most, 2^-21 of the largest of the 128.  hi and lo are neighbouring
 // columns of one MMA.  A stage is one block of the weights' scales, so its product, times one number per token, is added to float32
 // registers by the write-out warps; the weights' scales may be any numbers.
 //   warp 0       TMA producer         warp 1       MMA issuer         warps 2, 3  the router's outputs
@@ -346,7 +346,7 @@ first_layer_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
                 h[v] = 0.f;
                 for (int s = 0; s < S; ++s) h[v] += ld_cluster_f32(cta + tok * Cf::PITCH + W * lane + v, first + s);
                 if (a.b1 && col < a.d_e) h[v] += to_f32(((const bf16*)a.b1)[(size_t)e * a.d_e + col]);
-                // (half a step, 2^-9 of the value, like the hidden rows of uoe_mlp_forward)
+                // (half a step, 2^-8 of the value, like the hidden rows of uoe_mlp_forward)
                 h[v] = col < a.d_e ? to_f32(__float2bfloat16_rn(act_precise(h[v], a.act))) : 0.f;
             }
             if constexpr (WT == kFp8) {

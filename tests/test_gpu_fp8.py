@@ -6,7 +6,7 @@ error is its float32 arithmetic and the rounding of the result.  Per element of 
 2 x 4 bits), at most 128 additions in the tensor core and Kb additions outside it, two roundings of the scales' product.  (With scales
 that are powers of two the tensor core adds all of K, 32 products a step.)  With gamma = (128 + 4 Kb + 4) 2^-23 (a tensor-core addition counted
 as truncating: one step of float32) the error is at most
-gamma * sum |a| |b|; bfloat16 results add half a step, 2^-8 / 2 ... counted as 2^-8 of the result.
+gamma * sum |a| |b|; bfloat16 results add half a step, 2^-8 of the result.
 """
 import numpy as np
 import pytest

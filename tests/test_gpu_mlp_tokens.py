@@ -4,6 +4,8 @@ Bounds, element by element, from the float64 values themselves.  With u = 2^-24 
 K 2^-23 sum |terms| (any order of additions).  Router: a score off by ds changes a softmax gate by at most a factor exp(2 ds), the
 combine weight (its square) by twice that; expf and the division add 2^-20.  Hidden rows: phi grows no faster than 1.13; it is evaluated to
 2^-20 of its value and stored with half a step (2^-8 for bfloat16, 2^-24 for float32).  The result's own rounding is half a step again.
+8-bit weights: the rows' two e4m3 terms s (hi + lo / 16), s <= max / 224, are exact from 2^-6 s on; below, 16 times what hi leaves is rounded
+to steps of 2^-9, half a step 2^-10 / 16 s = 2^-14 s < 2^-21 max, max the largest magnitude in the block of 128.
 """
 import math
 
@@ -23,8 +25,8 @@ def _phi(h, act):
     return torch.nn.functional.gelu(h, approximate="none" if act == "gelu_erf" else "tanh")
 
 
-def _case(T, d, d_e, n, k, weights="bf16", act="silu", bias=False, gate=True, residual=True, seed=0):
-    return dict(T=T, d=d, d_e=d_e, n=n, k=k, weights=weights, act=act, bias=bias, gate=gate, residual=residual, seed=seed)
+def _case(T, d, d_e, n, k, weights="bf16", act="silu", bias=False, gate=True, residual=True, seed=0, spread=0):
+    return dict(spread=spread, T=T, d=d, d_e=d_e, n=n, k=k, weights=weights, act=act, bias=bias, gate=gate, residual=residual, seed=seed)
 
 
 CASES = {
@@ -46,6 +48,7 @@ CASES = {
     "fp8_tail": _case(18, 328, 200, 7, 2, "fp8", residual=False),
     "fp8_many": _case(64, 264, 136, 6, 3, "fp8", bias=True, gate=False),
     "fp8_wide": _case(4, 2056, 1032, 4, 2, "fp8"),
+    "fp8_range": _case(6, 392, 200, 5, 2, "fp8", act="identity", residual=False, spread=24),
     "f32_one": _case(1, 64, 32, 2, 1, "f32"),
     "f32_smallest": _case(1, 4, 4, 1, 1, "f32"),
     "f32_odd": _case(9, 132, 68, 5, 3, "f32", bias=True, act="gelu_erf"),
@@ -58,8 +61,18 @@ def make(c):
     g = torch.Generator().manual_seed(100 + c["seed"])
     rn = lambda *s, std=1.0: (torch.randn(*s, generator=g, dtype=torch.float64) * std).to(dt)
     n, d, d_e = c["n"], c["d"], c["d_e"]
-    return dict(x=rn(c["T"], 1, d), Wr=rn(d, n, std=3 * d ** -0.5), W1=rn(n, d, d_e, std=d ** -0.5), W2=rn(n, d_e, d, std=d_e ** -0.5),
+    x = rn(c["T"], 1, d)
+    if c["spread"]:       # values of very different sizes in a row, and so hidden values too; the router hardly sees the small ones
+        x = (x.double() * torch.exp2(-torch.randint(0, c["spread"], (1, 1, d), generator=g).double())).to(dt)
+    return dict(x=x, Wr=rn(d, n, std=3 * d ** -0.5), W1=rn(n, d, d_e, std=d ** -0.5), W2=rn(n, d_e, d, std=d_e ** -0.5),
                 b1=rn(n, d_e, std=0.3) if c["bias"] else None, b2=rn(n, d, std=0.3) if c["bias"] else None)
+
+
+def _terms_error(v):
+    """Per element of v [K]: 2^-21 of the largest in its block of 128, where the element is not exact for certain."""
+    K = v.shape[0]
+    top = torch.nn.functional.pad(v.abs(), (0, -K % BLOCK)).view(-1, BLOCK).amax(1).repeat_interleave(BLOCK)[:K]
+    return torch.where(v.abs() < 2.0 ** -5 / 224 * top, 2.0 ** -21 * top, torch.zeros_like(top))
 
 
 def reference(c, x, Wr, W1, W2, b1, b2, experts=None):
@@ -79,12 +92,16 @@ def reference(c, x, Wr, W1, W2, b1, b2, experts=None):
     for t in range(x.shape[0]):
         for i in e[t].tolist():
             h, hb = x[t] @ W1[i].double(), (d + 8) * 2.0 ** -23 * (x[t].abs() @ W1[i].double().abs())
+            if c["weights"] == "fp8":
+                hb = hb + _terms_error(x[t]) @ W1[i].double().abs()
             if b1 is not None:
                 h = h + b1[i].double()
             a = _phi(h, c["act"])
             da = 1.13 * hb + (2.0 ** -20 + half) * a.abs() + 2.0 ** -126
             z = a @ W2[i].double() + (b2[i].double() if b2 is not None else 0)
             dz = da @ W2[i].double().abs() + (d_e * k + 16) * 2.0 ** -23 * (a.abs() @ W2[i].double().abs()) + 2.0 ** -22 * z.abs()
+            if c["weights"] == "fp8":
+                dz = dz + _terms_error(a) @ W2[i].double().abs()
             w = p[t, i] ** 2 if c["gate"] else torch.tensor(1.0, dtype=torch.float64)
             y[t] += w * z
             err[t] += w * dz + (w * 2 * rel_p[t] * z.abs() if c["gate"] else 0) + k * 2.0 ** -23 * (w * z).abs()
