@@ -70,7 +70,7 @@ __device__ __forceinline__ void act_precise_n(float* f, int act) {
 // x [rows of C elements] -> q [rows, Cp], scale [Cp / 128, rows]: every row by itself.  With map.on() row r of the output is the
 // token that routed row r holds (zeros on padding rows and unused slots), and only rows below offsets[n] are written.
 uoe_status launch_quantize_rows(const void* x, bool bf16, int G, long long rows, int C, void* q, float* scale, const SrcMap& map,
-                                const int* offsets, int n, const char* label, cudaStream_t s);
+                                const int* offsets, int n, const char* label, cudaStream_t s, bool beside_plan = false);
 
 // What a tile of the product becomes.
 enum Fp8Epilogue {

@@ -35,7 +35,7 @@ __device__ __forceinline__ uint4 load_piece(const T* row, int c, int C, bool who
 template <typename T>
 __global__ void __launch_bounds__(256)
 quantize_rows_kernel(const T* __restrict__ x, uint8_t* __restrict__ q, float* __restrict__ scale, long long rows, int C, int Cb, int groups /* of kBlocksPerCta blocks */,
-                     int splits, int whole, const SrcMap map, const int* __restrict__ offsets, int n) {
+                     int splits, int whole, const SrcMap map, const int* __restrict__ offsets, int n, int beside_plan) {
     pdl_trigger();
     constexpr int V = Vec16<T>::N;                    // elements per 16 bytes
     constexpr int LPB = kQ / V;                       // lanes per block: 16 or 32
@@ -48,7 +48,7 @@ quantize_rows_kernel(const T* __restrict__ x, uint8_t* __restrict__ q, float* __
     const long long mat = blockIdx.x / per_mat;
     const long long rest = blockIdx.x - mat * per_mat;
     const long long row0 = rest / splits * kRowsPerCta;
-    pdl_wait();
+    if (!beside_plan) pdl_wait();
     // where the warp's rows come from: looked up once for all columns, a lane per row
     long long mine = row0 + warp * RPW + (lane % RPW) < rows ? mat * rows + row0 + warp * RPW + (lane % RPW) : -1;
     if (map.on()) {
@@ -105,6 +105,7 @@ quantize_rows_kernel(const T* __restrict__ x, uint8_t* __restrict__ q, float* __
             if (cb < Cb && r < rows) scale[(mat * Cb + cb) * rows + r] = s_scale[b][threadIdx.x / kRowsPerCta][threadIdx.x % kRowsPerCta];
         }
     }
+    if (beside_plan) pdl_wait();                      // this kernel is complete only when the plan is: the next one reads both
 }
 
 template <typename T, int LAYOUT>
@@ -210,7 +211,7 @@ uoe_status launch_tile(int layout, int G, int R, int C, const void* x, void* q, 
 }  // namespace
 
 uoe_status launch_quantize_rows(const void* x, bool bf16, int G, long long rows, int C, void* q, float* scale, const SrcMap& map,
-                                const int* offsets, int n, const char* label, cudaStream_t s) {
+                                const int* offsets, int n, const char* label, cudaStream_t s, bool beside_plan) {
     const int Cb = q_blocks(C), groups = (Cb + kBlocksPerCta - 1) / kBlocksPerCta, whole = ((size_t)C * (bf16 ? 2 : 4)) % 16 == 0;
     // CTAs of a row block: as many as keep some eight per SM; a row's columns are a loop otherwise
     const long long row_ctas = (long long)G * ((rows + kRowsPerCta - 1) / kRowsPerCta);
@@ -219,8 +220,8 @@ uoe_status launch_quantize_rows(const void* x, bool bf16, int G, long long rows,
     const long long ctas = row_ctas * splits;
     if (ctas > 0x7fffffffll) return UOE_ERR_UNSUPPORTED;
     ProfScope ps(label, s);
-    if (bf16) launch_k(quantize_rows_kernel<__nv_bfloat16>, dim3((unsigned)ctas), dim3(256), 0, s, (const __nv_bfloat16*)x, (uint8_t*)q, scale, rows, C, Cb, groups, splits, whole, map, offsets, n);
-    else launch_k(quantize_rows_kernel<float>, dim3((unsigned)ctas), dim3(256), 0, s, (const float*)x, (uint8_t*)q, scale, rows, C, Cb, groups, splits, whole, map, offsets, n);
+    if (bf16) launch_k(quantize_rows_kernel<__nv_bfloat16>, dim3((unsigned)ctas), dim3(256), 0, s, (const __nv_bfloat16*)x, (uint8_t*)q, scale, rows, C, Cb, groups, splits, whole, map, offsets, n, beside_plan ? 1 : 0);
+    else launch_k(quantize_rows_kernel<float>, dim3((unsigned)ctas), dim3(256), 0, s, (const float*)x, (uint8_t*)q, scale, rows, C, Cb, groups, splits, whole, map, offsets, n, beside_plan ? 1 : 0);
     UOE_LAUNCHED();
     return UOE_OK;
 }

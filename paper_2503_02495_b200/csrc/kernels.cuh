@@ -194,9 +194,12 @@ __device__ __forceinline__ int src_of(const SrcMap& g, int r, int e, int off_e, 
 // Buffers in `tails` (rows of tails.row_bytes): the first 128 rows past the last expert region are zero-filled, as many as a
 // 128-row tile that starts inside the last region can reach.
 struct PlanTails { void* p[4] = {nullptr, nullptr, nullptr, nullptr}; long long row_bytes = 0; };
+// trigger_late: the kernel launched next may start its work beside this one, as far as it uses nothing of the plan (launch_quantize_rows'
+// beside_plan); what came before both is complete.
 uoe_status launch_plan(const Dims& D, const int* expert_idx, const int* patch_idx, const float* gate,
                        const int* offsets, const PlanPtrs& P, int* status, cudaStream_t s, bool use_gate = true,
-                       const PlanTails& tails = PlanTails());
+                       const PlanTails& tails = PlanTails(),
+                       bool trigger_late = false);
 
 // Eq. 18 / 24: copy the selected patches of `src` [B,L,d] into the routed buffer `dst` [rows,d];
 // unused slots and the padding rows of each expert region are zero-filled.

@@ -51,12 +51,12 @@ extern "C" uoe_status uoe_mlp_forward_fp8(const uoe_problem* prob, const void* x
     char* base = (char*)ws;
     int* status = (int*)base;
     const PlanPtrs P = plan_ptrs(D, base + W.plan);
-    st = launch_plan(D, expert_idx, patch_idx, gate, expert_offsets, P, status, s);
-    if (st != UOE_OK) return st;
     const bool any_scale = (prob->flags & UOE_FLAG_FP8_ANY_SCALE) != 0;
     const long long tokens = (long long)D.B * D.L;
     const bool gather = !any_scale && fp8_can_gather(D.l_p) && D.R >= tokens && tokens < (1ll << 31);
-    if (gather) st = launch_quantize_rows(x, true, 1, tokens, D.d, base + W.xq, (float*)(base + W.xs), SrcMap(), nullptr, 0, "fp8_quantize_x", s);
+    st = launch_plan(D, expert_idx, patch_idx, gate, expert_offsets, P, status, s, true, PlanTails(), gather);
+    if (st != UOE_OK) return st;
+    if (gather) st = launch_quantize_rows(x, true, 1, tokens, D.d, base + W.xq, (float*)(base + W.xs), SrcMap(), nullptr, 0, "fp8_quantize_x", s, true);
     else st = launch_quantize_rows(x, true, 1, D.Rmax, D.d, base + W.xq, (float*)(base + W.xs), row_map_of(D, P, patch_idx), expert_offsets, D.n, "fp8_gather", s);
     if (st != UOE_OK) return st;
     Fp8Gemm g1{base + W.xq, (float*)(base + W.xs), W1, w1_scale, expert_offsets, D.n, D.Rmax, D.d_e, D.d, false, nullptr, true};

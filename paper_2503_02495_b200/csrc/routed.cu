@@ -64,9 +64,10 @@ plan_kernel(const int* __restrict__ expert_idx, const int* __restrict__ patch_id
             int* __restrict__ expert_end, int* status, float* __restrict__ row_gate, float* __restrict__ row_valid,
             int Lv, int use_gate, int* __restrict__ src_patch, const PlanTails tails,
             long long rows_max, int rows_given /* pair_row and slot_pair are already there (plan_rows_kernel) */,
-            int* __restrict__ slot_pair, int slot_shift) {
-    pdl_trigger();
+            int* __restrict__ slot_pair, int slot_shift, int trigger_late) {
+    if (!trigger_late) pdl_trigger();
     pdl_wait();
+    if (trigger_late) pdl_trigger();           // the next kernel finds everything before this one finished
     extern __shared__ int s_dyn[];
     int* s_pi = s_dyn;                         // [k*c] patch indices of this sample
     float* s_g = (float*)(s_dyn + k * c);      // [k*c] gates
@@ -487,7 +488,8 @@ constexpr long long kF32LargeTiles = 160;
 }  // namespace
 
 uoe_status launch_plan(const Dims& D, const int* expert_idx, const int* patch_idx, const float* gate,
-                       const int* offsets, const PlanPtrs& P, int* status, cudaStream_t s, bool use_gate, const PlanTails& tails) {
+                       const int* offsets, const PlanPtrs& P, int* status, cudaStream_t s, bool use_gate, const PlanTails& tails,
+                       bool trigger_late) {
     const size_t smem = (size_t)D.k * D.c * 8;
     if (smem > 32 * 1024) return UOE_ERR_UNSUPPORTED;      // a sample's routing arrays live in shared memory
     const bool many = D.B > kPlanScanMaxB;
@@ -501,7 +503,7 @@ uoe_status launch_plan(const Dims& D, const int* expert_idx, const int* patch_id
     const int threads = P.row_gate ? 512 : 128;      // the backward's per-row weights: k*l_a rows per sample (image block, training step: 672 us with 128, 670 so)
     launch_k(plan_kernel, dim3(D.B), dim3(threads), smem, s, expert_idx, patch_idx, gate, offsets, D.B, D.n, D.k, D.m, D.c, D.l_p,
                                     P.pair_row, P.inv_row, P.inv_gate, P.expert_end, status, P.row_gate, P.row_valid,
-                                    D.Lv, use_gate ? 1 : 0, P.src_patch, tails, D.Rmax, many ? 1 : 0, P.slot_pair, pair_slot_shift(D.l_a));
+                                    D.Lv, use_gate ? 1 : 0, P.src_patch, tails, D.Rmax, many ? 1 : 0, P.slot_pair, pair_slot_shift(D.l_a), trigger_late ? 1 : 0);
     UOE_LAUNCHED();
     return UOE_OK;
 }
