@@ -291,3 +291,72 @@ def test_a_scale_that_is_no_power_of_two_is_reported():
         assert torch.isnan(C[150]).all()
         C[150] = ref[150]
         assert torch.equal(C, ref)
+
+
+@pytest.mark.parametrize("counts, N, K, any_scale", [([3], 300, 1000, False), ([250], 300, 9000, False), ([300, 0, 500], 200, 260, True),
+                                                     ([5000, 128, 4100], 1030, 640, False)])
+def test_captured_and_on_two_streams(counts, N, K, any_scale):
+    """Quantisation, product and weight gradient in one graph: replays follow what is in x; two streams with a workspace each do not meet."""
+    import paper_2503_02495_b200 as uoe
+    n, off = len(counts), _regions(counts)
+    M = counts[0] if n == 1 else off[-1]
+    live = torch.zeros(M, 1)
+    for o, cnt in zip(off, counts):
+        live[o:o + cnt] = 1
+    xs = [(_rand(3 + i, M, K) * live).cuda() for i in range(2)]
+    dy = (_rand(7, M, N) * live).cuda()
+    W, sw = uoe.uoe_fp8_quantize(_rand(2, n, N, K).cuda(), "blocks")
+    o = torch.tensor(off, dtype=torch.int32, device="cuda") if n > 1 else None
+    prob = uoe.Fp8Problem(n=n, M=M, N=N, K=K, any_scale=any_scale)
+    wprob = uoe.Fp8Problem(n=n, M=K, N=N, K=M, dtype="f32", any_scale=any_scale)
+
+    def step(x, ws):
+        A, sa = uoe.uoe_fp8_quantize(x, "rows")
+        C = uoe.uoe_fp8_gemm(prob, A, sa, W, sw, o, ws=ws, check=False)
+        return C[:off[-1]], uoe.uoe_fp8_wgrad(wprob, *uoe.uoe_fp8_quantize(x, "cols"), *uoe.uoe_fp8_quantize(dy, "cols"), o, ws=ws, check=False)
+
+    wss = [uoe.alloc_fp8_workspace(prob) for _ in range(2)]
+    want = [[t.clone() for t in step(x, wss[0])] for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(3):
+        got = [None, None]
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                got[i] = step(xs[i], wss[i])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for g, w in zip(got, want) for a, b in zip(g, w))
+    held = xs[0].clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step(held, wss[0])
+    for i in (0, 1, 0):
+        held.copy_(xs[i])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want[i]))
+
+
+def test_offsets_that_pass_32_bits():
+    """More than 2^32 bytes of input and 2^31 elements: the last rows are what they are alone."""
+    import paper_2503_02495_b200 as uoe
+    R, C = 2 ** 20 + 131, 2056
+    x = torch.zeros(R, C, dtype=torch.bfloat16, device="cuda")
+    tail = _rand(4, 200, C, dtype=torch.bfloat16)
+    x[-200:] = tail.cuda()
+    for layout in ("rows", "cols"):
+        q, s = uoe.uoe_fp8_quantize(x, layout)
+        if layout == "rows":
+            qr, sr = _layout_ref(tail, layout)
+            assert torch.equal(q[-200:].float().double().cpu(), qr) and torch.equal(s[:, -200:].double().cpu(), sr)
+        else:
+            rest = R % BLOCK or BLOCK                                      # rows of the last block
+            qr, sr = _layout_ref(tail[-rest:], layout)
+            assert torch.equal(q[:, -BLOCK:][:, :rest].float().double().cpu(), qr[:, :rest]) and torch.equal(s[-1].double().cpu(), sr[0])
+        del q, s
+    del x
+    A, sa = uoe.uoe_fp8_quantize(torch.cat([torch.zeros(R - 200, 24), tail[:, :24].float()]).cuda(), "rows")
+    W, sw = uoe.uoe_fp8_quantize(_rand(5, 1, C, 24).cuda(), "blocks")
+    got = uoe.uoe_fp8_gemm(uoe.Fp8Problem(n=1, M=R, N=C, K=24), A, sa, W, sw)[-200:]
+    a, w = _vec_values(A[-200:].cpu(), sa[:, -200:].cpu()), _blk_values(W[0].cpu(), sw[0].cpu())
+    _close(got, a @ w.t(), _gamma(1) * (a.abs() @ w.abs().t()), "bf16")

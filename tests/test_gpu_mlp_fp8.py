@@ -35,6 +35,7 @@ CASES = {
     "pairs_of_ctas": (_w(B=40, L=1152, L_valid=1152, m=9, c=3, d=256, n=4, k=2, d_ff=4 * 320, w_std=0.05), {}),
     "gathered_patches_of_8": (_w(B=14, L=1152, L_valid=1130, m=144, c=48, d=200, n=8, k=4, d_ff=8 * 320, w_std=0.05), dict(bias=True)),
     "gathered_patches_of_64": (_w(B=9, L=2048, L_valid=2048, m=32, c=9, d=264, n=12, k=4, d_ff=12 * 392, act="gelu_erf", w_std=0.05), {}),
+    "hidden_width_of_33": (_w(B=3, L=64, L_valid=64, m=4, c=3, d=72, n=4, k=2, d_ff=4 * 33, act="gelu_tanh"), dict(bias=True)),
     "gathered_whole_samples": (_w(B=7, L=256, L_valid=256, m=2, c=2, d=136, n=8, k=2, d_ff=8 * 136), {}),
 }
 
