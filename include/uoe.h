@@ -316,7 +316,8 @@ uoe_status uoe_fp8_wgrad(const uoe_fp8_problem* prob, const void* A, const float
  *   W1 [n, d_e, dp], w1_scale and W2 [n, d, d_ep], w2_scale: UOE_FP8_BLOCKS_T of W1 [n, d, d_e] and W2 [n, d_e, d] (dp, d_ep: d, d_e
  *   rounded up to UOE_FP8_BLOCK); scales other than powers of two only with UOE_FLAG_FP8_ANY_SCALE.
  * The rows that enter a product are quantised as UOE_FP8_ROWS, a scale per row and 128 columns: the routed rows of x, and
- * phi( ... + b1) in float32.  Products, biases and phi are float32; the experts' outputs are bfloat16 before the weighted sum.
+ * phi( ... + b1) in float32.  Products, biases and phi are float32; the experts' outputs are float32 or
+ * bfloat16 before the weighted sum, which is float32 (they stay float32 where patches are 128 tokens and enough to fill the GPU).
  * bfloat16 problems only (x, biases and y).  Everything else as for uoe_mlp_forward; workspace: UOE_OP_MLP_FWD_FP8.
  */
 uoe_status uoe_mlp_forward_fp8(const uoe_problem* prob, const void* x, const void* W1, const float* w1_scale, const void* W2,

@@ -96,4 +96,10 @@ struct Fp8Gemm {
 inline bool fp8_can_gather(int l_p) { return l_p % 8 == 0 && 128 % l_p == 0; }
 uoe_status launch_fp8_gemm(const Fp8Gemm& g, int* status, cudaStream_t s);
 
+// Second layer and combine in one kernel, walked by output patch (fp8_patch_tcgen05.cu; scales are powers of two).
+//   a [Rmax, d_e padded], as: the hidden rows, quantised by row; W2, w2_scale and b2 as for uoe_mlp_forward_fp8
+bool fp8_patch_can(const Dims& D);
+uoe_status launch_fp8_patch(const Dims& D, const void* a, const float* as, const void* W2, const float* w2_scale, const void* b2, const void* x, void* y,
+                            const int* offsets, const PlanPtrs& P, bool use_gate, bool residual, int* status, cudaStream_t s);
+
 }  // namespace uoe

@@ -53,15 +53,6 @@ struct Ctl {
 };
 static_assert(sizeof(Ctl) <= 1024, "control block");
 
-// The scale's exponent byte in all four bytes of a word; 0xff, which stands for NaN, where it is no power of two (a scale that is NaN
-// itself is no news).  Without a branch: a look at the status word per scale cost 1000 cycles per block.
-__device__ __forceinline__ uint32_t exponent_word(float s, bool there, bool& bad) {
-    const uint32_t b = there ? __float_as_uint(s) : 0x3f800000u, e = b >> 23;
-    const bool pow2 = (b & 0x7fffffu) == 0 && e - 1 < 254u;
-    bad |= !pow2 && e != 255;
-    return __byte_perm(pow2 ? e : 255u, 0, 0);
-}
-
 struct NoMap {};                          // what a kernel without gathered rows takes in the map's place
 
 template <int BN, bool WGRAD, int EPI, bool PAIR, bool SPLIT, bool GATHER>

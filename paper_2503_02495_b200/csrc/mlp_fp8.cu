@@ -1,8 +1,8 @@
 // uoe_mlp_forward_fp8: the UoME forward (Eq. 37-40) on 8-bit expert weights:
 //   plan, quantisation of x -> gather (Eq. 18) inside the product's loads, bias, phi and quantisation again (Eq. 38) -> product and bias
-//   (Eq. 39) -> weighted combine (Eq. 20 / 40).
+//   (Eq. 39) -> weighted combine (Eq. 20 / 40), these two in one kernel for patches of 128 tokens (fp8_patch_tcgen05.cu).
 // The rows exist as bytes only: every token is quantised once, the first product's write-out finds the largest of a row's 128 hidden columns
-// in one thread's registers, and only the experts' outputs are bfloat16.  Where patches do not tile 128 rows, where fewer rows are routed than
+// in one thread's registers, and only the experts' outputs are bfloat16, if they reach memory at all.  Where patches do not tile 128 rows, where fewer rows are routed than
 // there are tokens, or where the weights' scales are not powers of two, the routed rows are quantised into a buffer of their own (scale layer,
 // 4 x 4096 tokens of 4096, each routed twice: 79 us for that, 44 us for the tokens once, and 3 us more in the product).
 #include "fp8.cuh"
@@ -70,6 +70,9 @@ extern "C" uoe_status uoe_mlp_forward_fp8(const uoe_problem* prob, const void* x
     g1.label = "fp8_gemm1_act";
     st = launch_fp8_gemm(g1, status, s);
     if (st != UOE_OK) return st;
+    if (!any_scale && fp8_patch_can(D))
+        return launch_fp8_patch(D, base + W.aq, (float*)(base + W.as), W2, w2_scale, b2, x, y, expert_offsets, P, (prob->flags & UOE_FLAG_GATE) != 0,
+                                (prob->flags & UOE_FLAG_RESIDUAL) != 0, status, s);
     Fp8Gemm g2{base + W.aq, (float*)(base + W.as), W2, w2_scale, expert_offsets, D.n, D.Rmax, D.d, D.d_e, false, base + W.z, true};
     g2.bias = b2;
     g2.any_scale = any_scale;

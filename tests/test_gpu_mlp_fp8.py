@@ -36,6 +36,9 @@ CASES = {
     "gathered_patches_of_8": (_w(B=14, L=1152, L_valid=1130, m=144, c=48, d=200, n=8, k=4, d_ff=8 * 320, w_std=0.05), dict(bias=True)),
     "gathered_patches_of_64": (_w(B=9, L=2048, L_valid=2048, m=32, c=9, d=264, n=12, k=4, d_ff=12 * 392, act="gelu_erf", w_std=0.05), {}),
     "hidden_width_of_33": (_w(B=3, L=64, L_valid=64, m=4, c=3, d=72, n=4, k=2, d_ff=4 * 33, act="gelu_tanh"), dict(bias=True)),
+    "by_patch": (_w(B=11, L=1280, L_valid=1201, m=10, c=5, d=520, n=7, k=5, d_ff=7 * 200, act="gelu_tanh", w_std=0.05), dict(bias=True)),
+    "by_patch_one_block": (_w(B=30, L=768, L_valid=768, m=6, c=2, d=264, n=5, k=2, d_ff=5 * 40), dict(gate=False, residual=False)),
+    "by_patch_all_experts": (_w(B=20, L=1024, L_valid=900, m=8, c=8, d=136, n=3, k=3, d_ff=3 * 392, w_std=0.05), {}),
     "gathered_whole_samples": (_w(B=7, L=256, L_valid=256, m=2, c=2, d=136, n=8, k=2, d_ff=8 * 136), {}),
 }
 
@@ -124,7 +127,7 @@ def test_mlp_fp8(name):
     assert torch.equal(got, uoe.uoe_mlp_forward_fp8(prob, to_dev(x), W1, s1, W2, s2, r, b1=bd[0], b2=bd[1]))
 
 
-@pytest.mark.parametrize("name", ["several_tiles", "gathered_patches_of_8", "small"])
+@pytest.mark.parametrize("name", ["several_tiles", "gathered_patches_of_8", "small", "by_patch"])
 def test_captured_and_on_two_streams(name):
     """Replays follow the tensors' contents; two streams with a workspace each do not meet."""
     import paper_2503_02495_b200 as uoe
