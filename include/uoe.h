@@ -268,6 +268,13 @@ typedef enum { UOE_FP8_ROWS = 0, UOE_FP8_COLS = 1, UOE_FP8_BLOCKS = 2, UOE_FP8_B
 uoe_status uoe_fp8_quantize(int32_t G, int32_t R, int32_t C, int32_t dtype, int32_t layout, const void* x, void* q, float* scale,
                             void* cuda_stream);
 
+/*
+ * Values of a quantised operand that lie the other way round (the contraction not contiguous, as a quantiser that keeps the input's layout
+ * leaves a scale per column): q [G, C, R] = x [G, R, C] transposed, bytes; R a multiple of UOE_FP8_BLOCK.  The scales are laid out alike
+ * either way.  Device pointers; q distinct from x.
+ */
+uoe_status uoe_fp8_transpose(int32_t G, int32_t R, int32_t C, const void* x, void* q, void* cuda_stream);
+
 /* A product of 8-bit operands.  Any sizes >= 1; n <= 32. */
 typedef struct {
     int32_t n;        /* experts */

@@ -9,6 +9,6 @@ from .binding import (  # noqa: F401
     uoe_smha_forward, uoe_smha_backward, uoe_workspace_bytes, UOE_OP_ROUTE, UOE_OP_MLP_FWD, UOE_OP_MLP_BWD, UOE_OP_SMHA_FWD,
     UOE_OP_SMHA_BWD,
     UOE_ROW_ALIGN, alloc_block_workspace, uoe_block_forward, uoe_block_workspace_bytes,
-    Fp8Problem, alloc_fp8_workspace, uoe_fp8_gemm, uoe_fp8_quantize, uoe_fp8_wgrad, uoe_fp8_workspace_bytes, UOE_FP8_BLOCK,
+    Fp8Problem, alloc_fp8_workspace, uoe_fp8_gemm, uoe_fp8_quantize, uoe_fp8_transpose, uoe_fp8_wgrad, uoe_fp8_workspace_bytes, UOE_FP8_BLOCK,
     uoe_mlp_forward_fp8, uoe_mlp_tokens, UOE_OP_MLP_FWD_FP8, UOE_OP_MLP_TOKENS,
 )

@@ -142,6 +142,8 @@ def _load():
     p8, i32 = ctypes.POINTER(_Fp8Problem), ctypes.c_int32
     lib.uoe_fp8_quantize.restype = ctypes.c_int
     lib.uoe_fp8_quantize.argtypes = [i32, i32, i32, i32, i32, vp, vp, f32p, vp]
+    lib.uoe_fp8_transpose.restype = ctypes.c_int
+    lib.uoe_fp8_transpose.argtypes = [i32, i32, i32, vp, vp, vp]
     lib.uoe_fp8_workspace_bytes.restype = sz
     lib.uoe_fp8_workspace_bytes.argtypes = [p8]
     for f in (lib.uoe_fp8_gemm, lib.uoe_fp8_wgrad):
@@ -445,6 +447,20 @@ def uoe_fp8_quantize(x, layout: str, q=None, scale=None):
     return q, scale
 
 
+def uoe_fp8_transpose(x, q=None):
+    """Values of 8-bit operands [.., R, C], R a multiple of 128, as [.., C, R] (see uoe.h)."""
+    assert x.dim() in (2, 3), "x must be [R,C] or [G,R,C]"
+    _contig(x, torch.float8_e4m3fn)
+    _here(x)
+    shape = (*x.shape[:-2], x.shape[-1], x.shape[-2])
+    q = q if q is not None else torch.empty(shape, dtype=torch.float8_e4m3fn, device=x.device)
+    _contig(q, torch.float8_e4m3fn)
+    assert tuple(q.shape) == shape, f"expected q {shape}"
+    st = _lib.uoe_fp8_transpose(x.shape[0] if x.dim() == 3 else 1, x.shape[-2], x.shape[-1], _ptr(x), _ptr(q), _stream())
+    _check(st, "uoe_fp8_transpose")
+    return q
+
+
 def uoe_fp8_workspace_bytes(prob: Fp8Problem) -> int:
     return int(_lib.uoe_fp8_workspace_bytes(ctypes.byref(prob.c_struct())))
 
@@ -459,6 +475,13 @@ def alloc_fp8_workspace(prob: Fp8Problem, device="cuda") -> torch.Tensor:
     return ws
 
 
+def _fp8_laid_out(t):
+    """An operand whose contraction is not contiguous (the transpose of a contiguous tensor) as the products take it."""
+    if t.is_contiguous() or t.dim() not in (2, 3) or not t.transpose(-1, -2).is_contiguous():
+        return t
+    return uoe_fp8_transpose(t.transpose(-1, -2))
+
+
 def _fp8_operand(t, scale, shape, s_shape):
     _contig(t, torch.float8_e4m3fn)
     _contig(scale, torch.float32)
@@ -468,8 +491,9 @@ def _fp8_operand(t, scale, shape, s_shape):
 
 def uoe_fp8_gemm(prob: Fp8Problem, A, a_scale, W, w_scale, expert_offsets=None, C=None, ws=None, check: bool = True):
     """C [M,N] = rows A times the weights of each row's expert (8-bit operands, see uoe.h).  Without C a new tensor is returned, zero
-    behind the last region."""
+    behind the last region.  A and W may be transposes of contiguous tensors; the call then lays their values out first."""
     _here(A)
+    A, W = _fp8_laid_out(A), _fp8_laid_out(W)
     blk = lambda v: -(-v // UOE_FP8_BLOCK)
     Kb, Nb = blk(prob.K), blk(prob.N)
     _fp8_operand(A, a_scale, (1, prob.M, Kb * UOE_FP8_BLOCK), (1, Kb, prob.M))
@@ -489,8 +513,10 @@ def uoe_fp8_gemm(prob: Fp8Problem, A, a_scale, W, w_scale, expert_offsets=None, 
 
 
 def uoe_fp8_wgrad(prob: Fp8Problem, A, a_scale, B, b_scale, expert_offsets=None, dW=None, ws=None, check: bool = True):
-    """dW [n,M,N] float32 = A B^T over the rows of each expert's region (8-bit operands, see uoe.h)."""
+    """dW [n,M,N] float32 = A B^T over the rows of each expert's region (8-bit operands, see uoe.h).  A and B may be transposes of contiguous
+    tensors, as quantising by columns without turning leaves them; the call then lays their values out first."""
     _here(A)
+    A, B = _fp8_laid_out(A), _fp8_laid_out(B)
     Kb = -(-prob.K // UOE_FP8_BLOCK)
     _fp8_operand(A, a_scale, (1, prob.M, Kb * UOE_FP8_BLOCK), (1, Kb, prob.M))
     _fp8_operand(B, b_scale, (1, prob.N, Kb * UOE_FP8_BLOCK), (1, Kb, prob.N))

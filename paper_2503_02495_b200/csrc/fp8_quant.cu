@@ -9,6 +9,8 @@
 //                          it is or transposed, or a scale per column and 128 rows, transposed.  Transposed bytes pass through
 //                          shared memory, eight rows of a column in one 8-byte store, swizzled so that neither side meets a bank
 //                          twice.
+//   transpose_kernel       uoe_fp8_transpose: bytes of a quantised operand whose contraction is not contiguous, a CTA per 128 x 128 tile, a
+//                          thread 4 rows x 16 columns: 4 x 4 bytes turned in registers, words swizzled through shared memory.
 #include "fp8.cuh"
 
 namespace uoe {
@@ -194,6 +196,51 @@ quantize_tile_kernel(const T* __restrict__ x, uint8_t* __restrict__ q, float* __
     }
 }
 
+// q [C, R] = x [R, C] transposed, R a multiple of 128: the rows of q are whole 16-byte pieces, those of x where whole16 says so.
+__global__ void __launch_bounds__(256)
+transpose_kernel(const uint8_t* __restrict__ x, uint8_t* __restrict__ q, int R, int C, int Cb, int whole16) {
+    pdl_trigger();
+    __shared__ __align__(16) uint32_t s_t[kQ * 32];   // word (column, four rows g) at column * 32 + (g ^ 4 (column / 16)): no bank twice on either side
+    const int tid = threadIdx.x, cg = tid & 7, rg = tid >> 3;
+    const long long per_mat = (long long)(R / kQ) * Cb;
+    const long long mat = blockIdx.x / per_mat;
+    const int rb = (int)((blockIdx.x - mat * per_mat) / Cb), cb = (int)((blockIdx.x - mat * per_mat) % Cb);
+    const int c0 = cb * kQ + cg * 16;
+    x += (mat * R + rb * kQ + rg * 4) * C;
+    pdl_wait();
+    uint32_t v[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint8_t* row = x + (long long)i * C;
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (whole16) {
+            if (c0 < C) w = ld_stream16(row + c0);
+        } else {
+            uint32_t b[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (c0 + j < C) b[j / 4] |= (uint32_t)row[c0 + j] << (8 * (j % 4));
+            w = make_uint4(b[0], b[1], b[2], b[3]);
+        }
+        v[i][0] = w.x; v[i][1] = w.y; v[i][2] = w.z; v[i][3] = w.w;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {                      // columns 4 j .. 4 j + 3 of the thread's sixteen
+        const uint32_t a = __byte_perm(v[0][j], v[1][j], 0x5140), b = __byte_perm(v[2][j], v[3][j], 0x5140);      // columns 0, 1 of rows 0, 1 / 2, 3
+        const uint32_t c = __byte_perm(v[0][j], v[1][j], 0x7362), d = __byte_perm(v[2][j], v[3][j], 0x7362);      // columns 2, 3
+        const uint32_t o[4] = {__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632), __byte_perm(c, d, 0x5410), __byte_perm(c, d, 0x7632)};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s_t[(cg * 16 + 4 * j + i) * 32 + (rg ^ (4 * cg))] = o[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const int col = p * 32 + (tid >> 3), t = tid & 7;
+        const uint4 w = *(const uint4*)(s_t + col * 32 + 4 * (t ^ (col >> 4)));
+        if (cb * kQ + col < C) *(uint4*)(q + (mat * C + cb * kQ + col) * R + rb * kQ + t * 16) = w;
+    }
+}
+
 template <typename T>
 uoe_status launch_tile(int layout, int G, int R, int C, const void* x, void* q, float* scale, cudaStream_t s) {
     const int Rb = q_blocks(R), Cb = q_blocks(C), whole = ((size_t)C * sizeof(T)) % 16 == 0;
@@ -239,4 +286,19 @@ extern "C" uoe_status uoe_fp8_quantize(int32_t G, int32_t R, int32_t C, int32_t 
     cudaStream_t s = (cudaStream_t)cuda_stream;
     if (layout == UOE_FP8_ROWS) return launch_quantize_rows(x, dtype == UOE_BF16, G, R, C, q, scale, SrcMap(), nullptr, 0, "fp8_quantize", s);
     return dtype == UOE_BF16 ? launch_tile<__nv_bfloat16>(layout, G, R, C, x, q, scale, s) : launch_tile<float>(layout, G, R, C, x, q, scale, s);
+}
+
+extern "C" uoe_status uoe_fp8_transpose(int32_t G, int32_t R, int32_t C, const void* x, void* q, void* cuda_stream) {
+    if (G < 1 || R < 1 || C < 1 || R % kQ != 0) return UOE_ERR_INVALID_ARG;
+    if (!x || !q || x == q || !aligned16(x) || !aligned16(q)) return UOE_ERR_INVALID_ARG;
+    if (C > 0x7fffffff - kQ) return UOE_ERR_UNSUPPORTED;
+    const int Cb = q_blocks(C);
+    // (three factors of up to 2^24: past 64 bits, so that the first two are looked at alone)
+    const long long rows = (long long)G * (R / kQ);
+    if (rows > 0x7fffffffll || rows * Cb > 0x7fffffffll) return UOE_ERR_UNSUPPORTED;
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    ProfScope ps("fp8_transpose", s);
+    launch_k(transpose_kernel, dim3((unsigned)(rows * Cb)), dim3(256), 0, s, (const uint8_t*)x, (uint8_t*)q, R, C, Cb, C % 16 == 0 ? 1 : 0);
+    UOE_LAUNCHED();
+    return UOE_OK;
 }

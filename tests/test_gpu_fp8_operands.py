@@ -1,0 +1,88 @@
+"""GPU parity: operands of the 8-bit products as callers hold them.
+
+A transposed operand holds the same values, so the product has the same bits; its values are moved, not computed, and are compared exactly.
+"""
+import pytest
+import torch
+
+from tests.test_gpu_fp8 import BLOCK, _blk_values, _close, _gamma, _rand, _regions, _vec_values
+
+pytestmark = pytest.mark.gpu
+
+
+def _turned(q):
+    """The same values with the contraction not contiguous."""
+    t = q.transpose(-1, -2).view(torch.uint8).contiguous().view(q.dtype).transpose(-1, -2)
+    assert t.shape == q.shape and (1 in q.shape or not t.is_contiguous())
+    return t
+
+
+@pytest.mark.parametrize("G, R, C", [(1, 128, 1), (1, 128, 16), (1, 256, 77), (3, 384, 129), (2, 128, 1000), (1, 1280, 4096), (5, 256, 33)])
+def test_transpose(G, R, C):
+    import paper_2503_02495_b200 as uoe
+    g = torch.Generator().manual_seed(R + C)
+    x = torch.randint(0, 256, (G, R, C), generator=g, dtype=torch.uint8)
+    buf = torch.full((G * R * C + 256,), 7, dtype=torch.uint8, device="cuda")
+    q = buf[:G * R * C].view(G, C, R).view(torch.float8_e4m3fn)
+    uoe.uoe_fp8_transpose(x.cuda().view(torch.float8_e4m3fn), q=q)
+    assert torch.equal(q.view(torch.uint8).cpu(), x.transpose(1, 2)) and (buf[G * R * C:] == 7).all()
+
+
+@pytest.mark.parametrize("any_scale", [False, True])
+@pytest.mark.parametrize("counts, M, N", [([1], 8, 8), ([130, 0, 400, 1], 77, 333), ([300, 0, 128, 500], 512, 256), ([3000, 1000], 1100, 600)])
+def test_wgrad_of_operands_that_lie_the_other_way_round(counts, M, N, any_scale):
+    """Operands quantised by columns and not turned, strides (1, M): against float64, and with the bits of the turned ones."""
+    import paper_2503_02495_b200 as uoe
+    off = _regions(counts)
+    x, dy = torch.zeros(off[-1], M), torch.zeros(off[-1], N)
+    for o, cnt in zip(off, counts):
+        x[o:o + cnt], dy[o:o + cnt] = _rand(o + 1, cnt, M, wide=True), _rand(o + 2, cnt, N)
+    A, sa = uoe.uoe_fp8_quantize(x.cuda(), "cols")
+    B, sb = uoe.uoe_fp8_quantize(dy.cuda(), "cols")
+    prob = uoe.Fp8Problem(n=len(counts), M=M, N=N, K=off[-1], dtype="f32", any_scale=any_scale)
+    o = torch.tensor(off, dtype=torch.int32, device="cuda")
+    got = uoe.uoe_fp8_wgrad(prob, _turned(A), sa, _turned(B), sb, o)
+    assert torch.equal(got, uoe.uoe_fp8_wgrad(prob, A, sa, B, sb, o))
+    assert torch.equal(got, uoe.uoe_fp8_wgrad(prob, A, sa, _turned(B), sb, o))
+    a, b = _vec_values(A.cpu(), sa.cpu()), _vec_values(B.cpu(), sb.cpu())
+    for e, cnt in enumerate(counts):
+        ae, be = a[:, off[e]:off[e + 1]], b[:, off[e]:off[e + 1]]
+        _close(got[e], ae @ be.t(), _gamma(-(-cnt // BLOCK)) * (ae.abs() @ be.abs().t()), "f32")
+
+
+@pytest.mark.parametrize("counts, N, K", [([3], 300, 1000), ([200, 0, 70], 140, 330)])
+def test_gemm_of_operands_that_lie_the_other_way_round(counts, N, K):
+    import paper_2503_02495_b200 as uoe
+    n, off = len(counts), _regions(counts)
+    M = counts[0] if n == 1 else off[-1]
+    A, sa = uoe.uoe_fp8_quantize(_rand(1, M, K).cuda(), "rows")
+    W, sw = uoe.uoe_fp8_quantize(_rand(2, n, N, K).cuda(), "blocks")
+    o = torch.tensor(off, dtype=torch.int32, device="cuda") if n > 1 else None
+    prob = uoe.Fp8Problem(n=n, M=M, N=N, K=K)
+    got = uoe.uoe_fp8_gemm(prob, _turned(A), sa, _turned(W), sw, o)
+    assert torch.equal(got, uoe.uoe_fp8_gemm(prob, A, sa, W, sw, o))
+    a = _vec_values(A.cpu(), sa.cpu())
+    for e in range(n):
+        s = slice(off[e], off[e + 1] if n > 1 else M)
+        w = _blk_values(W[e].cpu(), sw[e].cpu())
+        _close(got[s], a[s] @ w.t(), _gamma(-(-K // BLOCK)) * (a[s].abs() @ w.abs().t()), "bf16")
+
+
+def test_wgrad_of_turned_operands_captured():
+    import paper_2503_02495_b200 as uoe
+    q = [uoe.uoe_fp8_quantize(_rand(s, 256, c).cuda(), "cols") for s, c in ((1, 200), (2, 72))]
+    (A, sa), (B, sb) = q
+    At, Bt = _turned(A), _turned(B)
+    prob = uoe.Fp8Problem(n=1, M=200, N=72, K=256, dtype="f32")
+    ws = uoe.alloc_fp8_workspace(prob)
+    want = uoe.uoe_fp8_wgrad(prob, A, sa, B, sb, ws=ws)
+    dW = torch.empty_like(want)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        uoe.uoe_fp8_wgrad(prob, At, sa, Bt, sb, dW=dW, ws=ws, check=False)
+    for _ in range(2):
+        dW.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(dW, want)
