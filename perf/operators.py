@@ -130,7 +130,7 @@ def _q_vec(x):
     x = torch.nn.functional.pad(x, (0, -C % BLOCK))
     t = x.unflatten(-1, (-1, BLOCK))
     r, s = _amax_scale(t.abs().amax(-1))
-    return (t * r.unsqueeze(-1)).flatten(-2).to(F8).contiguous(), s.transpose(-1, -2).contiguous()
+    return (t * r.unsqueeze(-1)).flatten(-2).to(F8), s.transpose(-1, -2).contiguous()
 
 
 def _q_blk(x):
