@@ -375,8 +375,8 @@ uoe_status uoe_block_forward(const uoe_problem* att, const uoe_problem* mlp, con
  *   y[b] = x[b] + sum over the k chosen experts i of token b  gate[b,i] * ( phi( x[b] W1[i] + b1[i] ) W2[i] + b2[i] )
  * with gate = p_samp^2 (UOE_FLAG_GATE: P_samp times the gate of the token's one patch) or 1, and the residual by UOE_FLAG_RESIDUAL.  Every
  * chosen expert's weights are read once.
- *   Weights in prob->dtype as for uoe_mlp_forward (w1_scale = w2_scale = NULL), or, for bfloat16 problems, 8-bit as for
- *   uoe_mlp_forward_fp8 with any float32 scales.  x and the hidden rows (rounded to bfloat16) enter those products as two e4m3 terms
+ *   Weights in prob->dtype as for uoe_mlp_forward (w1_scale = w2_scale = NULL; rows of d_e elements are multiples of 16 bytes, else
+ *   UOE_ERR_UNSUPPORTED), or, for bfloat16 problems, 8-bit as for uoe_mlp_forward_fp8 with any float32 scales and any d_e.  x and the hidden rows (rounded to bfloat16) enter those products as two e4m3 terms
  *   each: exactly, but for values below 2^-13 of the largest in their block of 128, which are off by 2^-21 of that largest at most.
  *   r: host pointer to device arrays that receive the router's outputs, or NULL.    y: distinct from x.
  *   A token that holds a NaN gets the first k experts.

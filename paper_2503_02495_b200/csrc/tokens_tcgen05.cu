@@ -512,7 +512,8 @@ extern "C" uoe_status uoe_mlp_tokens(const uoe_problem* prob, const void* x, con
         if (p && !aligned16(p)) return UOE_ERR_INVALID_ARG;
     if (x == y) return UOE_ERR_INVALID_ARG;
     if (r && (!r->expert_idx || !r->patch_idx || !r->gate || !r->p_samp || !r->p_patch || !r->expert_offsets)) return UOE_ERR_INVALID_ARG;
-    if (D.L != 1 || D.B > kMaxTokens || (D.d_e * D.esize) % 16 != 0 || (w1_scale && !D.bf16)) return UOE_ERR_UNSUPPORTED;
+    if (D.L != 1 || D.B > kMaxTokens || (w1_scale && !D.bf16)) return UOE_ERR_UNSUPPORTED;
+    if (!w1_scale && (D.d_e * D.esize) % 16 != 0) return UOE_ERR_UNSUPPORTED;      // rows of W1 and of the hidden values move in 16-byte pieces
     if (ws_bytes < mlp_tokens_workspace_bytes(D)) return UOE_ERR_WORKSPACE;
     TokArgs a = {};
     a.x = x; a.Wr = W_r; a.W1 = W1; a.W2 = W2; a.b1 = b1; a.b2 = b2; a.s1 = w1_scale; a.s2 = w2_scale;
