@@ -97,7 +97,7 @@ __device__ __forceinline__ void store_tile(const Fp8Args& a, const CUtensorMap* 
         static_assert(EPI != kFp8ActQuant || (!WGRAD && CW == kQ), "a thread holds one block of the result");
         if (row >= row_end) return;
         uint32_t m = 0;
-        act_precise_n<CW>(sum, a.act);
+        act_fast_n<CW>(sum, a.act);
 #pragma unroll
         for (int q = 0; q < CW; ++q) m = max(m, abs_bits(sum[q]));
         const BlockScale b = block_scale(m);

@@ -144,7 +144,7 @@ first_layer_f32_kernel(const TokArgs a, int S) {
             if (col >= a.d_e || !((R.of[slot] >> tok) & 1)) continue;
             float h = a.b1 ? ((const float*)a.b1)[(size_t)e * a.d_e + col] : 0.f;
             for (int s = 0; s < S; ++s) h += ld_cluster_f32(sm.cta + q, first + s);
-            out[(size_t)tok * a.d_e + col] = act_precise(h, a.act);
+            out[(size_t)tok * a.d_e + col] = act_f32(h, a.act);
         }
     }
     if (S > 1) cluster_sync_all();      // nobody's shared memory goes while another CTA may read it

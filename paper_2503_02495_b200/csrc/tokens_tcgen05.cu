@@ -347,7 +347,7 @@ first_layer_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
                 for (int s = 0; s < S; ++s) h[v] += ld_cluster_f32(cta + tok * Cf::PITCH + W * lane + v, first + s);
                 if (a.b1 && col < a.d_e) h[v] += to_f32(((const bf16*)a.b1)[(size_t)e * a.d_e + col]);
                 // (half a step, 2^-8 of the value, like the hidden rows of uoe_mlp_forward)
-                h[v] = col < a.d_e ? to_f32(__float2bfloat16_rn(act_precise(h[v], a.act))) : 0.f;
+                h[v] = col < a.d_e ? to_f32(__float2bfloat16_rn(act_fast(h[v], a.act))) : 0.f;
             }
             if constexpr (WT == kFp8) {
                 uint32_t hi, lo;

@@ -23,3 +23,24 @@ def test_8_bit_weights_of_any_hidden_width(T, d, d_e, bias):
     assert torch.equal(r.expert_idx.cpu().long(), e)
     _check(got, y, bound)
     assert torch.equal(got, call())
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu_tanh"])
+def test_float32_activation_keeps_its_bits(act):
+    """phi alone (both layers the identity, no gate, no residual) over the whole range where it is not zero.
+
+    SiLU h / (1 + e^-h): e^-h is off by 2 steps of float32 (2 x 2^-23 of it), the sum and the quotient by half a step each: 3 x 2^-23 of the
+    result; from |h| = 88.7 on e^-h passes the largest float32, and the quotient, at most 89 / 3.4e38, is taken as 0.  tanh GELU the same with
+    e^-2u: u = 0.798 (h + 0.0447 h^3) is off by seven roundings (two constants, four products, a sum), 7 x 2^-24 |2u| of e^-2u.  The products with the identity are
+    exact."""
+    import paper_2503_02495_b200 as uoe
+    h = torch.cat([torch.linspace(-95, 30, 240), torch.linspace(-1, 1, 16)]).view(64, 1, 4)
+    prob = uoe.Problem(B=64, L=1, L_valid=1, d=4, n=1, k=1, m=1, c=1, d_e=4, act=act, gate=False, residual=False, dtype="f32")
+    eye = torch.eye(4, device="cuda").view(1, 4, 4)
+    got = uoe.uoe_mlp_tokens(prob, h.cuda(), torch.zeros(4, 1, device="cuda"), eye, eye.clone()).cpu().double()
+    x = h.double()
+    u2 = x if act == "silu" else 2 * (2 / torch.pi) ** 0.5 * (x + 0.044715 * x ** 3)
+    ref = x / (1 + torch.exp(-u2))
+    rel = 3 * 2.0 ** -23 + (7 * 2.0 ** -24 * u2.abs() if act != "silu" else 0)
+    diff = (got - ref).abs()
+    assert (diff <= rel * ref.abs() + 2.7e-37).all(), float((diff / (rel * ref.abs() + 2.7e-37)).max())
