@@ -66,6 +66,22 @@ __device__ __forceinline__ bool mbar_wait_warp_quick(uint64_t* bar, uint32_t par
     return __all_sync(0xffffffffu, mbar_try_wait(bar, parity)) || mbar_wait_warp(bar, parity, abort_flag, status);
 }
 
+// The same where arrivals come from another CTA of the cluster: what was written before a release there (or before a fence of cluster scope and
+// a relaxed arrival) is visible here.
+__device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ bool mbar_wait_warp_cluster(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* status) {
+    if (__all_sync(0xffffffffu, mbar_try_wait_cluster(bar, parity))) return true;
+    return mbar_wait_warp(bar, parity, abort_flag, status) && __all_sync(0xffffffffu, mbar_try_wait_cluster(bar, parity));
+}
+
 // ---- small asynchronous copies ------------------------------------------------------------------
 __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" :: "r"(dst), "l"(src) : "memory");
@@ -240,12 +256,13 @@ __device__ __forceinline__ float ld_cluster_f32(const float* p, uint32_t rank) {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(cluster_addr) : "memory");
 }
-// The same without release: for hand-overs whose data is not the generic proxy's to order (TMEM, behind tcgen05.wait and tcgen05.fence;
-// shared memory that only the writing SM's asynchronous copies read, behind fence.proxy.async).  A release at cluster scope waits for
-// everything the thread has under way: 2000 cycles, where a hand-over is due every 500.
+// The same without release, for two kinds of hand-over: of TMEM, which tcgen05.wait and tcgen05.fence::before_thread_sync order before the
+// arrival and tcgen05.fence::after_thread_sync behind the wait; and of memory behind a fence of cluster scope of its own (one for several
+// arrivals).
 __device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" :: "r"(cluster_addr) : "memory");
 }
+__device__ __forceinline__ void fence_cluster() { asm volatile("fence.acq_rel.cluster;" ::: "memory"); }
 // tensor loads into this CTA's shared memory whose bytes are counted by a barrier of either CTA of the pair
 __device__ __forceinline__ void tma_load_2d_pair(void* dst, const CUtensorMap* m, int c0, int c1, uint32_t bar_cluster_addr) {
     asm volatile(
