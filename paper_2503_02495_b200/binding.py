@@ -47,8 +47,26 @@ class _Fp8Problem(ctypes.Structure):
     _fields_ = [(f, ctypes.c_int32) for f in ("n", "M", "N", "K", "dtype")] + [("flags", ctypes.c_uint32)]
 
 
+class _Mirror:
+    """A dataclass with a C struct: `ref` passes the struct, which is built again only when a field has changed."""
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        self.__dict__.pop("_ref", None)
+
+    @property
+    def ref(self):
+        ref = self.__dict__.get("_ref")
+        if ref is None:
+            ref = self.__dict__["_ref"] = ctypes.byref(self.c_struct())
+        return ref
+
+    def __getstate__(self):
+        return {k: v for k, v in self.__dict__.items() if k != "_ref"}
+
+
 @dataclass
-class Fp8Problem:
+class Fp8Problem(_Mirror):
     """Mirror of the C struct uoe_fp8_problem: a product of 8-bit operands (dtype: of the result)."""
     n: int
     M: int
@@ -67,7 +85,7 @@ class Fp8Problem:
 
 
 @dataclass
-class Problem:
+class Problem(_Mirror):
     """Mirror of the C struct uoe_problem."""
     B: int
     L: int
@@ -418,9 +436,25 @@ def uoe_route_balance_backward(prob: Problem, x, W_r, p_patch, alpha: float, dlo
 
 def _here(t):
     """The library works on the current device: a tensor of another one is refused."""
-    assert t.is_cuda, "tensors must be contiguous CUDA tensors"
-    if t.device.index != torch.cuda.current_device():
+    dev = t.get_device()
+    assert dev >= 0, "tensors must be contiguous CUDA tensors"
+    if dev != torch.cuda.current_device():
         raise ValueError(f"tensors on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
+
+
+_OPTIONAL = ("b1", "b2", "expert_offsets")
+
+
+def _args(dev, *args):
+    """Every (name, tensor, type, elements): there (or optional), contiguous, on device `dev`, of that type and size.  The library sees nothing but
+    addresses, so that what this lets through is read or written in full."""
+    for name, t, dtype, numel in args:
+        if t is None:
+            assert name in _OPTIONAL, f"{name} is missing"
+        elif t.get_device() != dev or t.dtype is not dtype or t.numel() != numel or not t.is_contiguous():
+            _here(t)
+            raise AssertionError(f"{name}: expected {numel} contiguous elements of {dtype}, got {tuple(t.shape)} of {t.dtype}"
+                                 f"{'' if t.is_contiguous() else ', not contiguous'}")
 
 
 def uoe_fp8_quantize(x, layout: str, q=None, scale=None):
@@ -438,9 +472,8 @@ def uoe_fp8_quantize(x, layout: str, q=None, scale=None):
     s_shape = (*lead, blk(inner), rows) if layout in ("rows", "cols") else (*lead, blk(rows), blk(inner))
     q = q if q is not None else torch.empty(shape, dtype=torch.float8_e4m3fn, device=x.device)
     scale = scale if scale is not None else torch.empty(s_shape, dtype=torch.float32, device=x.device)
-    _contig(q, torch.float8_e4m3fn)
-    _contig(scale, torch.float32)
     assert tuple(q.shape) == shape and tuple(scale.shape) == s_shape, f"expected q {shape} and scale {s_shape}"
+    _args(x.get_device(), ("q", q, torch.float8_e4m3fn, q.numel()), ("scale", scale, torch.float32, scale.numel()))
     st = _lib.uoe_fp8_quantize(lead[0] if lead else 1, R, C, UOE_BF16 if x.dtype == torch.bfloat16 else UOE_F32, FP8_LAYOUTS[layout],
                                _ptr(x), _ptr(q), _ptr(scale), _stream())
     _check(st, "uoe_fp8_quantize")
@@ -454,15 +487,15 @@ def uoe_fp8_transpose(x, q=None):
     _here(x)
     shape = (*x.shape[:-2], x.shape[-1], x.shape[-2])
     q = q if q is not None else torch.empty(shape, dtype=torch.float8_e4m3fn, device=x.device)
-    _contig(q, torch.float8_e4m3fn)
     assert tuple(q.shape) == shape, f"expected q {shape}"
+    _args(x.get_device(), ("q", q, torch.float8_e4m3fn, q.numel()))
     st = _lib.uoe_fp8_transpose(x.shape[0] if x.dim() == 3 else 1, x.shape[-2], x.shape[-1], _ptr(x), _ptr(q), _stream())
     _check(st, "uoe_fp8_transpose")
     return q
 
 
 def uoe_fp8_workspace_bytes(prob: Fp8Problem) -> int:
-    return int(_lib.uoe_fp8_workspace_bytes(ctypes.byref(prob.c_struct())))
+    return int(_lib.uoe_fp8_workspace_bytes(prob.ref))
 
 
 def alloc_fp8_workspace(prob: Fp8Problem, device="cuda") -> torch.Tensor:
@@ -482,30 +515,29 @@ def _fp8_laid_out(t):
     return uoe_fp8_transpose(t.transpose(-1, -2))
 
 
-def _fp8_operand(t, scale, shape, s_shape):
-    _contig(t, torch.float8_e4m3fn)
-    _contig(scale, torch.float32)
-    assert t.numel() == shape[0] * shape[1] * shape[2] and scale.numel() == s_shape[0] * s_shape[1] * s_shape[2], \
-        f"expected values {shape} and scales {s_shape}, got {tuple(t.shape)} and {tuple(scale.shape)}"
+def _fp8_rows(t, Kp):
+    """Rows of Kp values, or all of them flat.  (A matrix that lies the other way round has the right number of elements, too.)"""
+    assert t.size(-1) == Kp or t.dim() < 2, f"expected rows of {Kp} values, got {tuple(t.shape)}"
 
 
 def uoe_fp8_gemm(prob: Fp8Problem, A, a_scale, W, w_scale, expert_offsets=None, C=None, ws=None, check: bool = True):
     """C [M,N] = rows A times the weights of each row's expert (8-bit operands, see uoe.h).  Without C a new tensor is returned, zero
     behind the last region.  A and W may be transposes of contiguous tensors; the call then lays their values out first."""
-    _here(A)
+    n, M, N, Kb, dev, dt = prob.n, prob.M, prob.N, -(-prob.K // UOE_FP8_BLOCK), torch.cuda.current_device(), prob.torch_dtype
+    Kp = Kb * UOE_FP8_BLOCK
+    if C is None or ws is None:
+        _here(A)
     A, W = _fp8_laid_out(A), _fp8_laid_out(W)
-    blk = lambda v: -(-v // UOE_FP8_BLOCK)
-    Kb, Nb = blk(prob.K), blk(prob.N)
-    _fp8_operand(A, a_scale, (1, prob.M, Kb * UOE_FP8_BLOCK), (1, Kb, prob.M))
-    _fp8_operand(W, w_scale, (prob.n, prob.N, Kb * UOE_FP8_BLOCK), (prob.n, Nb, Kb))
-    _contig(expert_offsets, torch.int32)
     if C is None:
-        C = (torch.empty if expert_offsets is None else torch.zeros)(prob.M, prob.N, dtype=prob.torch_dtype, device=A.device)
-    _contig(C, prob.torch_dtype)
-    assert C.numel() == prob.M * prob.N and (expert_offsets is None or expert_offsets.numel() == prob.n + 1)
+        C = (torch.empty if expert_offsets is None else torch.zeros)(M, N, dtype=dt, device=A.device)
     ws = ws if ws is not None else alloc_fp8_workspace(prob, A.device)
-    st = _lib.uoe_fp8_gemm(ctypes.byref(prob.c_struct()), _ptr(A), _ptr(a_scale), _ptr(W), _ptr(w_scale), _ptr(expert_offsets), _ptr(C),
-                           _ptr(ws), ws.numel(), _stream())
+    _args(dev, ("A", A, torch.float8_e4m3fn, M * Kp), ("a_scale", a_scale, torch.float32, Kb * M), ("W", W, torch.float8_e4m3fn, n * N * Kp),
+          ("w_scale", w_scale, torch.float32, n * -(-N // UOE_FP8_BLOCK) * Kb), ("expert_offsets", expert_offsets, torch.int32, n + 1),
+          ("C", C, dt, M * N), ("ws", ws, ws.dtype, ws.numel()))
+    _fp8_rows(A, Kp)
+    _fp8_rows(W, Kp)
+    st = _lib.uoe_fp8_gemm(prob.ref, A.data_ptr(), a_scale.data_ptr(), W.data_ptr(), w_scale.data_ptr(), _ptr(expert_offsets), C.data_ptr(),
+                           ws.data_ptr(), ws.numel(), _stream())
     _check(st, "uoe_fp8_gemm")
     if check:
         _check(uoe_read_device_status(ws), "uoe_fp8_gemm (device)")
@@ -515,40 +547,58 @@ def uoe_fp8_gemm(prob: Fp8Problem, A, a_scale, W, w_scale, expert_offsets=None, 
 def uoe_fp8_wgrad(prob: Fp8Problem, A, a_scale, B, b_scale, expert_offsets=None, dW=None, ws=None, check: bool = True):
     """dW [n,M,N] float32 = A B^T over the rows of each expert's region (8-bit operands, see uoe.h).  A and B may be transposes of contiguous
     tensors, as quantising by columns without turning leaves them; the call then lays their values out first."""
-    _here(A)
+    n, M, N, Kb, dev = prob.n, prob.M, prob.N, -(-prob.K // UOE_FP8_BLOCK), torch.cuda.current_device()
+    Kp = Kb * UOE_FP8_BLOCK
+    if dW is None or ws is None:
+        _here(A)
     A, B = _fp8_laid_out(A), _fp8_laid_out(B)
-    Kb = -(-prob.K // UOE_FP8_BLOCK)
-    _fp8_operand(A, a_scale, (1, prob.M, Kb * UOE_FP8_BLOCK), (1, Kb, prob.M))
-    _fp8_operand(B, b_scale, (1, prob.N, Kb * UOE_FP8_BLOCK), (1, Kb, prob.N))
-    _contig(expert_offsets, torch.int32)
-    dW = dW if dW is not None else torch.empty(prob.n, prob.M, prob.N, dtype=torch.float32, device=A.device)
-    _contig(dW, torch.float32)
-    assert dW.numel() == prob.n * prob.M * prob.N and (expert_offsets is None or expert_offsets.numel() == prob.n + 1)
+    dW = dW if dW is not None else torch.empty(n, M, N, dtype=torch.float32, device=A.device)
     ws = ws if ws is not None else alloc_fp8_workspace(prob, A.device)
-    st = _lib.uoe_fp8_wgrad(ctypes.byref(prob.c_struct()), _ptr(A), _ptr(a_scale), _ptr(B), _ptr(b_scale), _ptr(expert_offsets), _ptr(dW),
-                            _ptr(ws), ws.numel(), _stream())
+    _args(dev, ("A", A, torch.float8_e4m3fn, M * Kp), ("a_scale", a_scale, torch.float32, Kb * M), ("B", B, torch.float8_e4m3fn, N * Kp),
+          ("b_scale", b_scale, torch.float32, Kb * N), ("expert_offsets", expert_offsets, torch.int32, n + 1),
+          ("dW", dW, torch.float32, n * M * N), ("ws", ws, ws.dtype, ws.numel()))
+    _fp8_rows(A, Kp)
+    _fp8_rows(B, Kp)
+    st = _lib.uoe_fp8_wgrad(prob.ref, A.data_ptr(), a_scale.data_ptr(), B.data_ptr(), b_scale.data_ptr(), _ptr(expert_offsets), dW.data_ptr(),
+                            ws.data_ptr(), ws.numel(), _stream())
     _check(st, "uoe_fp8_wgrad")
     if check:
         _check(uoe_read_device_status(ws), "uoe_fp8_wgrad (device)")
     return dW
 
 
-def _fp8_weights(prob: Problem, W1, s1, W2, s2):
-    blk = lambda v: -(-v // UOE_FP8_BLOCK)
-    db, eb = blk(prob.d), blk(prob.d_e)
-    _fp8_operand(W1, s1, (prob.n, prob.d_e, db * UOE_FP8_BLOCK), (prob.n, eb, db))
-    _fp8_operand(W2, s2, (prob.n, prob.d, eb * UOE_FP8_BLOCK), (prob.n, db, eb))
+def _weight_args(prob: Problem, W1, s1, W2, s2):
+    """The two layers' weights in the problem's type, or 8-bit with their scales."""
+    n, d, d_e = prob.n, prob.d, prob.d_e
+    if s1 is None and s2 is None:
+        return ("W1", W1, prob.torch_dtype, n * d * d_e), ("W2", W2, prob.torch_dtype, n * d_e * d)
+    assert s1 is not None and s2 is not None, "8-bit weights need the scales of both layers"
+    db, eb = -(-d // UOE_FP8_BLOCK), -(-d_e // UOE_FP8_BLOCK)
+    return (("W1", W1, torch.float8_e4m3fn, n * d_e * db * UOE_FP8_BLOCK), ("s1", s1, torch.float32, n * eb * db),
+            ("W2", W2, torch.float8_e4m3fn, n * d * eb * UOE_FP8_BLOCK), ("s2", s2, torch.float32, n * db * eb))
+
+
+def _routing_args(prob: Problem, r: Routing, scores: bool):
+    pairs, i32, f32 = prob.B * prob.k, torch.int32, torch.float32
+    a = (("expert_idx", r.expert_idx, i32, pairs), ("patch_idx", r.patch_idx, i32, pairs * prob.c), ("gate", r.gate, f32, pairs * prob.c),
+         ("routing's expert_offsets", r.expert_offsets, i32, prob.n + 1))
+    if scores:
+        a += (("p_samp", r.p_samp, f32, prob.B * prob.n), ("p_patch", r.p_patch, f32, prob.B * prob.n * prob.m))
+    return a
 
 
 def uoe_mlp_forward_fp8(prob: Problem, x, W1, s1, W2, s2, r: Routing, b1=None, b2=None, y=None, ws=None, check: bool = True):
     """uoe_mlp_forward on 8-bit weights: (W1, s1), (W2, s2) = uoe_fp8_quantize(W1 [n,d,d_e], "blocks_t"), (W2 [n,d_e,d], "blocks_t")."""
-    for t in (x, b1, b2):
-        _contig(t, prob.torch_dtype)
     _here(x)
-    _fp8_weights(prob, W1, s1, W2, s2)
+    assert s1 is not None and s2 is not None, "8-bit weights need the scales of both layers"
     y = y if y is not None else torch.empty_like(x)
     ws = ws if ws is not None else alloc_workspace(prob, UOE_OP_MLP_FWD_FP8, x.device)
-    st = _lib.uoe_mlp_forward_fp8(ctypes.byref(prob.c_struct()), _ptr(x), _ptr(W1), _ptr(s1), _ptr(W2), _ptr(s2), _ptr(b1), _ptr(b2),
+    dt, size, n = prob.torch_dtype, prob.B * prob.L * prob.d, prob.n
+    _args(x.get_device(), ("x", x, dt, size), ("y", y, dt, size), ("b1", b1, dt, n * prob.d_e), ("b2", b2, dt, n * prob.d),
+          ("ws", ws, ws.dtype, ws.numel()), *_weight_args(prob, W1, s1, W2, s2), *_routing_args(prob, r, False))
+    _fp8_rows(W1, -(-prob.d // UOE_FP8_BLOCK) * UOE_FP8_BLOCK)
+    _fp8_rows(W2, -(-prob.d_e // UOE_FP8_BLOCK) * UOE_FP8_BLOCK)
+    st = _lib.uoe_mlp_forward_fp8(prob.ref, _ptr(x), _ptr(W1), _ptr(s1), _ptr(W2), _ptr(s2), _ptr(b1), _ptr(b2),
                                   _ptr(r.expert_idx), _ptr(r.patch_idx), _ptr(r.gate), _ptr(r.expert_offsets), _ptr(y), _ptr(ws),
                                   ws.numel(), _stream())
     _check(st, "uoe_mlp_forward_fp8")
@@ -561,17 +611,16 @@ def uoe_mlp_tokens(prob: Problem, x, W_r, W1, W2, s1=None, s2=None, b1=None, b2=
                    check: bool = True):
     """Router, experts and combine of a UoME layer for up to 64 tokens x [B,1,d] (or [B,d]) in two kernels; prob has L = m = c = 1.
     Weights in the problem's type, or 8-bit with their scales s1, s2 as for uoe_mlp_forward_fp8.  Fills r when given."""
-    for t in (x, W_r, b1, b2):
-        _contig(t, prob.torch_dtype)
     _here(x)
-    if s1 is None:
-        _contig(W1, prob.torch_dtype)
-        _contig(W2, prob.torch_dtype)
-    else:
-        _fp8_weights(prob, W1, s1, W2, s2)
     y = y if y is not None else torch.empty_like(x)
     ws = ws if ws is not None else alloc_workspace(prob, UOE_OP_MLP_TOKENS, x.device)
-    st = _lib.uoe_mlp_tokens(ctypes.byref(prob.c_struct()), _ptr(x), _ptr(W_r), _ptr(W1), _ptr(s1), _ptr(W2), _ptr(s2), _ptr(b1), _ptr(b2),
+    dt, size, n = prob.torch_dtype, prob.B * prob.L * prob.d, prob.n
+    _args(x.get_device(), ("x", x, dt, size), ("y", y, dt, size), ("W_r", W_r, dt, prob.d * n), ("b1", b1, dt, n * prob.d_e), ("b2", b2, dt, n * prob.d),
+          ("ws", ws, ws.dtype, ws.numel()), *_weight_args(prob, W1, s1, W2, s2), *(_routing_args(prob, r, True) if r is not None else ()))
+    if s1 is not None:
+        _fp8_rows(W1, -(-prob.d // UOE_FP8_BLOCK) * UOE_FP8_BLOCK)
+        _fp8_rows(W2, -(-prob.d_e // UOE_FP8_BLOCK) * UOE_FP8_BLOCK)
+    st = _lib.uoe_mlp_tokens(prob.ref, _ptr(x), _ptr(W_r), _ptr(W1), _ptr(s1), _ptr(W2), _ptr(s2), _ptr(b1), _ptr(b2),
                              _routing_struct(r), _ptr(y), _ptr(ws), ws.numel(), _stream())
     _check(st, "uoe_mlp_tokens")
     if check:
@@ -598,8 +647,8 @@ def alloc_block_workspace(att: Problem | None, mlp: Problem | None, device="cuda
 def _routing_struct(r: Routing | None):
     if r is None:
         return None
-    return ctypes.byref(_Routing(*(t.data_ptr() for t in (r.expert_idx, r.patch_idx, r.gate, r.p_samp, r.p_patch,
-                                                          r.expert_offsets))))
+    return ctypes.byref(_Routing(r.expert_idx.data_ptr(), r.patch_idx.data_ptr(), r.gate.data_ptr(), r.p_samp.data_ptr(), r.p_patch.data_ptr(),
+                                 r.expert_offsets.data_ptr()))
 
 
 def uoe_block_forward(att: Problem | None, mlp: Problem | None, x, weights: dict, r_att: Routing | None = None,
