@@ -141,7 +141,7 @@ fp8_patch_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                 for (int q = 0; q < CW; ++q) sum[q] = 0.f;
             }
             for (int i = 0; i < w->count && !stop; ++i) {
-                const float gate = w->gate[i];
+                const float gate = real ? w->gate[i] : 0.f;          // (on a pad token 0 times 0 is added, whatever the patch's gate is)
                 if (!mbar_wait_warp_quick(&ctl->tfull, phase, abort_flag, p.status)) { stop = true; break; }
                 phase ^= 1;
                 tc_fence_after();
