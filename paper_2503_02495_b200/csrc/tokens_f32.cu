@@ -50,12 +50,19 @@ __device__ __forceinline__ void accumulate(float (&c)[8 * TG][4], const float* A
 #pragma unroll
         for (int i = 0; i < 8; ++i) *(float*)(b + (k8 + i) * Sm::PITCH + 4 * tok) = f[i];
     };
-    // (columns past the matrix are other columns again, whose sums nobody takes; rows past it meet activations of zero)
+    // (columns past the matrix are other columns again, whose sums nobody takes; rows past it are zeros: the last row in their place would make
+    // NaN of an infinity there, times activations of zero)
     const float* w0 = W + min(c0 + 4 * (lane & 15), N - 4);
     uint4 w[2][8];
     auto load = [&](uint4* o, int kk) {
+        const float* r = w0 + (size_t)(kk + 16 * warp + h) * N;
+        if (kk + kStep <= K) {                                 // (looking at every row by itself: eight tokens, d = 4096, 192 -> 202 us)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = ld_stream16(w0 + (size_t)min(kk + 16 * warp + 2 * i + h, K - 1) * N);
+            for (int i = 0; i < 8; ++i) o[i] = ld_stream16(r + (size_t)(2 * i) * N);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[i] = kk + 16 * warp + h + 2 * i < K ? ld_stream16(r + (size_t)(2 * i) * N) : make_uint4(0, 0, 0, 0);
+        }
     };
     load(w[0], k0);
     hold(k0);

@@ -44,3 +44,19 @@ def test_float32_activation_keeps_its_bits(act):
     rel = 3 * 2.0 ** -23 + (7 * 2.0 ** -24 * u2.abs() if act != "silu" else 0)
     diff = (got - ref).abs()
     assert (diff <= rel * ref.abs() + 2.7e-37).all(), float((diff / (rel * ref.abs() + 2.7e-37)).max())
+
+
+@pytest.mark.parametrize("weights", ["bf16", "f32"])
+@pytest.mark.parametrize("layer", ["W1", "W2"])
+@pytest.mark.parametrize("d, d_e", [(64, 40), (136, 72), (320, 264)])
+def test_an_infinite_weight_in_the_last_row_is_an_infinity(weights, layer, d, d_e):
+    """No step of the contraction past the matrix may meet it: 0 * Inf would make a NaN of it."""
+    c = _case(5, d, d_e, 2, 2, weights, act="identity", gate=False)
+    m = make(c)
+    m[layer][:, -1, 0] = float("inf")
+    got = run(c, m)[1]().cpu().double().view(5, d)
+    x, W1, W2 = m["x"].double().view(5, d), m["W1"].double(), m["W2"].double()
+    ref = x + sum((x @ W1[i]) @ W2[i] for i in range(2))
+    assert torch.isinf(ref).any() and torch.equal(torch.isnan(ref), torch.isnan(got))
+    inf = torch.isinf(ref)
+    assert torch.equal(got[inf], ref[inf]) and torch.isfinite(got[~inf & ~torch.isnan(ref)]).all()
