@@ -67,7 +67,7 @@ __device__ __forceinline__ void load_regions(Regions& g, const Fp8Args& a, int m
 __device__ __forceinline__ uint32_t exponent_word(float s, bool there, bool& bad) {
     const uint32_t b = there ? __float_as_uint(s) : 0x3f800000u, e = b >> 23;
     const bool pow2 = (b & 0x7fffffu) == 0 && e - 1 < 254u;
-    bad |= !pow2 && e != 255;
+    bad |= !pow2 && (b & 0x7fffffffu) <= 0x7f800000u;           // an infinity is no power of two; NaN of either sign
     return __byte_perm(pow2 ? e : 255u, 0, 0);
 }
 

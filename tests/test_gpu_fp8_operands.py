@@ -86,3 +86,22 @@ def test_wgrad_of_turned_operands_captured():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(dW, want)
+
+
+@pytest.mark.parametrize("scale, status", [(float("inf"), 8), (-float("inf"), 8), (float("nan"), 0), (-float("nan"), 0)])
+def test_a_scale_that_is_not_finite(scale, status):
+    """NaN is what the quantisation writes for a block without a finite maximum, whatever its sign bit; an infinity is no power of two."""
+    import math
+    import paper_2503_02495_b200 as uoe
+    A, sa = uoe.uoe_fp8_quantize(_rand(1, 200, 300).cuda(), "rows")
+    W, sw = uoe.uoe_fp8_quantize(_rand(2, 1, 64, 300).cuda(), "blocks")
+    prob = uoe.Fp8Problem(n=1, M=200, N=64, K=300)
+    ref = uoe.uoe_fp8_gemm(prob, A, sa, W, sw)
+    bits = {8: 0x7f800000, 0: 0x7fc00000}[status] | (0x80000000 if math.copysign(1, scale) < 0 else 0)
+    sa.view(torch.int32)[1, 150] = bits - (1 << 32) if bits >> 31 else bits
+    C, ws = torch.empty_like(ref), uoe.alloc_fp8_workspace(prob)
+    uoe.uoe_fp8_gemm(prob, A, sa, W, sw, C=C, ws=ws, check=False)
+    assert uoe.uoe_read_device_status(ws) == status
+    assert torch.isnan(C[150]).all()
+    C[150] = ref[150]
+    assert torch.equal(C, ref)
