@@ -140,6 +140,8 @@ size_t uoe_workspace_bytes(const uoe_problem* prob, int op);
  *   patch_idx[b,s,:] = for the s-th chosen expert i, the min(c, #patches with a real token) patches
  *                      with the largest p_patch[b,i,:], ascending; unused slots are -1            (Eq. 17)
  *                      (with UOE_FLAG_DYNAMIC_C also at most the sample's own capacity, Eq. 15-16)
+ *   (gates that are NaN, as a NaN or an infinity in x makes them, come last in either order: every sample gets k experts, every
+ *   expert min(c, ..) patches, whatever x holds)
  *   gate[b,s,u]     = p_samp[b,i] * p_patch[b,i,patch] with UOE_FLAG_GATE, else 1; 0 in unused slots
  *   expert_offsets  = row offsets of the per-expert regions (see "Routed buffers")               (Eq. 23)
  * All arguments except prob are device pointers.  x [B,L,d] and W_r [d,n] have prob->dtype;

@@ -18,6 +18,11 @@ namespace {
 
 constexpr int kScoreThreads = 256;
 
+// A gate (0 .. 1, or NaN) as selection orders it.  NaN compares with nothing: beaten by none, every NaN gate would be selected.  So it becomes a
+// negative number, behind every gate and, by `place`, in order among its like.
+__device__ __forceinline__ float order_key(float p, int place) { return p == p ? p : (float)(-1 - place); }
+__device__ __forceinline__ float gate_of_key(float key) { return key < 0.f ? __int_as_float(0x7fffffff) : key; }
+
 // Selection for sample b by one CTA of NT threads (all threads call).  pp: n*m floats of shared memory.
 // Written for a short dependent chain (the router is latency-bound on all but the largest inputs): a CTA barrier between
 // the first phase and the others, the ticket under the last of them.
@@ -92,7 +97,7 @@ __device__ void select_sample(float* pp, const float* __restrict__ partial, int 
             for (int o = np2 >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
             // (lanes outside the problem divide 1 by 1: a zero operand would send the whole warp through the division's slow path)
             const float pr = (valid ? e : 1.f) / (valid ? sum : 1.f);
-            if (valid) pp[i * m + j] = pr;
+            if (valid) pp[i * m + j] = order_key(pr, j);
             if (dynamic_c) {                        // Eq. 15: every real patch goes to its k best experts (ties: lower index)
                 int rank = 0;
                 for (int q = 0; q < n; ++q) {
@@ -108,7 +113,7 @@ __device__ void select_sample(float* pp, const float* __restrict__ partial, int 
     __syncthreads();
 
     // ---- B ----
-    for (int idx = tid; idx < n * m; idx += NT) p_patch[(size_t)b * n * m + idx] = pp[idx];
+    for (int idx = tid; idx < n * m; idx += NT) p_patch[(size_t)b * n * m + idx] = gate_of_key(pp[idx]);
     float ps;                                   // this lane's expert: sample gate
     unsigned chosen;                            // the chosen experts
     {
@@ -128,11 +133,12 @@ __device__ void select_sample(float* pp, const float* __restrict__ partial, int 
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         ps = (lane < n ? e : 1.f) / sum;        // (lanes past the experts: not zero, for the division's fast path)
         // Eq. 22: rank = number of experts that beat this one (larger value, or equal with lower index)
+        const float key = order_key(ps, lane);
         int rank = 0;
         if (!all_experts)
             for (int i = 0; i < n; ++i) {
-                const float w = __shfl_sync(0xffffffffu, ps, i);
-                rank += (w > ps) || (w == ps && i < lane);
+                const float w = __shfl_sync(0xffffffffu, key, i);
+                rank += (w > key) || (w == key && i < lane);
             }
         const bool pick = lane < n && rank < k;
         chosen = __ballot_sync(0xffffffffu, pick);
@@ -179,7 +185,7 @@ __device__ void select_sample(float* pp, const float* __restrict__ partial, int 
             const bool pick = valid && rank < take;
             const unsigned mask = __ballot_sync(0xffffffffu, pick);
             const int pos = before + __popc(mask & ((1u << lane) - 1u));
-            const float g = use_gate ? p_i * v : 1.0f;
+            const float g = use_gate ? p_i * gate_of_key(v) : 1.0f;
             if (pick) {
                 out_idx[pos] = j;
                 out_gate[pos] = g;
