@@ -105,3 +105,37 @@ def test_a_scale_that_is_not_finite(scale, status):
     assert torch.isnan(C[150]).all()
     C[150] = ref[150]
     assert torch.equal(C, ref)
+
+
+@pytest.mark.parametrize("any_scale", [False, True])
+@pytest.mark.parametrize("rows, M", [(40, 40 + 88), (40, 300), (300, 600)])
+def test_one_expert_with_offsets(rows, M, any_scale):
+    """n = 1 with offsets: the region's rows and no others, whichever kernel would take all M of them."""
+    import paper_2503_02495_b200 as uoe
+    end = -(-rows // BLOCK) * BLOCK
+    x = torch.zeros(M, 260)
+    x[:rows] = _rand(1, rows, 260, wide=True)
+    A, sa = uoe.uoe_fp8_quantize(x.cuda(), "rows")
+    W, sw = uoe.uoe_fp8_quantize(_rand(2, 1, 140, 260).cuda(), "blocks")
+    C = torch.full((M, 140), -3.0, device="cuda")
+    prob = uoe.Fp8Problem(n=1, M=M, N=140, K=260, dtype="f32", any_scale=any_scale)
+    uoe.uoe_fp8_gemm(prob, A, sa, W, sw, torch.tensor([0, end], dtype=torch.int32, device="cuda"), C=C)
+    a, w = _vec_values(A.cpu(), sa.cpu())[:end], _blk_values(W[0].cpu(), sw[0].cpu())
+    _close(C[:end], a @ w.t(), _gamma(3) * (a.abs() @ w.abs().t()), "f32")
+    assert (C[end:] == -3).all()
+
+
+@pytest.mark.parametrize("any_scale", [False, True])
+@pytest.mark.parametrize("counts, M, N", [([6500, 1], 130, 77), ([300, 0, 128, 500, 1000, 129, 1, 700], 1300, 1000), ([130, 0, 400, 1], 77, 333)])
+def test_wgrad_has_the_same_bits_each_time(counts, M, N, any_scale):
+    import paper_2503_02495_b200 as uoe
+    off = _regions(counts)
+    x, dy = torch.zeros(off[-1], M), torch.zeros(off[-1], N)
+    for o, cnt in zip(off, counts):
+        x[o:o + cnt], dy[o:o + cnt] = _rand(o + 1, cnt, M, wide=True), _rand(o + 2, cnt, N)
+    q = [*uoe.uoe_fp8_quantize(x.cuda(), "cols"), *uoe.uoe_fp8_quantize(dy.cuda(), "cols")]
+    prob = uoe.Fp8Problem(n=len(counts), M=M, N=N, K=off[-1], dtype="f32", any_scale=any_scale)
+    o = torch.tensor(off, dtype=torch.int32, device="cuda")
+    ref = uoe.uoe_fp8_wgrad(prob, *q, o)
+    for _ in range(5):
+        assert torch.equal(ref, uoe.uoe_fp8_wgrad(prob, *q, o))

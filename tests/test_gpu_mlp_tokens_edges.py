@@ -60,3 +60,60 @@ def test_an_infinite_weight_in_the_last_row_is_an_infinity(weights, layer, d, d_
     assert torch.isinf(ref).any() and torch.equal(torch.isnan(ref), torch.isnan(got))
     inf = torch.isinf(ref)
     assert torch.equal(got[inf], ref[inf]) and torch.isfinite(got[~inf & ~torch.isnan(ref)]).all()
+
+
+def _prepared(c, m):
+    """(call(W scales poisoned for one expert or None), problem): one workspace, behind its control block full of NaN patterns."""
+    import paper_2503_02495_b200 as uoe
+    prob = uoe.Problem(B=c["T"], L=1, L_valid=1, d=c["d"], n=c["n"], k=c["k"], m=1, c=1, d_e=c["d_e"], act=c["act"], gate=c["gate"],
+                       residual=c["residual"], dtype="f32" if c["weights"] == "f32" else "bf16")
+    ws = uoe.alloc_workspace(prob, uoe.UOE_OP_MLP_TOKENS)
+    dev = {q: v.cuda() if v is not None else None for q, v in m.items()}
+
+    def call(x=None, poison=None):
+        W, s = [dev["W1"].clone(), dev["W2"].clone()], [None, None]
+        if c["weights"] == "fp8":
+            W, s = zip(*[uoe.uoe_fp8_quantize(w, "blocks_t") for w in W])
+        for w, q in zip(W, s):
+            if poison is not None:
+                w[poison] = float("nan") if q is None else torch.full(w[poison].shape, 0x7f, dtype=torch.uint8, device="cuda").view(w.dtype)
+                if q is not None:
+                    q[poison] = float("nan")
+        ws[1024:].fill_(255)                            # stale hidden rows, terms and scales: all NaN
+        r = uoe.alloc_routing(prob)
+        y = uoe.uoe_mlp_tokens(prob, dev["x"] if x is None else x.cuda(), dev["Wr"], W[0], W[1], s1=s[0], s2=s[1], b1=dev["b1"], b2=dev["b2"], r=r, ws=ws)
+        return y, r
+    return call
+
+
+@pytest.mark.parametrize("weights", ["bf16", "fp8", "f32"])
+@pytest.mark.parametrize("T", [3, 14, 30, 60])
+def test_what_nobody_chose_and_what_a_workspace_held_stay_out(weights, T):
+    c = _case(T, 200, 136, 5, 2, weights, gate=True, seed=T)
+    m = make(c)
+    call = _prepared(c, m)
+    ref, r = call()
+    assert torch.isfinite(ref).all()
+    for bad in range(5):
+        got, r2 = call(poison=bad)
+        assert torch.equal(r2.expert_idx, r.expert_idx)
+        keep = (r.expert_idx != bad).all(1)
+        assert torch.equal(got[keep], ref[keep])
+        assert torch.isnan(got[~keep]).all()
+
+
+@pytest.mark.parametrize("weights", ["bf16", "fp8", "f32"])
+@pytest.mark.parametrize("T, at", [(1, 0), (7, 3), (20, 11), (33, 32), (64, 0)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_a_token_without_an_order_spoils_only_itself(weights, T, at, bad):
+    """Its scores have no order, so it gets the first k experts; the others' bits stay."""
+    c = _case(T, 136, 72, 6, 2, weights)
+    m = make(c)
+    call = _prepared(c, m)
+    ref, r = call()
+    x = m["x"].clone()
+    x[at, 0, 5] = bad
+    got, r2 = call(x=x)
+    keep = torch.arange(T) != at
+    assert torch.equal(got[keep], ref[keep]) and torch.equal(r2.expert_idx[keep], r.expert_idx[keep])
+    assert torch.isnan(got[at]).all() and r2.expert_idx[at].tolist() == [0, 1]
