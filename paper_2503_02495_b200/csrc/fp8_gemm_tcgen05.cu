@@ -8,7 +8,6 @@
 // kernel).  A persistent CTA (pair) per SM (two) walks the tiles, 128 x BN or, by a pair of CTAs (cta_group::2), 256 x 256:
 //   warp 0       TMA producer: a stage is one block of the contraction, 128 bytes of every row of A and of B (128-byte swizzle)
 //   warp 1       MMA issuer: four steps of 32 per stage
-//   warps 1..3   of a pair's second CTA: pass its scales on to the first one's issuer (pair_scales.h)
 //   warps 4..7   the stages' scales in turn: float32 -> exponent byte -> shared memory, in the order in which the issuer's copies put
 //                them into TMEM.  A scale holds for the whole stage, so its byte fills the word and the four steps need no index.
 //   warps 8..15  write-out: a warp has 32 rows (its TMEM lane quarter) and half of the columns, all of them in registers before it
@@ -18,7 +17,6 @@
 // source patch, their scales by their source rows.
 // Regions of experts are whole 128-row blocks; the second half of a pair's last tile may be rows of nobody, which are not stored.
 #include "fp8_tile.cuh"
-#include "pair_scales.h"
 #include "tc.cuh"
 #include "tmap.cuh"
 
@@ -38,7 +36,6 @@ template <int BN, bool PAIR> struct Cfg {
     static constexpr int TILE = PAIR ? 2 * BM : BM;
     static constexpr int A_BYTES = BM * kQ, B_BYTES = BN_CTA * kQ, STAGE = A_BYTES + B_BYTES;
     static constexpr int STAGES = BN_CTA == 256 ? 4 : 6;
-    static_assert(!PAIR || STAGES == kPairStages, "stages of a pair");
     static_assert(STAGES >= 4, "four warps in turn: none looks for a stage's last use by parity two uses ahead");
     static constexpr int NACC = BN == 256 ? 1 : 2;
     static constexpr int CW = BN / 2;
@@ -50,7 +47,6 @@ template <int BN, bool PAIR> struct Cfg {
 
 struct Ctl {
     uint64_t full[8], empty[8], tfull[2], tempty[2];
-    uint64_t sready[8];               // pair, second CTA: scales of a stage are in shared memory
     uint32_t tmem_base;
     int abort_flag;
     Regions reg;
@@ -78,7 +74,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     constexpr int CTAS = PAIR ? 2 : 1;
     if (threadIdx.x == 0) {
         // (a pair's products are issued by rank 0, on whose barriers both CTAs' copies, scales and write-outs arrive)
-        for (int s = 0; s < Cf::STAGES; ++s) { mbar_init(&ctl->full[s], 1 + CTAS); mbar_init(&ctl->empty[s], 1); mbar_init(&ctl->sready[s], 1); }
+        for (int s = 0; s < Cf::STAGES; ++s) { mbar_init(&ctl->full[s], 1 + CTAS); mbar_init(&ctl->empty[s], 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(&ctl->tfull[i], 1); mbar_init(&ctl->tempty[i], CTAS * Cf::EPI_WARPS); }
         ctl->abort_flag = 0;
         fence_barrier_init();
@@ -214,7 +210,14 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                     // (every lane's words are in place for the copy, which reads this SM's shared memory, once its fence is behind it)
                     fence_async_smem();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(PAIR && rank ? &ctl->sready[stage] : &ctl->full[stage]);
+                    if (lane == 0) {
+                        if (PAIR && rank) {                  // to the other CTA's issuer
+                            fence_release_smem();
+                            mbar_arrive_cluster_relaxed(map_to_cta(&ctl->full[stage], 0));
+                        } else {
+                            mbar_arrive(&ctl->full[stage]);
+                        }
+                    }
                 }
                 if (++stage == Cf::STAGES) { stage = 0; phase ^= 1; }
             }
@@ -310,29 +313,6 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 else mma_commit(el, &ctl->tfull[acc]);
                 if (++acc == Cf::NACC) { acc = 0; acc_phase ^= 1; }
             }
-        } else if (PAIR && rank == 1) {
-            int stage = 0, e = 0;
-            uint32_t phase = 0;
-            bool stop = false;
-            auto pass_on = [&](int to) {                      // the blocks of this warp's group, up to the one in stage `to`
-                if (lane == 0) {
-                    fence_cluster();                          // (the scale warps' words, seen by the waits before it, among what it orders)
-                    for (int q = pass_first(to); q <= to; ++q) mbar_arrive_cluster_relaxed(map_to_cta(&ctl->full[q], 0));
-                }
-                __syncwarp();
-            };
-            for (int tile = worker; tile < total && !stop; tile += workers) {
-                const Tile t = locate(tile, e);
-                for (int kb = 0; kb < t.kbs; ++kb) {
-                    if (pass_warp(stage) == warp - 1) {
-                        if (!mbar_wait_warp_quick(&ctl->sready[stage], phase, abort_flag, a.status)) { stop = true; break; }
-                        if (pass_now(stage, false)) pass_on(stage);
-                    }
-                    if (++stage == Cf::STAGES) { stage = 0; phase ^= 1; }
-                }
-            }
-            // a group that the line's end left half full
-            if (!stop && stage > pass_first(stage) && pass_warp(stage) == warp - 1) pass_on(stage - 1);
         }
     }
     if (warp >= 8 && lane == 0) bulk_wait_all();        // this warp's tensor stores are complete

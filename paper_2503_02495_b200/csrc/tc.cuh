@@ -66,8 +66,8 @@ __device__ __forceinline__ bool mbar_wait_warp_quick(uint64_t* bar, uint32_t par
     return __all_sync(0xffffffffu, mbar_try_wait(bar, parity)) || mbar_wait_warp(bar, parity, abort_flag, status);
 }
 
-// The same where arrivals come from another CTA of the cluster: what was written before a release there (or before a fence of cluster scope and
-// a relaxed arrival) is visible here.
+// The same where arrivals come from another CTA of the cluster: what was written before a release there (or before such a fence and a
+// relaxed arrival) is visible here.
 __device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t* bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
@@ -257,12 +257,14 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(cluster_addr) : "memory");
 }
 // The same without release, for two kinds of hand-over: of TMEM, which tcgen05.wait and tcgen05.fence::before_thread_sync order before the
-// arrival and tcgen05.fence::after_thread_sync behind the wait; and of memory behind a fence of cluster scope of its own (one for several
-// arrivals).
+// arrival and tcgen05.fence::after_thread_sync behind the wait; and of shared memory behind fence_release_smem.
 __device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" :: "r"(cluster_addr) : "memory");
 }
-__device__ __forceinline__ void fence_cluster() { asm volatile("fence.acq_rel.cluster;" ::: "memory"); }
+// A release at cluster scope of what this CTA wrote to its shared memory, for a relaxed arrival behind it.  (Of all memory, by the arrival itself or by
+// fence.acq_rel.cluster, an SM gets through one in some 550 cycles, where a block of an 8-bit product takes 500: 32768 x 4096 x 1024 135 us, with
+// three warps that pass on two blocks per fence 124, so 117.)
+__device__ __forceinline__ void fence_release_smem() { asm volatile("fence.release.sync_restrict::shared::cta.cluster;" ::: "memory"); }
 // tensor loads into this CTA's shared memory whose bytes are counted by a barrier of either CTA of the pair
 __device__ __forceinline__ void tma_load_2d_pair(void* dst, const CUtensorMap* m, int c0, int c1, uint32_t bar_cluster_addr) {
     asm volatile(
