@@ -244,8 +244,9 @@ transpose_kernel(const uint8_t* __restrict__ x, uint8_t* __restrict__ q, int R, 
 template <typename T>
 uoe_status launch_tile(int layout, int G, int R, int C, const void* x, void* q, float* scale, cudaStream_t s) {
     const int Rb = q_blocks(R), Cb = q_blocks(C), whole = ((size_t)C * sizeof(T)) % 16 == 0;
-    const long long tiles = (long long)G * Rb * Cb;
-    if (tiles > 0x7fffffffll) return UOE_ERR_UNSUPPORTED;
+    // (three factors, past 64 bits together: the first two are looked at alone)
+    const long long tile_rows = (long long)G * Rb, tiles = tile_rows * Cb;
+    if (tile_rows > 0x7fffffffll || tiles > 0x7fffffffll) return UOE_ERR_UNSUPPORTED;
     ProfScope ps("fp8_quantize", s);
     const dim3 grid((unsigned)tiles), block(256);
     if (layout == UOE_FP8_COLS) launch_k(quantize_tile_kernel<T, UOE_FP8_COLS>, grid, block, 0, s, (const T*)x, (uint8_t*)q, scale, R, C, Rb, Cb, whole);
@@ -262,6 +263,7 @@ uoe_status launch_quantize_rows(const void* x, bool bf16, int G, long long rows,
     const int Cb = q_blocks(C), groups = (Cb + kBlocksPerCta - 1) / kBlocksPerCta, whole = ((size_t)C * (bf16 ? 2 : 4)) % 16 == 0;
     // CTAs of a row block: as many as keep some eight per SM; a row's columns are a loop otherwise
     const long long row_ctas = (long long)G * ((rows + kRowsPerCta - 1) / kRowsPerCta);
+    if (row_ctas > 0x7fffffffll) return UOE_ERR_UNSUPPORTED;
     int splits = groups;
     while (splits > 1 && row_ctas * (splits / 2) >= 8ll * sm_count()) splits = (splits + 1) / 2;
     const long long ctas = row_ctas * splits;
@@ -293,7 +295,6 @@ extern "C" uoe_status uoe_fp8_transpose(int32_t G, int32_t R, int32_t C, const v
     if (!x || !q || x == q || !aligned16(x) || !aligned16(q)) return UOE_ERR_INVALID_ARG;
     if (C > 0x7fffffff - kQ) return UOE_ERR_UNSUPPORTED;
     const int Cb = q_blocks(C);
-    // (three factors of up to 2^24: past 64 bits, so that the first two are looked at alone)
     const long long rows = (long long)G * (R / kQ);
     if (rows > 0x7fffffffll || rows * Cb > 0x7fffffffll) return UOE_ERR_UNSUPPORTED;
     cudaStream_t s = (cudaStream_t)cuda_stream;

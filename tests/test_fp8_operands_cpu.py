@@ -12,7 +12,7 @@ def lib():
     ge.build()
     import paper_2503_02495_b200 as uoe
     lib = ctypes.CDLL(uoe.LIB_PATH)
-    lib.uoe_fp8_transpose.restype = ctypes.c_int
+    lib.uoe_fp8_transpose.restype = lib.uoe_fp8_quantize.restype = ctypes.c_int
     return lib
 
 
@@ -38,3 +38,11 @@ def test_layout_of_an_operand_is_told_from_its_strides(monkeypatch):
     assert B._fp8_laid_out(w.transpose(1, 2)).is_contiguous() and seen[1:] == [(3, 128, 40)]
     cut = torch.zeros(77, 512, dtype=torch.uint8)[:, :256]                # neither: left for the check to refuse
     assert B._fp8_laid_out(cut) is cut and len(seen) == 2
+
+
+@pytest.mark.parametrize("layout", [0, 1, 2, 3])
+@pytest.mark.parametrize("sizes", [(1 << 30, 1 << 30, 1 << 30), ((1 << 31) - 1,) * 2 + (1 << 20,), (1 << 21, 1 << 30, 1 << 27)])
+def test_quantise_refuses_what_no_grid_holds(lib, layout, sizes):
+    """The number of CTAs is a product of three factors that passes 64 bits."""
+    G, R, C = sizes
+    assert lib.uoe_fp8_quantize(G, min(R, 0x7fffffff - 128), C, 0, layout, OK_PTR, OTHER, ctypes.c_void_p(1 << 20), None) == 2
