@@ -10,7 +10,8 @@
 //                          shared memory, eight rows of a column in one 8-byte store, swizzled so that neither side meets a bank
 //                          twice.
 //   transpose_kernel       uoe_fp8_transpose: bytes of a quantised operand whose contraction is not contiguous, a CTA per 128 x 128 tile, a
-//                          thread 4 rows x 16 columns: 4 x 4 bytes turned in registers, words swizzled through shared memory.
+//                          thread 4 rows x 16 columns: 4 x 4 bytes turned in registers, words swizzled through shared memory (33920 x 4096 bytes: 50 us, 5.6 TB/s read and
+//                          written).
 #include "fp8.cuh"
 
 namespace uoe {

@@ -73,6 +73,8 @@ extern "C" uoe_status uoe_mlp_forward_fp8(const uoe_problem* prob, const void* x
     if (!any_scale && fp8_patch_can(D))
         return launch_fp8_patch(D, base + W.aq, (float*)(base + W.as), W2, w2_scale, b2, x, y, expert_offsets, P, (prob->flags & UOE_FLAG_GATE) != 0,
                                 (prob->flags & UOE_FLAG_RESIDUAL) != 0, status, s);
+    // z in bfloat16 (off by half a step, 2^-8 of the value, as between uoe_mlp_forward's product and combine): in float32 the combine, which these
+    // bytes bound, would read twice as many
     Fp8Gemm g2{base + W.aq, (float*)(base + W.as), W2, w2_scale, expert_offsets, D.n, D.Rmax, D.d, D.d_e, false, base + W.z, true};
     g2.bias = b2;
     g2.any_scale = any_scale;
